@@ -328,6 +328,73 @@ int freq_destroy(fc_freq* f);
 int table_reorder(const float* src_pinned, float* dst_pinned, const int32_t* inv_rank_host, int64_t num_rows,
                   int32_t dim, void* hip_stream);
 
+/* ---- operators beside the cached table ----
+ * A model has small tables and dense layers beside the one behind the cache: positions, item types, words; norms; gradients
+ * that are clipped together.  These calls work on the caller's device memory, in the model's types, on the stream of their handle; the
+ * results are complete in the order of that stream.  Values are worked out in 32 bits (norms over tensors: 64) and rounded once, to
+ * the type they are stored in.  Rows are `dim` neighbouring elements, `stride` elements apart (stride >= dim), and may start at any element.
+ * Results are reproducible: no sum depends on the order in which workgroups run.  Rows, tokens: below 2^31 - 2^16; dim: up to 2^20. */
+enum {                    /* element types */
+    FC_TYPE_F32 = 0,
+    FC_TYPE_BF16 = 1,
+    FC_TYPE_F16 = 2,
+    FC_TYPE_F8E4M3 = 3,   /* 8 bits: 4 of exponent, 3 of mantissa, no infinities, largest 448 (results of rms_norm_fwd) */
+    FC_TYPE_I8 = 4,       /* results of rms_norm_fwd */
+    FC_TYPE_I32 = 5,      /* ids */
+    FC_TYPE_I64 = 6
+};
+
+typedef struct fc_dense fc_dense; /* opaque: stream, workspace, sticky error; one per stream, not thread-safe */
+
+/* On the current device; hip_stream: hipStream_t (NULL = default stream) of all its calls. */
+int dense_create(void* hip_stream, fc_dense** out);
+/* Allocate now what calls up to these sizes need beyond the caller's memory (token_embed_bwd: max_tokens ids of a table of max_rows rows;
+ * max_dim columns; grad_norm_clip: max_tensors tensors).  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
+ * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured.  Synchronous.  Errors: INVALID_ARG, OOM_DEVICE, HIP. */
+int dense_reserve(fc_dense* d, int64_t max_tokens, int64_t max_rows, int32_t max_dim, int32_t max_tensors);
+/* Wait for the handle's stream and return the sticky error, if any (then clears it): FC_ERR_ID_OUT_OF_RANGE. */
+int dense_check(fc_dense* d);
+/* Waits for the stream, frees the workspace. */
+int dense_destroy(fc_dense* d);
+
+/* Token embedding: out[i, :] = scale * table[ids[i], :] for i in [0, n).
+ *   table, out types F32, BF16 or F16 each; ids I32 or I64.
+ * An id outside [0, num_rows) gives a row of zeros and raises a sticky FC_ERR_ID_OUT_OF_RANGE reported by dense_check. */
+int token_embed_fwd(fc_dense* d, const void* table_dev, int32_t table_type, int64_t table_stride, int64_t num_rows, int32_t dim, const void* ids_dev,
+                    int32_t id_type, int64_t n, float scale, void* out_dev, int32_t out_type, int64_t out_stride);
+/* Its gradient: grad_table[v, :] = scale * sum of grad_out[i, :] over the tokens i with ids[i] == v, for every row v of the table (zeros for one
+ * without tokens); with accumulate != 0 that is added to grad_table, and rows without tokens are not touched.
+ *   grad_out F32, BF16 or F16; grad_table F32 or grad_out's type.
+ * Tokens with padding_id (-1: none) and, with the sticky error, ids outside the table contribute nothing. */
+int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type, int64_t grad_out_stride, const void* ids_dev, int32_t id_type, int64_t n,
+                    int64_t num_rows, int32_t dim, float scale, int64_t padding_id, void* grad_table_dev, int32_t grad_table_type,
+                    int64_t grad_table_stride, int32_t accumulate);
+
+/* Root-mean-square norm of each of n rows, with the residual's addition: h = x + residual (rounded to its type; residual may be NULL),
+ * y = h * (mean(h^2) + eps)^-1/2 * weight.
+ *   x, residual, h: `type` (F32, BF16, F16); weight: F32 or `type`; h may be NULL (not wanted) and may be x or residual itself.
+ *   y: `type`, or F8E4M3 / I8 with scales: y ~ q * scale, one scale for each `group` columns (32, 64, 128, 256; the last group may be
+ *   narrower) or for the row (0): scales_dev fp32[n][ceil(dim / group)] = max |y| / (448 or 127) of the group, q rounded to nearest, ties to
+ *   even.  Where that is below 1.18e-38 q = 0; where y holds infinities or no numbers the scale is one. */
+int rms_norm_fwd(fc_dense* d, const void* x_dev, int32_t type, int64_t x_stride, const void* residual_dev, int64_t residual_stride, const void* weight_dev,
+                 int32_t weight_type, int64_t n, int32_t dim, float eps, void* h_dev, int64_t h_stride, void* y_dev, int32_t y_type, int64_t y_stride,
+                 float* scales_dev, int32_t group);
+/* Its backward pass: grad_x (the gradient of x and of residual alike) = grad_h + gradient of y's path, with grad_h what arrives at h by other
+ * paths (may be NULL), and grad_weight = sum over the rows (zeros for n = 0; not accumulated).
+ *   grad_y, h (as the forward pass stored it, or x without a residual), grad_h, grad_x: `type`; grad_weight: F32, BF16 or F16.
+ *   grad_x may be grad_y or grad_h itself (same stride). */
+int rms_norm_bwd(fc_dense* d, const void* grad_y_dev, int64_t grad_y_stride, const void* h_dev, int32_t type, int64_t h_stride, const void* weight_dev,
+                 int32_t weight_type, const void* grad_h_dev, int64_t grad_h_stride, int64_t n, int32_t dim, float eps, void* grad_x_dev,
+                 int64_t grad_x_stride, void* grad_weight_dev, int32_t grad_weight_type);
+
+/* Global norm of `count` tensors (sizes[k] contiguous elements of types[k]: F32, BF16, F16), and clipping by it:
+ *   norm_dev[0] = N = sqrt(sum of all squares);  out[k] = grads[k] * min(1, max_norm / (N + 1e-6)).
+ * grads_dev, out_dev, sizes, types are host arrays, read before the call returns; out_dev NULL: in place (tensors are then
+ * left alone where the factor is 1).  Tensors must not overlap, except that out[k] may be grads[k].  max_norm > 0; infinity: nothing is scaled.
+ * A norm that is infinite or no number makes the factor 0 or no number, as the formula says. */
+int grad_norm_clip(fc_dense* d, const void* const* grads_dev, void* const* out_dev, const int64_t* sizes, const int32_t* types, int32_t count,
+                   float max_norm, float* norm_dev);
+
 /* ---- per-kernel timing with HIP events on the handle's own streams (for the benchmark) ----
  * Each item stands for one kind of work.  While recording, what shares a launch otherwise is launched by itself: the sort of a small batch
  * ("sort_scatter") apart from its missing rows ("miss_fill"), and with FC_EVICT_DMA the evicted block of a small batch crosses the

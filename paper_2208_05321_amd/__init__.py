@@ -15,3 +15,4 @@ from .binding import (  # noqa: F401
     FC_EVICT_DMA,
     STAT_FIELDS,
 )
+from .dense import DenseOps  # noqa: F401

@@ -32,6 +32,8 @@ EXPORTS = (
     "cache_check", "cache_destroy", "cache_last_stats", "cache_copy_state", "cache_last_lists", "cache_copy_rows",
     "cache_host_weight", "cache_strerror", "cache_profile_enable", "cache_profile_count", "cache_profile_name",
     "cache_profile_get", "freq_create", "freq_add", "freq_build", "freq_destroy", "table_reorder",
+    "dense_create", "dense_reserve", "dense_check", "dense_destroy", "token_embed_fwd", "token_embed_bwd",
+    "rms_norm_fwd", "rms_norm_bwd", "grad_norm_clip",
 )
 
 
@@ -90,6 +92,16 @@ def load_library(path: str | None = None):
     L.freq_build.argtypes = [vp, vp, vp, vp]
     L.freq_destroy.argtypes = [vp]
     L.table_reorder.argtypes = [vp, vp, vp, i64, i32, vp]
+    f32 = ctypes.c_float
+    L.dense_create.argtypes = [vp, ctypes.POINTER(vp)]
+    L.dense_reserve.argtypes = [vp, i64, i64, i32, i32]
+    L.dense_check.argtypes = [vp]
+    L.dense_destroy.argtypes = [vp]
+    L.token_embed_fwd.argtypes = [vp, vp, i32, i64, i64, i32, vp, i32, i64, f32, vp, i32, i64]
+    L.token_embed_bwd.argtypes = [vp, vp, i32, i64, vp, i32, i64, i64, i32, f32, i64, vp, i32, i64, i32]
+    L.rms_norm_fwd.argtypes = [vp, vp, i32, i64, vp, i64, vp, i32, i64, i32, f32, vp, i64, vp, i32, i64, vp, i32]
+    L.rms_norm_bwd.argtypes = [vp, vp, i64, vp, i32, i64, vp, i32, vp, i64, i64, i32, f32, vp, i64, vp, i32]
+    L.grad_norm_clip.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp]
     for name in EXPORTS:
         if name not in ("cache_host_weight", "cache_strerror", "cache_profile_name"):
             getattr(L, name).restype = ctypes.c_int

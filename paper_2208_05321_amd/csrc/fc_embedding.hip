@@ -481,7 +481,7 @@ __global__ __launch_bounds__(256) void k_bwd_fixup(int C, float* cache, int D, i
 }
 
 // (Re)allocation of sort scratch and of the reduction's partial rows; growth is rare and waits for the whole device.
-static int ensure_sort(SortBufs& sb, int64_t n) {
+int ensure_sort(SortBufs& sb, int64_t n) {
     const int64_t nblk = cdiv(n, RS_TILE);
     if (n > sb.cap) {
         FC_HIP(hipDeviceSynchronize());
@@ -518,7 +518,7 @@ static int ensure_sort(SortBufs& sb, int64_t n) {
 }
 
 // radix_sort with the buffers of sb, keeping track of which of its two supertile tables is clean
-static int sort_in(SortJob& j, SortBufs& sb, hipStream_t st, const int32_t** kres, const int32_t** vres) {
+int sort_in(SortJob& j, SortBufs& sb, hipStream_t st, const int32_t** kres, const int32_t** vres) {
     j.keysA = sb.keysA; j.valsA = sb.valsA; j.keysB = sb.keysB; j.valsB = sb.valsB; j.ghist = sb.ghist; j.dtot = sb.dtot;
     if (sort_small_fits(j)) return sort_small(j, st, kres, vres);      // uses no tables
     int64_t dirtied = 0;

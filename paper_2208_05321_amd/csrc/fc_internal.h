@@ -455,6 +455,9 @@ struct SortJob {
 };
 int radix_sort(const SortJob& j, hipStream_t st, const int32_t** kres, const int32_t** vres);
 size_t sort_table_ints(int64_t n, int bits);   // ints of ghist for a job without supertile tables (max_bits 0)
+// The buffers of a sort of n pairs, and a sort that uses them (one workgroup's where that fits, else radix_sort): fc_embedding.hip
+int ensure_sort(SortBufs& sb, int64_t n);
+int sort_in(SortJob& j, SortBufs& sb, hipStream_t st, const int32_t** kres, const int32_t** vres);
 
 // ---- small batches (fc_small.hip) ----
 bool sort_small_fits(const SortJob& j);

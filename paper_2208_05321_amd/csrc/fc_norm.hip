@@ -1,0 +1,435 @@
+// Root-mean-square norm with the residual's addition, results in 8 bits with scales, and the backward pass.
+//
+//   forward   h = T(x + r),  rho = (mean(h^2) + eps)^-1/2,  y = h * rho * w
+//             8 bits: s = max |y| / qmax over the row or over each group of columns, q = Q(y / s)
+//   backward  c = dy * w,  dh = dh_in + rho * (c - h * rho^2 * mean(c * h)),  dw = sum over the rows of dy * h * rho
+//
+// A row stays in registers between the sums and the results, so each input is read once and each result written once: HBM bounds a
+// large call, the launch a small one.  Lanes of a row: as many as there are vectors of 16 bytes, up to a wavefront; wider rows take
+// a workgroup.  The norm is that of the stored h, so that the backward pass, which works rho out again, sees what the forward pass saw.
+#include "dense_device.h"
+
+#include <algorithm>
+#include <float.h>
+#include <math.h>
+
+namespace fc {
+
+struct F8 { uint8_t b; };                          // FC_TYPE_F8E4M3
+template <class Q> constexpr float QMAX = 0.f;
+template <> constexpr float QMAX<F8> = 448.f;
+template <> constexpr float QMAX<int8_t> = 127.f;
+
+// the larger one, or not a number if either is none
+__device__ __forceinline__ float nan_max(float a, float b) { return a > b || a != a ? a : b; }
+
+// lanes_of: lanes that hold one row; a workgroup has `threads` of them, 256 or one row's
+constexpr int norm_threads(int tpr) { return tpr < 256 ? 256 : tpr; }
+
+// Sum of x over the TPR lanes of a row, in each of them.  lds: TPR / 64 words for each of the two turns that alternate, so that one barrier a
+// sum is enough.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float x, float* lds) {
+    if constexpr (TPR <= 64) return lanes_sum<TPR>(x);
+    else {
+        x = wave_sum(x);
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < TPR / 64; ++k) s += lds[k];
+        return s;
+    }
+}
+template <int TPR>
+__device__ __forceinline__ float row_max(float x, float* lds) {
+#pragma unroll
+    for (int o = 1; o < (TPR < 64 ? TPR : 64); o <<= 1) x = nan_max(x, __shfl_xor(x, o));
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = lds[0];
+#pragma unroll
+        for (int k = 1; k < TPR / 64; ++k) x = nan_max(x, lds[k]);
+    }
+    return x;
+}
+
+template <int N, class T>
+__device__ __forceinline__ void load_weight(float (&v)[N], const void* w, bool f32, int col, int live) {
+    if (f32) load_as_float(v, (const float*)w + col, live);
+    else load_as_float(v, (const T*)w + col, live);
+}
+
+template <int N>
+__device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], float inv, int live) {
+    uint32_t word[N / 4];
+#pragma unroll
+    for (int k = 0; k < N; k += 4) {
+        float q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float t = v[k + e] * inv;
+            q[e] = t > 448.f ? 448.f : t < -448.f ? -448.f : t;      // (beyond its range the conversion gives no number)
+        }
+        int x = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+        word[k / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], x, true);
+    }
+    if (live >= N) {
+        typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
+        V x;
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) x[k] = word[k];
+        *reinterpret_cast<V*>(p) = x;
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) if (k < live) p[k].b = (uint8_t)(word[k / 4] >> (k % 4 * 8));
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], float inv, int live) {
+    typedef int8_t V __attribute__((ext_vector_type(N), aligned(1)));
+    V x;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float t = rintf(v[k] * inv);
+        x[k] = (int8_t)(t > 127.f ? 127.f : t < -127.f ? -127.f : t == t ? t : 0.f);
+    }
+    if (live >= N) *reinterpret_cast<V*>(p) = x;
+    else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) if (k < live) p[k] = x[k];
+    }
+}
+
+struct NormFwd {
+    const void *x, *residual, *weight;
+    void *h, *y;
+    float* scales;
+    int64_t x_stride, residual_stride, h_stride, y_stride, n;
+    int dim, weight_f32, group;          // group: columns of a scale, 0 = the row
+    float eps;
+};
+
+// KEEP: vectors of a row that a lane keeps in registers, 0: rows too wide for that, h is worked out again for each of the three steps
+template <int TPR, int KEEP, class T, class Q>
+__global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
+    constexpr int N = VECTOR<T>, NT = norm_threads(TPR), K = KEEP ? KEEP : 1;
+    constexpr bool QUANT = QMAX<Q> > 0.f;
+    __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
+    const int lane = threadIdx.x & (TPR - 1);
+    const int64_t row = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
+    if (TPR <= 64 && row >= a.n) return;          // (whole rows of lanes; a workgroup with one row always has it)
+    const T* const x = (const T*)a.x + row * a.x_stride;
+    const T* const r = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
+    T* const h = a.h ? (T*)a.h + row * a.h_stride : nullptr;
+    Q* const y = (Q*)a.y + row * a.y_stride;
+    const int vectors = KEEP ? KEEP : (a.dim + TPR * N - 1) / (TPR * N);
+    float v[K][N];
+    auto fetch = [&](float (&t)[N], int col) {
+        const int live = a.dim - col;
+        load_as_float(t, x + col, live);
+        if (r) {
+            float s[N];
+            load_as_float(s, r + col, live);
+#pragma unroll
+            for (int e = 0; e < N; ++e) t[e] = (float)(T)(t[e] + s[e]);
+        }
+    };
+    float s = 0.f;
+#pragma unroll K
+    for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
+        const int col = (k * TPR + lane) * N;
+        float (&t)[N] = v[KEEP ? k : 0];
+        if (col < a.dim) fetch(t, col);
+        else
+#pragma unroll
+            for (int e = 0; e < N; ++e) t[e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) s = fmaf(t[e], t[e], s);
+    }
+    const float rho = rsqrtf(row_sum<TPR>(s, lds[0]) / (float)a.dim + a.eps);
+    auto result = [&](float (&t)[N], int col) {                      // h -> y, and h stored on the way
+        const int live = a.dim - col;
+        float w[N];
+        load_weight<N, T>(w, a.weight, a.weight_f32, col, live);
+#pragma unroll
+        for (int e = 0; e < N; ++e) t[e] = t[e] * rho * w[e];
+    };
+    float most = 0.f;
+#pragma unroll K
+    for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
+        const int col = (k * TPR + lane) * N;
+        float (&t)[N] = v[KEEP ? k : 0];
+        if (col < a.dim) {
+            if (!KEEP) fetch(t, col);
+            if (KEEP && h) store_from_float(h + col, t, a.dim - col);
+            result(t, col);
+            if (!QUANT) {
+                if constexpr (!QUANT) {
+                    if (!KEEP && h) {
+                        float t0[N];
+                        fetch(t0, col);
+                        store_from_float(h + col, t0, a.dim - col);
+                    }
+                    store_from_float(y + col, t, a.dim - col);
+                }
+            } else
+#pragma unroll
+                for (int e = 0; e < N; ++e) most = nan_max(fabsf(t[e]), most);
+        }
+        if constexpr (QUANT) {
+            if (a.group) {                                           // neighbouring lanes hold a group's columns
+                float m = most;
+                const int lanes = min(a.group / N, TPR < 64 ? TPR : 64);
+                for (int o = 1; o < lanes; o <<= 1) m = nan_max(m, __shfl_xor(m, o));
+                most = 0.f;
+                if (col < a.dim) {
+                    const float scale = m * (1.f / QMAX<Q>);
+                    if (col % a.group == 0) a.scales[row * ((a.dim + a.group - 1) / a.group) + col / a.group] = scale;
+                    if (!KEEP && h) {
+                        float t0[N];
+                        fetch(t0, col);
+                        store_from_float(h + col, t0, a.dim - col);
+                    }
+                    store_quantised(y + col, t, scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f, a.dim - col);
+                }
+            }
+        }
+    }
+    if constexpr (QUANT) {
+        if (a.group) return;
+        const float scale = row_max<TPR>(most, lds[1]) * (1.f / QMAX<Q>);
+        const float inv = scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f;
+        if (lane == 0) a.scales[row] = scale;
+#pragma unroll K
+        for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
+            const int col = (k * TPR + lane) * N;
+            float (&t)[N] = v[KEEP ? k : 0];
+            if (col >= a.dim) continue;
+            if (!KEEP) {
+                fetch(t, col);
+                if (h) {
+                    float t0[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) t0[e] = t[e];
+                    result(t, col);
+                    store_from_float(h + col, t0, a.dim - col);
+                } else result(t, col);
+            }
+            store_quantised(y + col, t, inv, a.dim - col);
+        }
+    }
+}
+
+struct NormBwd {
+    const void *dy, *h, *weight, *dh_in;
+    void* dx;
+    float* part;                         // [workgroups][dim]
+    int64_t dy_stride, h_stride, dh_in_stride, dx_stride, n;
+    int dim, weight_f32;
+    float eps;
+};
+
+// KEEP as above; with 0 a workgroup adds to its row of `part` in memory
+template <int TPR, int KEEP, class T>
+__global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
+    constexpr int N = VECTOR<T>, NT = norm_threads(TPR), GROUPS = NT / TPR, K = KEEP ? KEEP : 1;
+    __shared__ float lds[4][TPR > 64 ? TPR / 64 : 1];
+    __shared__ float cols[GROUPS > 1 ? GROUPS * TPR * K * N : 1];
+    const int lane = threadIdx.x & (TPR - 1);
+    const int vectors = KEEP ? KEEP : (a.dim + TPR * N - 1) / (TPR * N);
+    float* const part = a.part + (size_t)blockIdx.x * a.dim;
+    float w[K][N], dw[K][N];
+    if (KEEP) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int col = (k * TPR + lane) * N;
+            if (col < a.dim) load_weight<N, T>(w[k], a.weight, a.weight_f32, col, a.dim - col);
+#pragma unroll
+            for (int e = 0; e < N; ++e) { if (col >= a.dim) w[k][e] = 0.f; dw[k][e] = 0.f; }
+        }
+    } else
+        for (int col = threadIdx.x; col < a.dim; col += NT) part[col] = 0.f;
+    int turn = 0;
+    for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < a.n; row0 += (int64_t)gridDim.x * GROUPS, turn ^= 2) {
+        const int64_t row = row0 + threadIdx.x / TPR;
+        if (TPR <= 64 && row >= a.n) break;
+        const T* const dy = (const T*)a.dy + row * a.dy_stride;
+        const T* const h = (const T*)a.h + row * a.h_stride;
+        const T* const in = a.dh_in ? (const T*)a.dh_in + row * a.dh_in_stride : nullptr;
+        T* const dx = (T*)a.dx + row * a.dx_stride;
+        float g[K][N], x[K][N];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll K
+        for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
+            const int col = (k * TPR + lane) * N, b = KEEP ? k : 0;
+            if (col < a.dim) {
+                load_as_float(g[b], dy + col, a.dim - col);
+                load_as_float(x[b], h + col, a.dim - col);
+                if (!KEEP) load_weight<N, T>(w[0], a.weight, a.weight_f32, col, a.dim - col);
+            } else
+#pragma unroll
+                for (int e = 0; e < N; ++e) g[b][e] = x[b][e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                s1 = fmaf(g[b][e] * w[b][e], x[b][e], s1);
+                s2 = fmaf(x[b][e], x[b][e], s2);
+            }
+        }
+        s1 = row_sum<TPR>(s1, lds[turn]);
+        s2 = row_sum<TPR>(s2, lds[turn + 1]);
+        const float rho = rsqrtf(s2 / (float)a.dim + a.eps), m = rho * rho * (s1 / (float)a.dim);
+#pragma unroll K
+        for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
+            const int col = (k * TPR + lane) * N, b = KEEP ? k : 0;
+            if (col >= a.dim) continue;
+            const int live = a.dim - col;
+            if (!KEEP) {
+                load_as_float(g[0], dy + col, live);
+                load_as_float(x[0], h + col, live);
+                load_weight<N, T>(w[0], a.weight, a.weight_f32, col, live);
+                load_as_float(dw[0], part + col, live);
+            }
+            float o[N];
+            if (in) load_as_float(o, in + col, live);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                dw[b][e] = fmaf(g[b][e], x[b][e] * rho, dw[b][e]);
+                const float t = rho * (g[b][e] * w[b][e] - x[b][e] * m);
+                o[e] = in ? o[e] + t : t;
+            }
+            store_from_float(dx + col, o, live);
+            if (!KEEP) store_from_float(part + col, dw[0], live);
+        }
+    }
+    if constexpr (KEEP > 0) {
+        if constexpr (GROUPS == 1) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int col = (k * TPR + lane) * N;
+                if (col < a.dim) store_from_float(part + col, dw[k], a.dim - col);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int e = 0; e < N; ++e) cols[threadIdx.x / TPR * (TPR * K * N) + (k * TPR + lane) * N + e] = dw[k][e];
+            __syncthreads();
+            for (int col = threadIdx.x; col < a.dim; col += NT) {
+                float s = 0.f;
+                for (int gr = 0; gr < GROUPS; ++gr) s += cols[gr * (TPR * K * N) + col];
+                part[col] = s;
+            }
+        }
+    }
+}
+
+// Columns of the workgroups' sums added up: 64 columns a workgroup, each by 16 threads that take the rows in turn.
+constexpr int DW_COLS = 64, DW_PARTS = 16;
+template <class W>
+__global__ __launch_bounds__(DW_COLS * DW_PARTS) void k_norm_dw(const float* __restrict__ part, int rows, int dim, W* __restrict__ dw) {
+    __shared__ float lds[DW_PARTS][DW_COLS];
+    const int c = threadIdx.x % DW_COLS, p = threadIdx.x / DW_COLS, col = blockIdx.x * DW_COLS + c;
+    float s = 0.f;
+    if (col < dim) {
+#pragma unroll 8
+        for (int r = p; r < rows; r += DW_PARTS) s += part[(size_t)r * dim + col];
+    }
+    lds[p][c] = s;
+    __syncthreads();
+    if (p == 0 && col < dim) {
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < DW_PARTS; ++k) s += lds[k][c];
+        dw[col] = (W)s;
+    }
+}
+
+constexpr int NORM_BWD_BLOCKS = 1024;
+size_t norm_work_bytes(int64_t dim) { return (size_t)NORM_BWD_BLOCKS * dim * 4; }
+
+// f(lanes of a row, vectors a lane keeps) as integral constants
+template <int TPR_, int KEEP_> struct NormShape { static constexpr int TPR = TPR_, KEEP = KEEP_; };
+template <class F>
+static void norm_shape(int64_t vectors, F f) {
+    if (vectors <= 8) f(NormShape<8, 1>());
+    else if (vectors <= 16) f(NormShape<16, 1>());
+    else if (vectors <= 32) f(NormShape<32, 1>());
+    else if (vectors <= 64) f(NormShape<64, 1>());
+    else if (vectors <= 128) f(NormShape<64, 2>());
+    else if (vectors <= 256) f(NormShape<256, 1>());
+    else if (vectors <= 512) f(NormShape<256, 2>());
+    else if (vectors <= 1024) f(NormShape<256, 4>());
+    else if (vectors <= 4096) f(NormShape<1024, 4>());
+    else f(NormShape<1024, 0>());
+}
+
+}  // namespace fc
+
+using namespace fc;
+
+extern "C" {
+
+int rms_norm_fwd(fc_dense* d, const void* x_dev, int32_t type, int64_t x_stride, const void* residual_dev, int64_t residual_stride, const void* weight_dev,
+                 int32_t weight_type, int64_t n, int32_t dim, float eps, void* h_dev, int64_t h_stride, void* y_dev, int32_t y_type, int64_t y_stride,
+                 float* scales_dev, int32_t group) {
+    const bool quant = y_type == FC_TYPE_F8E4M3 || y_type == FC_TYPE_I8;
+    if (!d || n < 0 || n >= DENSE_LIMIT || dim <= 0 || dim > DENSE_MAX_DIM || !is_float_type(type) || (weight_type != FC_TYPE_F32 && weight_type != type) ||
+        (!quant && y_type != type) || (quant ? group != 0 && group != 32 && group != 64 && group != 128 && group != 256 : group != 0) ||
+        !(eps >= 0.f) || x_stride < dim || (residual_dev && residual_stride < dim) || (h_dev && h_stride < dim) || y_stride < dim || !weight_dev ||
+        (n > 0 && (!x_dev || !y_dev || (quant && !scales_dev))))
+        return FC_ERR_INVALID_ARG;
+    if (n == 0) return FC_OK;
+    FC_HIP(hipSetDevice(d->device));
+    const NormFwd a{x_dev, residual_dev, weight_dev, h_dev, y_dev, scales_dev, x_stride, residual_stride, h_stride, y_stride, n, dim,
+                    weight_type == FC_TYPE_F32, group, eps};
+    return with_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        norm_shape(cdiv(dim, VECTOR<T>), [&](auto s) {
+            using S = decltype(s);
+            constexpr int NT = norm_threads(S::TPR);
+            const unsigned blocks = (unsigned)cdiv(n, NT / S::TPR);
+            if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, T, F8><<<blocks, NT, 0, d->stream>>>(a);
+            else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
+            else k_norm_fwd<S::TPR, S::KEEP, T, T><<<blocks, NT, 0, d->stream>>>(a);
+        });
+        FC_HIP(hipGetLastError());
+        return FC_OK;
+    });
+}
+
+int rms_norm_bwd(fc_dense* d, const void* grad_y_dev, int64_t grad_y_stride, const void* h_dev, int32_t type, int64_t h_stride, const void* weight_dev,
+                 int32_t weight_type, const void* grad_h_dev, int64_t grad_h_stride, int64_t n, int32_t dim, float eps, void* grad_x_dev,
+                 int64_t grad_x_stride, void* grad_weight_dev, int32_t grad_weight_type) {
+    if (!d || n < 0 || n >= DENSE_LIMIT || dim <= 0 || dim > DENSE_MAX_DIM || !is_float_type(type) || (weight_type != FC_TYPE_F32 && weight_type != type) ||
+        !is_float_type(grad_weight_type) || !(eps >= 0.f) || grad_y_stride < dim || h_stride < dim || (grad_h_dev && grad_h_stride < dim) ||
+        grad_x_stride < dim || !weight_dev || !grad_weight_dev || (n > 0 && (!grad_y_dev || !h_dev || !grad_x_dev)))
+        return FC_ERR_INVALID_ARG;
+    FC_HIP(hipSetDevice(d->device));
+    FC_TRY(dense_work(d, norm_work_bytes(dim)));
+    float* part = reinterpret_cast<float*>(d->work);
+    const NormBwd a{grad_y_dev, h_dev, weight_dev, grad_h_dev, grad_x_dev, part, grad_y_stride, h_stride, grad_h_stride, grad_x_stride, n, dim,
+                    weight_type == FC_TYPE_F32, eps};
+    int64_t blocks = 0;
+    const int rc = with_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        if (n > 0) norm_shape(cdiv(dim, VECTOR<T>), [&](auto s) {
+            using S = decltype(s);
+            constexpr int NT = norm_threads(S::TPR);
+            blocks = std::min<int64_t>(cdiv(n, NT / S::TPR), NORM_BWD_BLOCKS);
+            k_norm_bwd<S::TPR, S::KEEP, T><<<(unsigned)blocks, NT, 0, d->stream>>>(a);
+        });
+        FC_HIP(hipGetLastError());
+        return FC_OK;
+    });
+    if (rc != FC_OK) return rc;
+    return with_type(grad_weight_type, [&](auto t) -> int {
+        using W = decltype(t);
+        k_norm_dw<<<(unsigned)cdiv(dim, DW_COLS), DW_COLS * DW_PARTS, 0, d->stream>>>(part, (int)blocks, dim, (W*)grad_weight_dev);
+        FC_HIP(hipGetLastError());
+        return FC_OK;
+    });
+}
+
+}  // extern "C"

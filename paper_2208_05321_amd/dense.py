@@ -1,0 +1,269 @@
+"""ctypes binding of the operators beside the cached table (include/freqcache.h): token embedding, root-mean-square norm, clipping by the
+global norm.  Marshalling only: shapes, types and strides are checked here, PyTorch supplies device memory and streams."""
+from __future__ import annotations
+
+import ctypes
+from array import array
+
+from .binding import FreqCacheError, load_library
+
+_TYPE_NAMES = {"float32": 0, "bfloat16": 1, "float16": 2, "float8_e4m3fn": 3, "int8": 4, "int32": 5, "int64": 6}
+_FLOATS = (0, 1, 2)
+
+
+def _refuse(what: str):
+    raise FreqCacheError(-1, what)
+
+
+class DenseOps:
+    """Operators on the caller's device tensors, on one stream.  Each method is one C-ABI call.
+
+    The work runs on `stream` (the current stream of the constructor's call if not given).  A method called while another stream is current
+    waits for that stream, and that stream waits for the method's work, so that tensors may come from, and go to, either.
+    Rows are the last dimension of a tensor; its elements have to be neighbours, rows may be any distance apart."""
+
+    def __init__(self, stream=None):
+        import torch
+
+        if not torch.cuda.is_available():
+            raise FreqCacheError(-8, "no GPU visible; this library has no CPU path")
+        self._L = load_library()
+        self._torch = torch
+        self._type = {getattr(torch, name): k for name, k in _TYPE_NAMES.items()}
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self.device = self.stream.device
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            rc = self._L.dense_create(ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h))
+        self._h = h if rc == 0 else None
+        self._check(rc, "dense_create")
+
+    def _check(self, rc: int, what: str):
+        if rc != 0:
+            raise FreqCacheError(rc, what)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._L.dense_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def reserve(self, max_tokens: int = 0, max_rows: int = 0, max_dim: int = 0, max_tensors: int = 0):
+        self._check(self._L.dense_reserve(self._h, int(max_tokens), int(max_rows), int(max_dim), int(max_tensors)), "dense_reserve")
+
+    def check(self):
+        """Waits for the stream; raises ID_OUT_OF_RANGE if a call since the last check met an id outside its table."""
+        self._check(self._L.dense_check(self._h), "dense_check")
+
+    # ---- arguments ----
+    def _rows(self, t, what: str):
+        """(type, rows, columns, distance of rows in elements) of a tensor whose leading dimensions have one distance between rows."""
+        if t.device != self.device:
+            _refuse(f"{what} is on {t.device}, the handle on {self.device}")
+        k = self._type.get(t.dtype)
+        if k is None:
+            _refuse(f"{what}: type {t.dtype}")
+        shape, stride = t.shape, t.stride()
+        if t.dim() == 0 or shape[-1] == 0:
+            _refuse(f"{what}: shape {tuple(shape)}")
+        d = shape[-1]
+        n = t.numel() // d
+        if d > 1 and stride[-1] != 1:
+            _refuse(f"{what}: the elements of a row have to be neighbours")
+        if t.dim() == 2 and n > 1:
+            step = stride[0]
+        elif n <= 1:
+            step = d
+        else:
+            step, size = None, 1            # leading dimensions, innermost first
+            for length, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+                if length == 1:
+                    continue
+                if step is None:
+                    step = st
+                elif st != step * size:
+                    _refuse(f"{what}: rows have to be one distance apart")
+                size *= length
+        if step < d:
+            _refuse(f"{what}: rows overlap")
+        return k, n, d, step
+
+    def _ids(self, ids):
+        if ids.device != self.device:
+            _refuse(f"ids are on {ids.device}, the handle on {self.device}")
+        k = self._type.get(ids.dtype)
+        if k not in (5, 6):
+            _refuse(f"ids: type {ids.dtype}")
+        if not ids.is_contiguous():
+            _refuse("ids have to be contiguous")
+        return k
+
+    def _vector(self, t, d: int, what: str, types):
+        if t.device != self.device:
+            _refuse(f"{what} is on {t.device}, the handle on {self.device}")
+        k = self._type.get(t.dtype)
+        if k not in types:
+            _refuse(f"{what}: type {t.dtype}")
+        if t.numel() != d or not t.is_contiguous():
+            _refuse(f"{what}: {d} contiguous elements are wanted")
+        return k
+
+    def _run(self, what: str, call, tensors, *args):
+        """The call, in order with the current stream where that is another one than the handle's."""
+        cur = self._torch.cuda.current_stream(self.device)
+        if cur == self.stream:
+            rc = call(self._h, *args)
+        else:
+            self.stream.wait_stream(cur)
+            rc = call(self._h, *args)
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+            cur.wait_stream(self.stream)
+        if rc != 0:
+            raise FreqCacheError(rc, what)
+
+    # ---- token embedding ----
+    def token_embed_fwd(self, table, ids, scale: float = 1.0, out=None, out_dtype=None):
+        """scale * table[ids]: table [rows, dim] (f32, bf16, f16), ids of any shape (int32, int64) -> ids.shape + [dim]."""
+        torch = self._torch
+        if table.dim() != 2:
+            _refuse("table: [rows, dim] is wanted")
+        tk, rows, d, ts = self._rows(table, "table")
+        ik, n = self._ids(ids), ids.numel()
+        if out is None:
+            out = torch.empty((*ids.shape, d), dtype=out_dtype or table.dtype, device=self.device)
+        elif out.shape != (*ids.shape, d) or (out_dtype is not None and out.dtype != out_dtype):
+            _refuse("out: another shape or type")
+        ok, _, _, os = self._rows(out, "out")
+        if tk not in _FLOATS or ok not in _FLOATS:
+            _refuse(f"types {table.dtype} -> {out.dtype}")
+        self._run("token_embed_fwd", self._L.token_embed_fwd, (table, ids, out), table.data_ptr(), tk, ts, rows, d, ids.data_ptr(), ik, n, scale,
+                  out.data_ptr(), ok, os)
+        return out
+
+    def token_embed_bwd(self, grad_out, ids, num_rows: int, scale: float = 1.0, padding_id: int = -1, grad=None, grad_dtype=None,
+                        accumulate: bool = False):
+        """Gradient of the table [num_rows, dim]: scale * the sums of grad_out's rows by id, in f32 (default) or grad_out's type; accumulate
+        adds them to `grad`, whose rows without tokens are then left alone."""
+        torch = self._torch
+        gk, n, d, gs = self._rows(grad_out, "grad_out")
+        ik = self._ids(ids)
+        if n != ids.numel() or gk not in _FLOATS:
+            _refuse(f"grad_out {tuple(grad_out.shape)} {grad_out.dtype} for ids {tuple(ids.shape)}")
+        if grad is None:
+            if accumulate:
+                _refuse("accumulate needs grad")
+            grad = torch.empty((num_rows, d), dtype=grad_dtype or torch.float32, device=self.device)
+        elif grad.shape != (num_rows, d) or (grad_dtype is not None and grad.dtype != grad_dtype):
+            _refuse("grad: another shape or type")
+        tk, _, _, ts = self._rows(grad, "grad")
+        if tk != 0 and tk != gk:
+            _refuse(f"types {grad_out.dtype} -> {grad.dtype}")
+        self._run("token_embed_bwd", self._L.token_embed_bwd, (grad_out, ids, grad), grad_out.data_ptr(), gk, gs, ids.data_ptr(), ik, n, num_rows, d,
+                  scale, padding_id, grad.data_ptr(), tk, ts, 1 if accumulate else 0)
+        return grad
+
+    # ---- root-mean-square norm ----
+    def rms_norm_fwd(self, x, weight, residual=None, eps: float = 1e-6, out_dtype=None, group: int = 0, h_out=None, out=None):
+        """(y, h, scales): h = x + residual (x itself without one), y = h * rsqrt(mean(h^2) + eps) * weight over the last dimension.
+        out_dtype float8_e4m3fn or int8: y ~ q * scale with scales [..., groups] (f32) of `group` columns, or of the row (0); else scales is None.
+        h_out may be x or residual."""
+        torch = self._torch
+        k, n, d, xs = self._rows(x, "x")
+        wk = self._vector(weight, d, "weight", (0, k))
+        if k not in _FLOATS:
+            _refuse(f"x: type {x.dtype}")
+        rs = hs = d
+        h, hp, rp = x, None, None
+        if residual is not None:
+            rk, _, _, rs = self._rows(residual, "residual")
+            if rk != k or residual.shape != x.shape:
+                _refuse("residual: another shape or type than x")
+            rp = residual.data_ptr()
+            h = h_out if h_out is not None else torch.empty(x.shape, dtype=x.dtype, device=self.device)
+            hk, _, _, hs = self._rows(h, "h_out")
+            if hk != k or h.shape != x.shape:
+                _refuse("h_out: another shape or type than x")
+            hp = h.data_ptr()
+        elif h_out is not None:
+            _refuse("h_out without residual: h is x")
+        y = out if out is not None else torch.empty(x.shape, dtype=out_dtype or x.dtype, device=self.device)
+        yk, _, _, ys = self._rows(y, "out")
+        if y.shape != x.shape or (out_dtype is not None and y.dtype != out_dtype) or yk not in (k, 3, 4):
+            _refuse(f"out: {tuple(y.shape)} {y.dtype}")
+        scales = None
+        if yk >= 3:
+            if group not in (0, 32, 64, 128, 256):
+                _refuse(f"group {group}")
+            scales = torch.empty((*x.shape[:-1], -(-d // group) if group else 1), dtype=torch.float32, device=self.device)
+        elif group:
+            _refuse("group without a result in 8 bits")
+        self._run("rms_norm_fwd", self._L.rms_norm_fwd, (x, weight, residual, h, y, scales), x.data_ptr(), k, xs, rp, rs, weight.data_ptr(), wk, n, d, eps,
+                  hp, hs, y.data_ptr(), yk, ys, scales.data_ptr() if scales is not None else None, group)
+        return y, h, scales
+
+    def rms_norm_bwd(self, grad_y, h, weight, grad_h=None, eps: float = 1e-6, grad_weight_dtype=None, out=None):
+        """(grad_x, grad_weight): the gradient of x and of residual alike, and the weight's (in weight's type if not given).  grad_h: the
+        gradient that arrives at h by other paths, added.  `out` (for grad_x) may be grad_y or grad_h."""
+        torch = self._torch
+        k, n, d, hs = self._rows(h, "h")
+        yk, _, _, ys = self._rows(grad_y, "grad_y")
+        wk = self._vector(weight, d, "weight", (0, k))
+        if k not in _FLOATS or yk != k or grad_y.shape != h.shape:
+            _refuse(f"grad_y {tuple(grad_y.shape)} {grad_y.dtype} for h {tuple(h.shape)} {h.dtype}")
+        gs, gp = d, None
+        if grad_h is not None:
+            gk, _, _, gs = self._rows(grad_h, "grad_h")
+            if gk != k or grad_h.shape != h.shape:
+                _refuse("grad_h: another shape or type than h")
+            gp = grad_h.data_ptr()
+        dx = out if out is not None else torch.empty(h.shape, dtype=h.dtype, device=self.device)
+        dk, _, _, ds = self._rows(dx, "out")
+        if dk != k or dx.shape != h.shape:
+            _refuse("out: another shape or type than h")
+        dw = torch.empty(d, dtype=grad_weight_dtype or weight.dtype, device=self.device)
+        wt = self._type.get(dw.dtype)
+        if wt not in _FLOATS:
+            _refuse(f"grad_weight: type {dw.dtype}")
+        self._run("rms_norm_bwd", self._L.rms_norm_bwd, (grad_y, h, weight, grad_h, dx, dw), grad_y.data_ptr(), ys, h.data_ptr(), k, hs, weight.data_ptr(),
+                  wk, gp, gs, n, d, eps, dx.data_ptr(), ds, dw.data_ptr(), wt)
+        return dx, dw
+
+    # ---- clipping ----
+    def _dense_tensors(self, tensors, what: str):
+        types = self._type
+        for t in tensors:
+            if types.get(t.dtype) not in _FLOATS or t.device != self.device:
+                _refuse(f"{what}: {t.dtype} on {t.device}")
+            if not t.is_contiguous():
+                _refuse(f"{what}: tensors have to be contiguous")
+
+    def grad_norm_clip(self, grads, max_norm: float, out=None):
+        """Global norm of the tensors (f32 [1]), which are scaled by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
+        torch = self._torch
+        grads = list(grads)
+        self._dense_tensors(grads, "grads")
+        n = len(grads)
+        outs = None
+        if out is not None:
+            out = list(out)
+            self._dense_tensors(out, "out")
+            if len(out) != n or any(a.dtype != b.dtype or a.numel() != b.numel() for a, b in zip(grads, out)):
+                _refuse("out: other sizes or types than grads")
+            outs = array("Q", [t.data_ptr() for t in out])
+        if not max_norm > 0:
+            _refuse(f"max_norm {max_norm}")
+        types = self._type
+        src = array("Q", [t.data_ptr() for t in grads])
+        sizes = array("q", [t.numel() for t in grads])
+        kinds = array("i", [types[t.dtype] for t in grads])
+        norm = torch.empty(1, dtype=torch.float32, device=self.device)
+        self._run("grad_norm_clip", self._L.grad_norm_clip, (*grads, *(out or ()), norm), src.buffer_info()[0],
+                  outs.buffer_info()[0] if outs is not None else None, sizes.buffer_info()[0], kinds.buffer_info()[0], n, max_norm, norm.data_ptr())
+        return norm
