@@ -28,6 +28,21 @@ template <class T, int N> struct Pack { typedef T V __attribute__((ext_vector_ty
 template <class T> constexpr int VECTOR = 16 / (int)sizeof(T);
 
 template <int N, class T>
+__device__ __forceinline__ void load_vector(float (&v)[N], const T* __restrict__ p) {
+    const auto x = *reinterpret_cast<const typename Pack<T, N>::V*>(p);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = (float)x[k];
+}
+template <int N, class T>
+__device__ __forceinline__ void store_vector(T* __restrict__ p, const float (&v)[N]) {
+    typename Pack<T, N>::V x;
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = (T)v[k];
+    *reinterpret_cast<typename Pack<T, N>::V*>(p) = x;
+}
+
+// The same for the `live` first of N elements.
+template <int N, class T>
 __device__ __forceinline__ void load_as_float(float (&v)[N], const T* __restrict__ p, int live) {
     if (live >= N) {
         const auto x = *reinterpret_cast<const typename Pack<T, N>::V*>(p);

@@ -6,20 +6,47 @@
 // Backward: the tokens are put in order by id with the sort of the bags' backward pass (stable, so that an id's tokens keep their
 // order) and every row of the gradient is written once, by the lanes that add its tokens up; without accumulation a row without
 // tokens gets its zeros in the same pass.  Popular ids are what a sum by rows has to be protected from: the sorted tokens are cut
-// into chunks of 64, and a chunk that lies inside one id's run is added up beforehand, by lanes of its own, as are 64 such chunks
-// in a row.  A row then adds at most 126 tokens, 126 chunks and n / 4096 stretches, whatever the ids.  All sums are in 32 bits and in
-// an order that depends on the ids alone: results are reproducible.
+// into chunks of 16, and a chunk that lies inside one id's run is added up beforehand, by lanes of its own, as are 16 such chunks
+// in a row (a stretch) and 16 stretches (a mile).  A row then adds at most 30 tokens, 30 chunks, 30 stretches and n / 4096 miles, whatever the
+// ids.  All sums are in 32 bits and in an order that depends on the ids alone: results are reproducible.
+// (With chunks of 64 a popular row's 126 tokens, one after the other, were the kernel's duration: dense gradient of 131,072 rows of 2048
+// columns, 16,384 tokens, 330 us.)
 #include "dense_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fc {
 
 constexpr int TOK_THREADS = 256;
-constexpr int TOK_CHUNK = 64;                     // sorted tokens to a chunk, and chunks to a stretch
-constexpr int TOK_STRETCH = TOK_CHUNK * TOK_CHUNK;
+constexpr int TOK_CHUNK = 16;                     // sorted tokens to a chunk, chunks to a stretch, stretches to a mile
+constexpr int TOK_STRETCH = TOK_CHUNK * TOK_CHUNK, TOK_MILE = TOK_CHUNK * TOK_STRETCH;
+constexpr int64_t TOK_MILES_FROM = 8 * TOK_MILE;  // tokens from which on miles are added up: fewer cost a row less than the launch
+constexpr int TOK_BLOCK = 64;                     // sorted tokens whose run heads are one word
 
 // ---- forward ----
+// Rows are walked in vectors of N columns; the columns left over at the end (fewer than N) are taken by a lane each, in code of their own:
+// with a partial vector handled wherever one is loaded or stored, the backward pass's kernels grew to 1200 branches and waited for their
+// own instructions (dense gradient of 131,072 rows of 2048 columns: 380 us).
+template <int ROWS, int N, class S, class D>
+__device__ __forceinline__ void token_columns(const S* const (&row)[ROWS], float scale, D* __restrict__ out, int64_t out_stride, int64_t rows, int col, int end, int step) {
+    for (; col < end; col += step) {
+        float v[ROWS][N];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            if (row[k]) load_vector(v[k], row[k] + col);
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            if (k >= rows) break;
+            // (a row of an id outside stays zero even where the scale is infinite)
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[k][e] = row[k] ? v[k][e] * scale : 0.f;
+            store_vector(out + k * out_stride + col, v[k]);
+        }
+    }
+}
+
 template <int ROWS, class S, class D, class I>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_fwd(const S* __restrict__ table, int64_t table_stride, int rows, int dim, int lpr_shift,
                                                            const I* __restrict__ ids, int64_t n, float scale, D* __restrict__ out,
@@ -37,207 +64,462 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_fwd(const S* __restrict__
         row[k] = ok ? table + (size_t)id * table_stride : nullptr;
     }
     if (bad && lane == 0 && first < n) atomicOr(flags, EF_ID_RANGE);
-    for (int col = lane * N; col < dim; col += lpr * N) {
-        float v[ROWS][N];
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            if (row[k]) load_as_float(v[k], row[k] + col, dim - col);
-            else
-#pragma unroll
-                for (int e = 0; e < N; ++e) v[k][e] = 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            if (first + k >= n) break;
-            // (a row of an id outside stays zero even where the scale is infinite)
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[k][e] = row[k] ? v[k][e] * scale : 0.f;
-            store_from_float(out + (first + k) * out_stride + col, v[k], dim - col);
-        }
-    }
+    const int whole = dim & -N;
+    D* const o = out + first * out_stride;
+    token_columns<ROWS, N>(row, scale, o, out_stride, n - first, lane * N, whole, lpr * N);
+    if (whole != dim) token_columns<ROWS, 1>(row, scale, o, out_stride, n - first, whole + lane, dim, lpr);
 }
 
 // ---- backward ----
-// Sort keys: the id, or `rows` for the padding id and for ids outside.  first: one word per table row, "no token" to begin with.
+// Workgroups that share a row's columns are neighbours.
+struct Tile { unsigned block; int tile; bool last; };
+__device__ __forceinline__ Tile my_tile(int tiles) {
+    const unsigned b = blockIdx.x / (unsigned)tiles;
+    const int t = (int)(blockIdx.x - b * (unsigned)tiles);
+    return Tile{b, t, t == tiles - 1};
+}
+
+// Where an id's tokens begin and end among the sorted ones; begin < 0: it has none.
+struct TokenRun { int begin, end; };
+
+// Sort keys: the id, or `rows` for the padding id and for ids outside.  runs: one per table row, without tokens to begin with.
+template <class I>
+__device__ __forceinline__ int token_key(I id, int rows, int64_t padding_id, bool& bad) {
+    const bool ok = id >= 0 && id < (I)rows, pad = (int64_t)id == padding_id;
+    bad |= !ok && !pad;
+    return ok && !pad ? (int)id : rows;
+}
 template <class I>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_keys(const I* __restrict__ ids, int64_t n, int rows, int64_t padding_id, int32_t* __restrict__ keys,
-                                                            int32_t* __restrict__ first, uint32_t* flags) {
+                                                            TokenRun* __restrict__ runs, uint32_t* flags) {
     const int64_t i = (int64_t)blockIdx.x * TOK_THREADS + threadIdx.x;
     bool bad = false;
-    if (i < n) {
-        const I id = ids[i];
-        const bool ok = id >= 0 && id < (I)rows;
-        bad = !ok && (int64_t)id != padding_id;
-        keys[i] = ok && (int64_t)id != padding_id ? (int)id : rows;
-    }
-    if (first && i < rows) first[i] = -1;
+    if (i < n) keys[i] = token_key(ids[i], rows, padding_id, bad);
+    if (runs && i < rows) runs[i] = TokenRun{-1, -1};
     if (bad) atomicOr(flags, EF_ID_RANGE);
 }
 
-// acc += rows vals[a .. b) of grad_out, columns from `col`, in order
-template <int N, class S>
-__device__ __forceinline__ void add_tokens(float (&acc)[N], const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ vals, int a, int b,
-                                           int col, int dim) {
-    constexpr int AT_ONCE = 8;
-    for (; a + AT_ONCE <= b; a += AT_ONCE) {
-        float v[AT_ONCE][N];
-        int at[AT_ONCE];
+// acc += the rows at(a) .. at(b - 1) of src, in order: U vectors of N columns, `step` columns apart, those before `end`.  AT rows' loads are on
+// their way together; the last ones that do not make AT go in halves of it, with rows beyond the last read again and not counted.
+template <int AT, int U, int N, class S, class F>
+__device__ __forceinline__ void add_rows(float (&acc)[U][N], const S* __restrict__ src, int64_t stride, F at, int a, int b, int col, int end, int step) {
+    auto batch = [&](auto size, bool whole) {
+        constexpr int B = decltype(size)::value;
+        int p[B];
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) at[k] = vals[a + k];
+        for (int k = 0; k < B; ++k) p[k] = at(whole ? a + k : min(a + k, b - 1));
+        float v[B][U][N];
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) load_as_float(v[k], grad_out + (size_t)at[k] * stride + col, dim - col);
+        for (int u = 0; u < U; ++u)
+            if (col + u * step < end)
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k)
+                for (int k = 0; k < B; ++k) load_vector(v[k][u], src + (size_t)p[k] * stride + col + u * step);
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += v[k][e];
-    }
-    for (; a < b; ++a) {
-        float v[N];
-        load_as_float(v, grad_out + (size_t)vals[a] * stride + col, dim - col);
+        for (int k = 0; k < B; ++k)
+            if (whole || a + k < b)
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += v[e];
-    }
-}
-// the same for partial rows [a .. b), which are `dim` floats apart
-template <int N>
-__device__ __forceinline__ void add_parts(float (&acc)[N], const float* __restrict__ part, int a, int b, int col, int dim) {
-#pragma unroll 4
-    for (; a < b; ++a) {
-        float v[N];
-        load_as_float(v, part + (size_t)a * dim + col, dim - col);
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += v[e];
-    }
+                    for (int e = 0; e < N; ++e) acc[u][e] += v[k][u][e];
+        a += B;
+    };
+    while (b - a >= AT) batch(std::integral_constant<int, AT>(), true);
+    while (a < b) batch(std::integral_constant<int, (AT > 1 ? AT / 2 : 1)>(), false);
 }
 
-// Chunks inside one id's run are added up; first[id] = where its run begins.
-template <class S>
-__global__ __launch_bounds__(TOK_THREADS) void k_token_chunks(const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys,
-                                                              const int32_t* __restrict__ vals, int n, int rows, int dim, int lpr_shift,
-                                                              float* __restrict__ part, int32_t* __restrict__ first) {
-    constexpr int N = VECTOR<S>;
-    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1);
-    const int64_t chunk = ((int64_t)blockIdx.x * TOK_THREADS + threadIdx.x) >> lpr_shift;
-    const int64_t a = chunk * TOK_CHUNK;
-    if (a >= n) return;
-    if (first)
-        for (int j = lane; j < TOK_CHUNK && a + j < n; j += lpr) {
-            const int key = keys[a + j];
-            if (key < rows && (a + j == 0 || keys[a + j - 1] != key)) first[key] = (int)(a + j);
-        }
-    if (a + TOK_CHUNK > n || keys[a] == rows || keys[a] != keys[a + TOK_CHUNK - 1]) return;
-    for (int col = lane * N; col < dim; col += lpr * N) {
-        float acc[N] = {};
-        add_tokens(acc, grad_out, stride, vals, (int)a, (int)a + TOK_CHUNK, col, dim);
-        store_from_float(part + chunk * dim + col, acc, dim - col);
-    }
-}
-
-// Stretches inside one id's run: the chunks' sums added up.
-__global__ __launch_bounds__(TOK_THREADS) void k_token_stretches(const int32_t* __restrict__ keys, int n, int rows, int dim, int lpr_shift,
-                                                                 const float* __restrict__ part, float* __restrict__ far_part) {
-    constexpr int N = 4;
-    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1);
-    const int64_t s = ((int64_t)blockIdx.x * TOK_THREADS + threadIdx.x) >> lpr_shift, a = s * TOK_STRETCH;
-    if (a + TOK_STRETCH > n || keys[a] == rows || keys[a] != keys[a + TOK_STRETCH - 1]) return;
-    for (int col = lane * N; col < dim; col += lpr * N) {
-        float acc[N] = {};
-        add_parts(acc, part, (int)s * TOK_CHUNK, ((int)s + 1) * TOK_CHUNK, col, dim);
-        store_from_float(far_part + s * dim + col, acc, dim - col);
-    }
-}
-
-// end of the run of `key` that holds position i
-__device__ __forceinline__ int run_end(const int32_t* __restrict__ keys, int n, int i, int key) {
-    int64_t step = 1;
-    while (i + step < n && keys[i + step] == key) step <<= 1;
-    int lo = (int)(i + step / 2), hi = (int)min((int64_t)n, i + step);       // keys[lo] is in, hi is out
+// End of the run of `key`, which holds the last position of block c and the first of block c + 1, by a wavefront: 64 blocks are tried at a time.
+__device__ __forceinline__ int run_end(const int32_t* __restrict__ keys, int n, int64_t c, int key, int lane) {
+    int64_t lo = c + 1, hi = (n + TOK_BLOCK - 1) / TOK_BLOCK;      // block lo begins with the key, block hi does not
     while (hi - lo > 1) {
-        const int mid = lo + (hi - lo) / 2;
-        if (keys[mid] == key) lo = mid; else hi = mid;
+        const int64_t step = (hi - lo + 63) / 64, p = lo + (lane + 1) * step;
+        const int t = __popcll(__ballot(p < hi && keys[p * TOK_BLOCK] == key));
+        hi = min(hi, lo + (t + 1) * step);
+        lo += t * step;
     }
-    return hi;
+    const int64_t i = lo * TOK_BLOCK + lane;
+    return (int)(lo * TOK_BLOCK) + __popcll(__ballot(i < n && keys[i] == key));
 }
 
-template <int N, class S>
-__device__ __forceinline__ void add_run(float (&acc)[N], const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ vals, int a, int b,
-                                        const float* __restrict__ part, const float* __restrict__ far_part, int col, int dim) {
-    int c = (a + TOK_CHUNK - 1) / TOK_CHUNK;
-    const int c1 = b / TOK_CHUNK;
-    if (c >= c1) { add_tokens(acc, grad_out, stride, vals, a, b, col, dim); return; }
-    add_tokens(acc, grad_out, stride, vals, a, c * TOK_CHUNK, col, dim);
-    int s = (c + TOK_CHUNK - 1) / TOK_CHUNK;
-    const int s1 = c1 / TOK_CHUNK;
-    if (s < s1) {
-        add_parts(acc, part, c, s * TOK_CHUNK, col, dim);
-        add_parts(acc, far_part, s, s1, col, dim);
-        c = s1 * TOK_CHUNK;
-    }
-    add_parts(acc, part, c, c1, col, dim);
-    add_tokens(acc, grad_out, stride, vals, c1 * TOK_CHUNK, b, col, dim);
-}
-
-// ADD: the lanes of a row-group look at PER sorted positions and take the rows whose runs begin there; else at PER rows of the gradient.
-template <bool ADD, int PER, class S, class G>
-__global__ __launch_bounds__(TOK_THREADS) void k_token_rows(const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys,
-                                                            const int32_t* __restrict__ vals, int n, int rows, int dim, int lpr_shift, float scale,
-                                                            const float* __restrict__ part, const float* __restrict__ far_part,
-                                                            const int32_t* __restrict__ first, G* __restrict__ grad, int64_t grad_stride) {
-    constexpr int N = VECTOR<S>;
-    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1);
-    const int64_t at = (((int64_t)blockIdx.x * TOK_THREADS + threadIdx.x) >> lpr_shift) * PER;
-    const int64_t end = ADD ? n : rows;
-    for (int k = 0; k < PER && at + k < end; ++k) {
-        int row, a;
-        if (ADD) {
-            a = (int)(at + k);
-            row = keys[a];
-            if (row == rows || (a > 0 && keys[a - 1] == row)) continue;
+// Runs, block by block, by the wavefronts of a workgroup that has positions first .. first + count - 1.
+// runs: every id's run is written there.  Without it (the gradient accumulates) heads, ends: of each block, which of its positions begin a
+// run, and where the run ends that holds its last one.
+__device__ __forceinline__ void mark_runs(const int32_t* __restrict__ keys, int n, int rows, int64_t first, int count, TokenRun* __restrict__ runs,
+                                          uint64_t* __restrict__ heads, int32_t* __restrict__ ends) {
+    const int lane = threadIdx.x & 63;
+    for (int w = threadIdx.x >> 6; w < count / TOK_BLOCK; w += blockDim.x >> 6) {
+        const int64_t c = first / TOK_BLOCK + w, i = c * TOK_BLOCK + lane;
+        if (c * TOK_BLOCK >= n) break;
+        const bool in = i < n;
+        const int key = in ? keys[i] : rows;
+        const bool head = in && (i == 0 || keys[i - 1] != key);           // (tokens without a row have a run, too: it ends the one before)
+        const bool tail = in && (i + 1 == n || keys[i + 1] != key);
+        if (runs) {
+            if (head && key < rows) runs[key].begin = (int)i;
+            if (tail && key < rows) runs[key].end = (int)i + 1;
         } else {
-            row = (int)(at + k);
-            a = first[row];
-        }
-        const int b = a < 0 ? a : run_end(keys, n, a, row);
-        G* const out = grad + (size_t)row * grad_stride;
-        for (int col = lane * N; col < dim; col += lpr * N) {
-            float acc[N] = {};
-            if (a < b) add_run(acc, grad_out, stride, vals, a, b, part, far_part, col, dim);
-            float old[N] = {};
-            if (ADD) load_as_float(old, out + col, dim - col);
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] = ADD ? fmaf(acc[e], scale, old[e]) : a < b ? acc[e] * scale : 0.f;
-            store_from_float(out + col, acc, dim - col);
+            const uint64_t mask = __ballot(head);
+            const int last = __builtin_amdgcn_readlane(key, 63);
+            int end = (int)min((int64_t)n, (c + 1) * TOK_BLOCK);
+            if (end < n && last < rows && keys[end] == last) end = run_end(keys, n, c, last, lane);
+            if (lane == 0) { heads[c] = mask; ends[c] = end; }
         }
     }
 }
 
-template <class G>
-__global__ __launch_bounds__(TOK_THREADS) void k_token_no_rows(G* __restrict__ grad, int64_t stride, int64_t rows, int dim) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < dim; c += TOK_THREADS) grad[r * stride + c] = (G)0.f;
+// all of `count` sorted positions from i are there and have one row
+__device__ __forceinline__ bool one_row(const int32_t* __restrict__ keys, int n, int rows, int64_t i, int count) {
+    if (i + count > n) return false;
+    const int key = keys[i];
+    return key < rows && keys[i + count - 1] == key;
 }
 
-struct TokenWork { size_t keys, first, part, far_part, bytes; };
+// Chunks and stretches inside one run: a row-group to a chunk, 16 neighbouring ones to a stretch, whose sum they work out together; the
+// chunks of such a stretch are not asked for.  Columns first .. end of the row, N to a lane.
+template <int N, class S>
+__device__ __forceinline__ void chunk_sum(const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ vals, bool chunk, bool stretch, bool any_stretch,
+                                          int64_t c, float* __restrict__ part, float* __restrict__ far, int dim, int first, int end, int lpr_shift, float* lds) {
+    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1), col = first + lane * N, row0 = (int)c * TOK_CHUNK;
+    float acc[1][N] = {};
+    if (chunk && col < end) {
+        add_rows<8>(acc, grad_out, stride, [=](int i) { return vals[i]; }, row0, row0 + TOK_CHUNK, col, end, 0);
+        if (!stretch) store_vector(part + c * dim + col, acc[0]);
+    }
+    if (!any_stretch) return;
+    const int nt = blockDim.x;
+#pragma unroll
+    for (int e = 0; e < N; ++e) lds[e * nt + threadIdx.x] = acc[0][e];
+    __syncthreads();
+    if (stretch) {
+        // element j of the stretch's lpr * N columns: e = j / lpr, lane = j % lpr
+        const int base = threadIdx.x & ~((TOK_CHUNK << lpr_shift) - 1), t = threadIdx.x - base;
+        for (int j = t; j < lpr * N; j += TOK_CHUNK << lpr_shift) {
+            const int e = j >> lpr_shift, l = j & (lpr - 1), at = first + l * N + e;
+            if (at >= end) continue;
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < TOK_CHUNK; ++k) s += lds[e * nt + base + (k << lpr_shift) + l];
+            far[c / TOK_CHUNK * dim + at] = s;
+        }
+    }
+    __syncthreads();
+}
+
+// threads: 16 row-groups, or 256
+template <class S>
+__global__ __launch_bounds__(1024) void k_token_chunks(const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys,
+                                                       const int32_t* __restrict__ vals, int n, int rows, int dim, int lpr_shift, int tiles,
+                                                       float* __restrict__ part, float* __restrict__ far, TokenRun* __restrict__ runs,
+                                                       uint64_t* __restrict__ heads, int32_t* __restrict__ ends) {
+    constexpr int N = VECTOR<S>;
+    extern __shared__ float chunk_lds[];
+    const int groups = blockDim.x >> lpr_shift;
+    const Tile t = my_tile(tiles);
+    const int64_t c = (int64_t)t.block * groups + (threadIdx.x >> lpr_shift);
+    if (t.tile == 0) mark_runs(keys, n, rows, (int64_t)t.block * groups * TOK_CHUNK, groups * TOK_CHUNK, runs, heads, ends);
+    const bool chunk = one_row(keys, n, rows, c * TOK_CHUNK, TOK_CHUNK);
+    const bool stretch = chunk && one_row(keys, n, rows, c / TOK_CHUNK * TOK_STRETCH, TOK_STRETCH);
+    const bool any = __syncthreads_or(stretch);
+    const int whole = dim & -N;
+    chunk_sum<N>(grad_out, stride, vals, chunk, stretch, any, c, part, far, dim, t.tile * (N << lpr_shift), whole, lpr_shift, chunk_lds);
+    if (whole != dim && t.last)
+        chunk_sum<1>(grad_out, stride, vals, chunk, stretch, any, c, part, far, dim, whole, dim, lpr_shift, chunk_lds);
+}
+
+// Miles inside one run, out of the stretches' sums: a row-group each.
+__global__ __launch_bounds__(TOK_THREADS) void k_token_miles(const int32_t* __restrict__ keys, int n, int rows, int dim, int lpr_shift, int tiles,
+                                                             const float* __restrict__ far, float* __restrict__ miles) {
+    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1);
+    const Tile t = my_tile(tiles);
+    const int64_t m = ((int64_t)t.block * TOK_THREADS + threadIdx.x) >> lpr_shift;
+    if (!one_row(keys, n, rows, m * TOK_MILE, TOK_MILE)) return;
+    auto columns = [&](auto w, int col, int end) {
+        float acc[1][decltype(w)::value] = {};
+        if (col >= end) return;
+        add_rows<TOK_CHUNK>(acc, far, dim, [](int i) { return i; }, (int)m * TOK_CHUNK, ((int)m + 1) * TOK_CHUNK, col, end, 0);
+        store_vector(miles + m * dim + col, acc[0]);
+    };
+    const int whole = dim & -4;
+    columns(std::integral_constant<int, 4>(), (t.tile * lpr + lane) * 4, whole);
+    if (whole != dim && t.last) columns(std::integral_constant<int, 1>(), whole + lane, dim);
+}
+
+struct TokenRows {
+    const int32_t* vals;
+    const float *part, *far, *miles;              // sums of chunks, stretches, miles (null: none are there)
+    int dim, lpr_shift, tiles;
+    float scale;
+};
+
+// U vectors of a lane in one row of the gradient: the sum of rows, scaled, stored or added.
+template <bool ADD, int U, int N, class G, class F>
+__device__ __forceinline__ void token_row(float scale, G* __restrict__ out, int col, int end, int step, F sum) {
+    float acc[U][N] = {}, old[U][N];
+    if (ADD) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) if (col + u * step < end) load_vector(old[u], out + col + u * step);
+    }
+    sum(acc);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (col + u * step >= end) break;
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[u][e] = ADD ? fmaf(acc[u][e], scale, old[u][e]) : acc[u][e] * scale;
+        store_vector(out + col + u * step, acc[u]);
+    }
+}
+
+// Sorted tokens a .. b - 1, with the chunks, stretches and miles among them already summed.  token(i): the i-th sorted token.
+template <int U, int N, class S, class F>
+__device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, const S* __restrict__ grad_out, int64_t stride, F token, int a, int b, int col, int end,
+                                        int step) {
+    constexpr int AT = U > 1 ? 4 : 8;             // loads of a lane on their way together: more cost wavefronts
+    int c0 = (a + TOK_CHUNK - 1) / TOK_CHUNK, c1 = b / TOK_CHUNK;
+    const bool parts = c0 < c1;
+    for (int k = 0; k < (parts ? 2 : 1); ++k)     // before the first chunk, after the last
+        add_rows<AT>(acc, grad_out, stride, token, k ? c1 * TOK_CHUNK : a, parts && !k ? c0 * TOK_CHUNK : b, col, end, step);
+    if (!parts) return;
+    const float* src = q.part;
+    for (int level = 0; level < 3; ++level) {     // chunks before the first stretch and after the last; and so on
+        const float* const next = level == 0 ? q.far : level == 1 ? q.miles : nullptr;
+        const int s0 = (c0 + TOK_CHUNK - 1) / TOK_CHUNK, s1 = c1 / TOK_CHUNK;
+        const bool more = next && s0 < s1;
+        for (int k = 0; k < (more ? 2 : 1); ++k)
+            add_rows<AT>(acc, src, q.dim, [](int i) { return i; }, k ? s1 * TOK_CHUNK : c0, more && !k ? s0 * TOK_CHUNK : c1, col, end, step);
+        if (!more) return;
+        src = next; c0 = s0; c1 = s1;
+    }
+}
+
+// f(vectors of a lane, their columns, first column, end): a workgroup's columns of a row, and in the last workgroup of a row what is left over
+template <int U, int N, class F>
+__device__ __forceinline__ void token_tile(int dim, int lpr_shift, const Tile& t, F f) {
+    const int lane = threadIdx.x & ((1 << lpr_shift) - 1), step = N << lpr_shift, whole = dim & -N;
+    f(std::integral_constant<int, U>(), std::integral_constant<int, N>(), t.tile * step * U + lane * N, whole, step);
+    if (whole != dim && t.last) f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>(), whole + lane, dim, 0);
+}
+
+// Every row of the gradient; a row-group takes PER of them, whose runs it reads together, and a workgroup's groups neighbours at a time.
+template <int PER, int U, class S, class G>
+__global__ __launch_bounds__(TOK_THREADS) void k_token_rows(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const TokenRun* __restrict__ runs,
+                                                            int rows, G* __restrict__ grad, int64_t grad_stride) {
+    const Tile tile = my_tile(q.tiles);
+    const int groups = TOK_THREADS >> q.lpr_shift;
+    const int64_t at = (int64_t)tile.block * groups * PER + (threadIdx.x >> q.lpr_shift);
+    TokenRun run[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) run[k] = runs[min(at + k * groups, (int64_t)rows - 1)];
+    token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto w, int col, int end, int step) {
+        constexpr int UU = decltype(u)::value, NN = decltype(w)::value;
+        const float none[NN] = {};
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (at + k * groups < rows && run[k].begin < 0)
+#pragma unroll
+                for (int v = 0; v < UU; ++v) if (col + v * step < end) store_vector(grad + (at + k * groups) * grad_stride + col + v * step, none);
+#pragma unroll 1
+        for (int k = 0; k < PER; ++k) {
+            if (at + k * groups >= rows) break;
+            const TokenRun r = runs[at + k * groups];
+            if (r.begin >= 0)
+                token_row<false, UU, NN>(q.scale, grad + (at + k * groups) * grad_stride, col, end, step,
+                                         [&](float (&acc)[UU][NN]) {
+                                             add_run(acc, q, grad_out, stride, [&](int i) { return q.vals[i]; }, r.begin, r.end, col, end, step);
+                                         });
+        }
+    });
+}
+
+// Rows with tokens, stored or (ADD) added to what the gradient holds: a row-group takes the runs that begin at its PER positions.
+template <bool ADD, int PER, int U, class S, class G>
+__global__ __launch_bounds__(TOK_THREADS) void k_token_runs(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys, int n,
+                                                            int rows, const uint64_t* __restrict__ heads, const int32_t* __restrict__ ends,
+                                                            G* __restrict__ grad, int64_t grad_stride) {
+    static_assert(TOK_BLOCK % PER == 0 && PER < 64, "positions of one block");
+    const Tile tile = my_tile(q.tiles);
+    const int64_t at = (((int64_t)tile.block * TOK_THREADS + threadIdx.x) >> q.lpr_shift) * PER;
+    if (at >= n) return;
+    const int64_t c = at / TOK_BLOCK;
+    const int bit = (int)(at % TOK_BLOCK);
+    const uint64_t all = heads[c];
+    const int last = ends[c];
+    // the positions' keys and tokens, one to a lane: read for each run as it comes up, they cost it two loads one after the other
+    const int lpr = 1 << q.lpr_shift, lane = threadIdx.x & (lpr - 1);
+    const bool held = lpr >= PER;
+    const int64_t i = min(at + min(lane, PER - 1), (int64_t)n - 1);
+    const int my_key = held ? keys[i] : 0, my_token = held ? q.vals[i] : 0;
+    token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto w, int col, int end, int step) {
+        constexpr int UU = decltype(u)::value, NN = decltype(w)::value;
+        for (uint64_t mine = all >> bit & (((uint64_t)1 << PER) - 1); mine; mine &= mine - 1) {
+            const int j = bit + __builtin_ctzll(mine);
+            const uint64_t later = j < 63 ? all >> (j + 1) : 0;
+            const int a = (int)(c * TOK_BLOCK) + j, b = later ? a + 1 + __builtin_ctzll(later) : last;
+            const int key = held ? __shfl(my_key, a - (int)at, lpr) : keys[a];
+            if (key >= rows) break;
+            token_row<ADD, UU, NN>(q.scale, grad + (size_t)key * grad_stride, col, end, step,
+                                   [&](float (&acc)[UU][NN]) {
+                                       add_run(acc, q, grad_out, stride, [&](int i) {
+                                           const int k = i - (int)at;
+                                           const int t = __shfl(my_token, k & (PER - 1), lpr);
+                                           return held && k < PER ? t : q.vals[i];
+                                       }, a, b, col, end, step);
+                                   });
+        }
+    });
+}
+
+// Few tokens: no sort.  Every workgroup reads all ids and lists, in order, the tokens whose rows are its own: with `per_block` neighbouring rows
+// to a workgroup, which also writes the zeros among them, or without (0: the gradient accumulates, or holds zeros already) as a hash of the id says.
+// A row-group then goes through the list's tokens that are the first of their row, puts the row's tokens together in LDS and adds them up.
+constexpr int TOK_FEW = 1024, TOK_FEW_ROWS = 1024;
+template <bool ADD, int U, class S, class G, class I>
+__global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const I* __restrict__ ids, int n, int rows,
+                                                           int64_t padding_id, int per_block, unsigned blocks, G* __restrict__ grad, int64_t grad_stride,
+                                                           uint32_t* flags) {
+    constexpr int PER = TOK_FEW / TOK_THREADS, WAVES = TOK_THREADS / 64;
+    __shared__ int list_key[TOK_FEW], list_pos[TOK_FEW], order[TOK_FEW], counts[PER * WAVES];
+    __shared__ uint32_t used[TOK_FEW_ROWS / 32];
+    const int lpr = 1 << q.lpr_shift, lane = threadIdx.x & (lpr - 1), groups = TOK_THREADS >> q.lpr_shift, g = threadIdx.x >> q.lpr_shift;
+    const int w = threadIdx.x >> 6, wl = threadIdx.x & 63;
+    const Tile tile = my_tile(q.tiles);
+    const int64_t row0 = (int64_t)tile.block * per_block;
+    bool bad = false;
+    I id[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) id[k] = ids[min(k * TOK_THREADS + (int)threadIdx.x, n - 1)];
+    if (threadIdx.x < TOK_FEW_ROWS / 32) used[threadIdx.x] = 0;
+    int key[PER];
+    uint64_t mask[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        key[k] = token_key(id[k], rows, padding_id, bad);
+        const bool mine = per_block ? key[k] >= row0 && key[k] < row0 + per_block : ((unsigned)key[k] * 2654435761u >> 16) % blocks == tile.block;
+        mask[k] = __ballot(mine && key[k] < rows && k * TOK_THREADS + (int)threadIdx.x < n);
+        if (wl == 0) counts[k * WAVES + w] = __popcll(mask[k]);
+    }
+    if (bad && blockIdx.x == 0) atomicOr(flags, EF_ID_RANGE);
+    __syncthreads();
+    int m = 0;
+    {
+        int at[PER];
+#pragma unroll
+        for (int j = 0; j < PER * WAVES; ++j) {
+            if (j % WAVES == w) at[j / WAVES] = m;
+            m += counts[j];
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (mask[k] >> wl & 1) {
+                const int e = at[k] + __popcll(mask[k] & ((1ull << wl) - 1));
+                list_key[e] = key[k];
+                list_pos[e] = k * TOK_THREADS + (int)threadIdx.x;
+                if (per_block) { const int r = (int)(key[k] - row0); atomicOr(&used[r / 32], 1u << r % 32); }
+            }
+    }
+    __syncthreads();
+    if (per_block) {
+        const int here = (int)min((int64_t)per_block, rows - row0);
+        for (int r = g; r < here; r += groups) {
+            if (used[r / 32] >> r % 32 & 1) continue;
+            token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto v, int col, int end, int step) {
+                const float none[decltype(v)::value] = {};
+#pragma unroll
+                for (int k = 0; k < decltype(u)::value; ++k) if (col + k * step < end) store_vector(grad + (row0 + r) * grad_stride + col + k * step, none);
+            });
+        }
+    }
+    // a lane looks at `per` neighbouring tokens of the list (an odd number, so that lanes are in different banks)
+    const int per = ((m + lpr - 1) >> q.lpr_shift) | 1, e0 = min(m, lane * per), e1 = min(m, e0 + per);
+    for (int j0 = 0; j0 < m; j0 += groups) {
+        const int j = min(j0 + g, m - 1), mine = list_key[j];
+        int less = 0, equal = 0, earlier = 0;
+        for (int e = e0; e < e1; ++e) {
+            const int k = list_key[e];
+            less += k < mine;
+            equal += k == mine;
+            earlier += k == mine && e < j;
+        }
+        const int own = equal;
+        int rank = equal;                                  // -> those of this lane and the lanes before it
+        for (int o = 1; o < lpr; o <<= 1) {
+            less += __shfl_xor(less, o);
+            equal += __shfl_xor(equal, o);
+            earlier += __shfl_xor(earlier, o);
+            const int x = __shfl_up(rank, o, lpr);
+            if (lane >= o) rank += x;
+        }
+        // (tokens of lower rows come first in `order`, so that the rows' parts of it are apart)
+        const bool owner = j0 + g < m && earlier == 0;
+        if (owner && own) {
+            rank += less - own;
+            for (int e = e0; e < e1; ++e)
+                if (list_key[e] == mine) order[rank++] = list_pos[e];
+        }
+        __syncthreads();
+        if (!owner) continue;
+        token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto v, int col, int end, int step) {
+            constexpr int UU = decltype(u)::value, NN = decltype(v)::value;
+            token_row<ADD, UU, NN>(q.scale, grad + (size_t)mine * grad_stride, col, end, step, [&](float (&acc)[UU][NN]) {
+                add_rows<(UU > 1 ? 4 : 8)>(acc, grad_out, stride, [&](int i) { return order[i]; }, less, less + equal, col, end, step);
+            });
+        });
+    }
+}
+
+// Zeros, one store to a lane: of what was tried (1, 2, 4, 8 stores of a lane to a row, contiguous or not, 1 to 8 rows, workgroups that go round) it
+// fills memory fastest (1 GB: 151 us, 170 to 270 us the others).
+template <class G>
+__global__ __launch_bounds__(TOK_THREADS) void k_token_zero(G* __restrict__ grad, int64_t stride, int64_t rows, int64_t dim, int lpr_shift, int tiles) {
+    constexpr int N = VECTOR<G>;
+    const Tile t = my_tile(tiles);
+    const int64_t row = ((int64_t)t.block * TOK_THREADS + threadIdx.x) >> lpr_shift;
+    const int64_t col = (((int64_t)t.tile << lpr_shift) + (threadIdx.x & ((1 << lpr_shift) - 1))) * N;
+    if (row >= rows || col >= dim) return;
+    const float none[N] = {};
+    store_from_float(grad + row * stride + col, none, (int)min((int64_t)N, dim - col));
+}
+
+// A gradient is written row by row, each once, where most rows may be in use or where it fits the memory-side cache (256 MB, with what is read);
+// else zeros go everywhere first, at the rate at which memory can be filled, and the rows in use are written again.
+// us a call, row by row / zeros first (16-bit rows in, f32 out; rows, columns, tokens): 131,072 x 64, 1024 19 / 23; 131,072 x 256, 16 k 51 / 56;
+// 131,072 x 384 (201 MB), 16 k 61 / 69; x 512 (268 MB) 105 / 90; x 2048, 16 k 313 / 240; 1 M x 64, 65 k 109 / 88; 131,072 x 1024, 131 k 285 / 269;
+// 32,768 x 4096, 65 k 340 / 373; 16,384 x 4096, 65 k 250 / 313; 1 M x 64, 1.7 M 265 / 278.
+static bool writes_every_row(int64_t n, int64_t rows, int64_t bytes) { return n >= rows || bytes < (int64_t)224 << 20; }
+
+struct TokenWork { size_t keys, runs, heads, ends, part, far, miles, bytes; };
 static TokenWork token_work(int64_t n, int64_t rows, int64_t dim) {
     TokenWork w;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) & ~(size_t)255; return p; };
     w.keys = take((size_t)n * 4);
-    w.first = take((size_t)rows * 4);
+    w.runs = take((size_t)rows * sizeof(TokenRun));
+    w.heads = take((size_t)cdiv(n, TOK_BLOCK) * 8);
+    w.ends = take((size_t)cdiv(n, TOK_BLOCK) * 4);
     w.part = take((size_t)(n / TOK_CHUNK) * dim * 4);
-    w.far_part = take((size_t)(n / TOK_STRETCH) * dim * 4);
+    w.far = take((size_t)(n / TOK_STRETCH) * dim * 4);
+    w.miles = take((size_t)(n / TOK_MILE) * dim * 4);
     w.bytes = at;
     return w;
 }
 size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim) { return token_work(n, rows, dim).bytes; }
 
-static int shift_for(int64_t dim, int per_lane) {
-    return __builtin_ctz(pow2_from(cdiv(dim, per_lane), TOK_THREADS));
+// log2 of the lanes of a row whose vectors have `per_lane` columns; enough of them for the columns left over to have a lane each
+static int shift_for(int dim, int per_lane, int most = 64) {
+    const int sh = __builtin_ctz(pow2_from(dim / per_lane, most));
+    return dim % per_lane && 1 << sh < per_lane ? __builtin_ctz(per_lane) : sh;
+}
+// workgroups beside one another on a row, at `columns` of its whole vectors each
+static int tiles_of(int dim, int per_lane, int64_t columns) { return (int)std::max<int64_t>(1, cdiv(dim / per_lane * per_lane, columns)); }
+
+// f(vectors that a lane takes of a row, as an integral constant); wider rows go to several workgroups
+template <int N, class F>
+static void by_vectors(int dim, int lpr_shift, F f) {
+    if (tiles_of(dim, N, (int64_t)N << lpr_shift) <= 1) f(std::integral_constant<int, 1>());
+    else f(std::integral_constant<int, 2>());
 }
 
 template <class S, class G>
 static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32_t* keys, int64_t n, int64_t rows, int dim, float scale, const TokenWork& w,
-                     G* grad, int64_t grad_stride, bool add) {
+                     TokenRun* runs, G* grad, int64_t grad_stride, bool add) {
     const hipStream_t st = d->stream;
     int bits = 1;
     while (((int64_t)1 << bits) <= rows) ++bits;                 // keys lie in [0, rows]
@@ -246,19 +528,74 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
     const int32_t *ks, *vs;
     FC_TRY(sort_in(j, d->sort, st, &ks, &vs));
     float* part = reinterpret_cast<float*>(d->work + w.part);
-    float* far_part = reinterpret_cast<float*>(d->work + w.far_part);
-    int32_t* first = add ? nullptr : reinterpret_cast<int32_t*>(d->work + w.first);
-    const int sh = shift_for(dim, VECTOR<S>);
-    const int64_t chunks = cdiv(n, TOK_CHUNK);
-    k_token_chunks<<<(unsigned)cdiv(chunks << sh, TOK_THREADS), TOK_THREADS, 0, st>>>(grad_out, stride, ks, vs, (int)n, (int)rows, dim, sh, part, first);
-    if (n >= TOK_STRETCH) {
-        const int s4 = shift_for(dim, 4);
-        k_token_stretches<<<(unsigned)cdiv((n / TOK_STRETCH) << s4, TOK_THREADS), TOK_THREADS, 0, st>>>(ks, (int)n, (int)rows, dim, s4, part, far_part);
+    float* far = reinterpret_cast<float*>(d->work + w.far);
+    float* miles = n >= TOK_MILES_FROM ? reinterpret_cast<float*>(d->work + w.miles) : nullptr;
+    uint64_t* heads = reinterpret_cast<uint64_t*>(d->work + w.heads);
+    int32_t* ends = reinterpret_cast<int32_t*>(d->work + w.ends);
+    {
+        const int sh = shift_for(dim, VECTOR<S>), threads = std::max(256, TOK_CHUNK << sh);
+        const int tiles = tiles_of(dim, VECTOR<S>, (int64_t)VECTOR<S> << sh);
+        k_token_chunks<<<(unsigned)(cdiv(cdiv(n, TOK_CHUNK), threads >> sh) * tiles), threads, (size_t)threads * VECTOR<S> * 4, st>>>(
+            grad_out, stride, ks, vs, (int)n, (int)rows, dim, sh, tiles, part, far, runs, heads, ends);
     }
-    constexpr int PER = 4;
-    const unsigned blocks = (unsigned)cdiv(cdiv(add ? n : rows, PER) << sh, TOK_THREADS);
-    if (add) k_token_rows<true, PER><<<blocks, TOK_THREADS, 0, st>>>(grad_out, stride, ks, vs, (int)n, (int)rows, dim, sh, scale, part, far_part, first, grad, grad_stride);
-    else k_token_rows<false, PER><<<blocks, TOK_THREADS, 0, st>>>(grad_out, stride, ks, vs, (int)n, (int)rows, dim, sh, scale, part, far_part, first, grad, grad_stride);
+    if (miles) {
+        const int sh = shift_for(dim, 4), tiles = tiles_of(dim, 4, (int64_t)4 << sh);
+        k_token_miles<<<(unsigned)(cdiv((n / TOK_MILE) << sh, TOK_THREADS) * tiles), TOK_THREADS, 0, st>>>(ks, (int)n, (int)rows, dim, sh, tiles, far, miles);
+    }
+    constexpr int N = VECTOR<G>;
+    TokenRows q{vs, part, far, miles, dim, shift_for(dim, N), 1, scale};
+    auto rows_of = [&](auto u) {
+        constexpr int U = decltype(u)::value;
+        q.tiles = tiles_of(dim, N, (int64_t)N * U << q.lpr_shift);
+        auto by_runs = [&](auto a) {
+            constexpr bool ADD = decltype(a)::value;
+            constexpr int PER = 8;                        // us a call, 2 / 4 / 8: 426 k tokens of 128 columns added to 1 M rows 113 / 107 / 105
+            k_token_runs<ADD, PER, U><<<(unsigned)(cdiv(cdiv(n, PER) << q.lpr_shift, TOK_THREADS) * q.tiles), TOK_THREADS, 0, st>>>(
+                q, grad_out, stride, ks, (int)n, (int)rows, heads, ends, grad, grad_stride);
+        };
+        if (add) by_runs(std::true_type());
+        else if (!runs) by_runs(std::false_type());
+        else {
+            constexpr int PER = 4;
+            k_token_rows<PER, U><<<(unsigned)(cdiv(cdiv(rows, PER) << q.lpr_shift, TOK_THREADS) * q.tiles), TOK_THREADS, 0, st>>>(q, grad_out, stride, runs, (int)rows, grad,
+                                                                                                                                 grad_stride);
+        }
+    };
+    by_vectors<N>(dim, q.lpr_shift, rows_of);
+    FC_HIP(hipGetLastError());
+    return FC_OK;
+}
+
+template <class S, class G, class I>
+static int token_bwd_few(fc_dense* d, const S* grad_out, int64_t stride, const I* ids, int64_t n, int64_t rows, int dim, float scale, int64_t padding_id,
+                         G* grad, int64_t grad_stride, bool add, bool zeros) {
+    constexpr int N = VECTOR<G>;
+    TokenRows q{nullptr, nullptr, nullptr, nullptr, dim, shift_for(dim, N), 1, scale};
+    by_vectors<N>(dim, q.lpr_shift, [&](auto u) {
+        constexpr int U = decltype(u)::value;
+        q.tiles = tiles_of(dim, N, (int64_t)N * U << q.lpr_shift);
+        const int groups = TOK_THREADS >> q.lpr_shift;
+        int per_block = 0;
+        int64_t blocks = cdiv(n, 16);                 // lists of some 16 tokens
+        if (zeros) {
+            per_block = groups * (int)std::max<int64_t>(1, std::min<int64_t>(TOK_FEW_ROWS / groups, rows * q.tiles / (groups * 4096)));
+            blocks = cdiv(rows, per_block);
+        }
+        const unsigned grid = (unsigned)(blocks * q.tiles);
+        if (add) k_token_few<true, U><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, 0, (unsigned)blocks, grad, grad_stride, d->flags);
+        else k_token_few<false, U><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, per_block, (unsigned)blocks, grad, grad_stride, d->flags);
+    });
+    FC_HIP(hipGetLastError());
+    return FC_OK;
+}
+
+template <class G>
+static int token_zero(fc_dense* d, G* grad, int64_t stride, int64_t rows, int64_t dim) {
+    constexpr int N = VECTOR<G>;
+    if (stride == dim) { dim *= rows; stride = dim; rows = 1; }
+    const int sh = __builtin_ctz(pow2_from(cdiv(dim, N), TOK_THREADS));
+    const int64_t tiles = cdiv(dim, (int64_t)N << sh);
+    k_token_zero<<<(unsigned)(cdiv(rows << sh, TOK_THREADS) * tiles), TOK_THREADS, 0, d->stream>>>(grad, stride, rows, dim, sh, (int)tiles);
     FC_HIP(hipGetLastError());
     return FC_OK;
 }
@@ -281,7 +618,7 @@ int token_embed_fwd(fc_dense* d, const void* table_dev, int32_t table_type, int6
         return with_type(out_type, [&](auto o) -> int {
             using S = decltype(s);
             using D = decltype(o);
-            const int sh = shift_for(dim, VECTOR<S>);
+            const int sh = shift_for(dim, VECTOR<S>, TOK_THREADS);
             auto run = [&](auto id) {
                 using I = decltype(id);
                 k_token_fwd<1><<<(unsigned)cdiv(n << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
@@ -304,27 +641,30 @@ int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type
     if (n == 0 && accumulate) return FC_OK;
     FC_HIP(hipSetDevice(d->device));
     const hipStream_t st = d->stream;
-    const TokenWork w = token_work(n, accumulate ? 0 : num_rows, dim);
-    if (n > 0) {
+    const bool add = accumulate != 0, every_row = !add && writes_every_row(n, num_rows, num_rows * dim * type_bytes(grad_table_type));
+    const TokenWork w = token_work(n, every_row ? num_rows : 0, dim);
+    int32_t* keys = nullptr;
+    TokenRun* runs = nullptr;
+    if (n > TOK_FEW) {
         FC_TRY(ensure_sort(d->sort, n));
         FC_TRY(dense_work(d, w.bytes));
-        int32_t* keys = reinterpret_cast<int32_t*>(d->work + w.keys);
-        int32_t* first = accumulate ? nullptr : reinterpret_cast<int32_t*>(d->work + w.first);
-        const unsigned blocks = (unsigned)cdiv(std::max<int64_t>(n, accumulate ? 0 : num_rows), TOK_THREADS);
+        keys = reinterpret_cast<int32_t*>(d->work + w.keys);
+        if (every_row) runs = reinterpret_cast<TokenRun*>(d->work + w.runs);
+        const unsigned blocks = (unsigned)cdiv(std::max<int64_t>(n, every_row ? num_rows : 0), TOK_THREADS);
         if (id_type == FC_TYPE_I32)
-            k_token_keys<<<blocks, TOK_THREADS, 0, st>>>((const int32_t*)ids_dev, n, (int)num_rows, padding_id, keys, first, d->flags);
-        else k_token_keys<<<blocks, TOK_THREADS, 0, st>>>((const int64_t*)ids_dev, n, (int)num_rows, padding_id, keys, first, d->flags);
+            k_token_keys<<<blocks, TOK_THREADS, 0, st>>>((const int32_t*)ids_dev, n, (int)num_rows, padding_id, keys, runs, d->flags);
+        else k_token_keys<<<blocks, TOK_THREADS, 0, st>>>((const int64_t*)ids_dev, n, (int)num_rows, padding_id, keys, runs, d->flags);
     }
     return with_type(grad_out_type, [&](auto s) -> int {
         using S = decltype(s);
+        const S* grad_out = (const S*)grad_out_dev;
         auto go = [&](auto* grad) -> int {
-            if (n == 0) {
-                k_token_no_rows<<<(unsigned)std::min<int64_t>(num_rows, 65536), TOK_THREADS, 0, st>>>(grad, grad_table_stride, num_rows, dim);
-                FC_HIP(hipGetLastError());
-                return FC_OK;
-            }
-            return token_bwd(d, (const S*)grad_out_dev, grad_out_stride, reinterpret_cast<const int32_t*>(d->work + w.keys), n, num_rows, dim, scale, w,
-                             grad, grad_table_stride, accumulate != 0);
+            if (!add && (!every_row || n == 0)) FC_TRY(token_zero(d, grad, grad_table_stride, num_rows, dim));
+            if (n > TOK_FEW) return token_bwd(d, grad_out, grad_out_stride, keys, n, num_rows, dim, scale, w, runs, grad, grad_table_stride, add);
+            if (n > 0 && id_type == FC_TYPE_I32)
+                return token_bwd_few(d, grad_out, grad_out_stride, (const int32_t*)ids_dev, n, num_rows, dim, scale, padding_id, grad, grad_table_stride, add, every_row);
+            if (n > 0) return token_bwd_few(d, grad_out, grad_out_stride, (const int64_t*)ids_dev, n, num_rows, dim, scale, padding_id, grad, grad_table_stride, add, every_row);
+            return FC_OK;
         };
         return grad_table_type == FC_TYPE_F32 ? go((float*)grad_table_dev) : go((S*)grad_table_dev);
     });
