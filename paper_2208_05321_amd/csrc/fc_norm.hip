@@ -26,6 +26,19 @@ __device__ __forceinline__ float nan_max(float a, float b) { return a > b || a !
 // lanes_of: lanes that hold one row; a workgroup has `threads` of them, 256 or one row's
 constexpr int norm_threads(int tpr) { return tpr < 256 ? 256 : tpr; }
 
+// Rows of whole vectors (WHOLE) need no code for partial ones, which is four fifths of a kernel that has it: 9 KB of instructions for 4096 16-bit
+// columns, fetched once a launch, and 4.1 us for a single row.
+template <bool WHOLE, int N, class T>
+__device__ __forceinline__ void load_some(float (&v)[N], const T* __restrict__ p, int live) {
+    if constexpr (WHOLE) load_vector(v, p);
+    else load_as_float(v, p, live);
+}
+template <bool WHOLE, int N, class T>
+__device__ __forceinline__ void store_some(T* __restrict__ p, const float (&v)[N], int live) {
+    if constexpr (WHOLE) store_vector(p, v);
+    else store_from_float(p, v, live);
+}
+
 // Sum of x over the TPR lanes of a row, in each of them.  lds: TPR / 64 words for each of the two turns that alternate, so that one barrier a
 // sum is enough.
 template <int TPR>
@@ -55,13 +68,13 @@ __device__ __forceinline__ float row_max(float x, float* lds) {
     return x;
 }
 
-template <int N, class T>
+template <bool WHOLE, class T, int N>
 __device__ __forceinline__ void load_weight(float (&v)[N], const void* w, bool f32, int col, int live) {
-    if (f32) load_as_float(v, (const float*)w + col, live);
-    else load_as_float(v, (const T*)w + col, live);
+    if (f32) load_some<WHOLE>(v, (const float*)w + col, live);
+    else load_some<WHOLE>(v, (const T*)w + col, live);
 }
 
-template <int N>
+template <bool WHOLE, int N>
 __device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], float inv, int live) {
     uint32_t word[N / 4];
 #pragma unroll
@@ -75,7 +88,7 @@ __device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], floa
         int x = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
         word[k / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], x, true);
     }
-    if (live >= N) {
+    if (WHOLE || live >= N) {
         typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
         V x;
 #pragma unroll
@@ -86,7 +99,7 @@ __device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], floa
         for (int k = 0; k < N; ++k) if (k < live) p[k].b = (uint8_t)(word[k / 4] >> (k % 4 * 8));
     }
 }
-template <int N>
+template <bool WHOLE, int N>
 __device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], float inv, int live) {
     typedef int8_t V __attribute__((ext_vector_type(N), aligned(1)));
     V x;
@@ -95,7 +108,7 @@ __device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], 
         const float t = rintf(v[k] * inv);
         x[k] = (int8_t)(t > 127.f ? 127.f : t < -127.f ? -127.f : t == t ? t : 0.f);
     }
-    if (live >= N) *reinterpret_cast<V*>(p) = x;
+    if (WHOLE || live >= N) *reinterpret_cast<V*>(p) = x;
     else {
 #pragma unroll
         for (int k = 0; k < N; ++k) if (k < live) p[k] = x[k];
@@ -112,7 +125,7 @@ struct NormFwd {
 };
 
 // KEEP: vectors of a row that a lane keeps in registers, 0: rows too wide for that, h is worked out again for each of the three steps
-template <int TPR, int KEEP, class T, class Q>
+template <int TPR, int KEEP, bool WHOLE, class T, class Q>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     constexpr int N = VECTOR<T>, NT = norm_threads(TPR), K = KEEP ? KEEP : 1;
     constexpr bool QUANT = QMAX<Q> > 0.f;
@@ -128,10 +141,10 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     float v[K][N];
     auto fetch = [&](float (&t)[N], int col) {
         const int live = a.dim - col;
-        load_as_float(t, x + col, live);
+        load_some<WHOLE>(t, x + col, live);
         if (r) {
             float s[N];
-            load_as_float(s, r + col, live);
+            load_some<WHOLE>(s, r + col, live);
 #pragma unroll
             for (int e = 0; e < N; ++e) t[e] = (float)(T)(t[e] + s[e]);
         }
@@ -152,7 +165,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     auto result = [&](float (&t)[N], int col) {                      // h -> y, and h stored on the way
         const int live = a.dim - col;
         float w[N];
-        load_weight<N, T>(w, a.weight, a.weight_f32, col, live);
+        load_weight<WHOLE, T>(w, a.weight, a.weight_f32, col, live);
 #pragma unroll
         for (int e = 0; e < N; ++e) t[e] = t[e] * rho * w[e];
     };
@@ -163,16 +176,16 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
         float (&t)[N] = v[KEEP ? k : 0];
         if (col < a.dim) {
             if (!KEEP) fetch(t, col);
-            if (KEEP && h) store_from_float(h + col, t, a.dim - col);
+            if (KEEP && h) store_some<WHOLE>(h + col, t, a.dim - col);
             result(t, col);
             if (!QUANT) {
                 if constexpr (!QUANT) {
                     if (!KEEP && h) {
                         float t0[N];
                         fetch(t0, col);
-                        store_from_float(h + col, t0, a.dim - col);
+                        store_some<WHOLE>(h + col, t0, a.dim - col);
                     }
-                    store_from_float(y + col, t, a.dim - col);
+                    store_some<WHOLE>(y + col, t, a.dim - col);
                 }
             } else
 #pragma unroll
@@ -190,9 +203,9 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
                     if (!KEEP && h) {
                         float t0[N];
                         fetch(t0, col);
-                        store_from_float(h + col, t0, a.dim - col);
+                        store_some<WHOLE>(h + col, t0, a.dim - col);
                     }
-                    store_quantised(y + col, t, scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f, a.dim - col);
+                    store_quantised<WHOLE>(y + col, t, scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f, a.dim - col);
                 }
             }
         }
@@ -214,10 +227,10 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) t0[e] = t[e];
                     result(t, col);
-                    store_from_float(h + col, t0, a.dim - col);
+                    store_some<WHOLE>(h + col, t0, a.dim - col);
                 } else result(t, col);
             }
-            store_quantised(y + col, t, inv, a.dim - col);
+            store_quantised<WHOLE>(y + col, t, inv, a.dim - col);
         }
     }
 }
@@ -232,7 +245,7 @@ struct NormBwd {
 };
 
 // KEEP as above; with 0 a workgroup adds to its row of `part` in memory
-template <int TPR, int KEEP, class T>
+template <int TPR, int KEEP, bool WHOLE, class T>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
     constexpr int N = VECTOR<T>, NT = norm_threads(TPR), GROUPS = NT / TPR, K = KEEP ? KEEP : 1;
     __shared__ float lds[4][TPR > 64 ? TPR / 64 : 1];
@@ -245,7 +258,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = (k * TPR + lane) * N;
-            if (col < a.dim) load_weight<N, T>(w[k], a.weight, a.weight_f32, col, a.dim - col);
+            if (col < a.dim) load_weight<WHOLE, T>(w[k], a.weight, a.weight_f32, col, a.dim - col);
 #pragma unroll
             for (int e = 0; e < N; ++e) { if (col >= a.dim) w[k][e] = 0.f; dw[k][e] = 0.f; }
         }
@@ -265,9 +278,9 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
         for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
             const int col = (k * TPR + lane) * N, b = KEEP ? k : 0;
             if (col < a.dim) {
-                load_as_float(g[b], dy + col, a.dim - col);
-                load_as_float(x[b], h + col, a.dim - col);
-                if (!KEEP) load_weight<N, T>(w[0], a.weight, a.weight_f32, col, a.dim - col);
+                load_some<WHOLE>(g[b], dy + col, a.dim - col);
+                load_some<WHOLE>(x[b], h + col, a.dim - col);
+                if (!KEEP) load_weight<WHOLE, T>(w[0], a.weight, a.weight_f32, col, a.dim - col);
             } else
 #pragma unroll
                 for (int e = 0; e < N; ++e) g[b][e] = x[b][e] = 0.f;
@@ -286,21 +299,21 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
             if (col >= a.dim) continue;
             const int live = a.dim - col;
             if (!KEEP) {
-                load_as_float(g[0], dy + col, live);
-                load_as_float(x[0], h + col, live);
-                load_weight<N, T>(w[0], a.weight, a.weight_f32, col, live);
-                load_as_float(dw[0], part + col, live);
+                load_some<WHOLE>(g[0], dy + col, live);
+                load_some<WHOLE>(x[0], h + col, live);
+                load_weight<WHOLE, T>(w[0], a.weight, a.weight_f32, col, live);
+                load_some<WHOLE>(dw[0], part + col, live);
             }
             float o[N];
-            if (in) load_as_float(o, in + col, live);
+            if (in) load_some<WHOLE>(o, in + col, live);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 dw[b][e] = fmaf(g[b][e], x[b][e] * rho, dw[b][e]);
                 const float t = rho * (g[b][e] * w[b][e] - x[b][e] * m);
                 o[e] = in ? o[e] + t : t;
             }
-            store_from_float(dx + col, o, live);
-            if (!KEEP) store_from_float(part + col, dw[0], live);
+            store_some<WHOLE>(dx + col, o, live);
+            if (!KEEP) store_some<WHOLE>(part + col, dw[0], live);
         }
     }
     if constexpr (KEEP > 0) {
@@ -308,7 +321,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int col = (k * TPR + lane) * N;
-                if (col < a.dim) store_from_float(part + col, dw[k], a.dim - col);
+                if (col < a.dim) store_some<WHOLE>(part + col, dw[k], a.dim - col);
             }
         } else {
 #pragma unroll
@@ -349,20 +362,58 @@ __global__ __launch_bounds__(DW_COLS * DW_PARTS) void k_norm_dw(const float* __r
 constexpr int NORM_BWD_BLOCKS = 1024;
 size_t norm_work_bytes(int64_t dim) { return (size_t)NORM_BWD_BLOCKS * dim * 4; }
 
-// f(lanes of a row, vectors a lane keeps) as integral constants
-template <int TPR_, int KEEP_> struct NormShape { static constexpr int TPR = TPR_, KEEP = KEEP_; };
+// f(shape): lanes of a row, vectors a lane keeps, whether rows are whole vectors.  Up to a wavefront a row's lanes are as many as its vectors.
+// Wider rows: a vector to a lane where there are few of them (`few`), which then wait for nothing but one round of loads; else more of them to a
+// lane, and fewer lanes.  Rows that end in a partial vector have six shapes.
+template <int TPR_, int KEEP_, bool WHOLE_> struct NormShape { static constexpr int TPR = TPR_, KEEP = KEEP_; static constexpr bool WHOLE = WHOLE_; };
 template <class F>
-static void norm_shape(int64_t vectors, F f) {
-    if (vectors <= 8) f(NormShape<8, 1>());
-    else if (vectors <= 16) f(NormShape<16, 1>());
-    else if (vectors <= 32) f(NormShape<32, 1>());
-    else if (vectors <= 64) f(NormShape<64, 1>());
-    else if (vectors <= 128) f(NormShape<64, 2>());
-    else if (vectors <= 256) f(NormShape<256, 1>());
-    else if (vectors <= 512) f(NormShape<256, 2>());
-    else if (vectors <= 1024) f(NormShape<256, 4>());
-    else if (vectors <= 4096) f(NormShape<1024, 4>());
-    else f(NormShape<1024, 0>());
+static void norm_shape(int64_t vectors, bool whole, bool few, F f) {
+    if (!whole) {
+        if (vectors <= 16) f(NormShape<16, 1, false>());
+        else if (vectors <= 64) f(NormShape<64, 1, false>());
+        else if (vectors <= 256) f(NormShape<256, 1, false>());
+        else if (vectors <= 1024) f(NormShape<256, 4, false>());
+        else if (vectors <= 4096) f(NormShape<1024, 4, false>());
+        else f(NormShape<1024, 0, false>());
+        return;
+    }
+    if (vectors <= 8) f(NormShape<8, 1, true>());
+    else if (vectors <= 16) f(NormShape<16, 1, true>());
+    else if (vectors <= 32) f(NormShape<32, 1, true>());
+    else if (vectors <= 64) f(NormShape<64, 1, true>());
+    else if (vectors <= 128 && !few) f(NormShape<64, 2, true>());
+    else if (vectors <= 256) f(NormShape<256, 1, true>());
+    else if (vectors <= 512 && few) f(NormShape<512, 1, true>());
+    else if (vectors <= 1024 && few) f(NormShape<1024, 1, true>());
+    else if (vectors <= 512) f(NormShape<256, 2, true>());
+    else if (vectors <= 1024) f(NormShape<256, 4, true>());
+    else if (vectors <= 4096) f(NormShape<1024, 4, true>());
+    else f(NormShape<1024, 0, true>());
+}
+constexpr int64_t NORM_FEW = 512;                  // rows
+
+// The backward pass keeps two rows, the weights and the weights' gradient: half as many vectors a lane (four: 202 registers, and with 1024 threads
+// they spill).
+template <class F>
+static void norm_bwd_shape(int64_t vectors, bool whole, F f) {
+    if (!whole) {
+        if (vectors <= 16) f(NormShape<16, 1, false>());
+        else if (vectors <= 64) f(NormShape<64, 1, false>());
+        else if (vectors <= 256) f(NormShape<256, 1, false>());
+        else if (vectors <= 1024) f(NormShape<512, 2, false>());
+        else f(NormShape<1024, 0, false>());
+        return;
+    }
+    if (vectors <= 8) f(NormShape<8, 1, true>());
+    else if (vectors <= 16) f(NormShape<16, 1, true>());
+    else if (vectors <= 32) f(NormShape<32, 1, true>());
+    else if (vectors <= 64) f(NormShape<64, 1, true>());
+    else if (vectors <= 128) f(NormShape<64, 2, true>());
+    else if (vectors <= 256) f(NormShape<256, 1, true>());
+    else if (vectors <= 512) f(NormShape<256, 2, true>());
+    else if (vectors <= 1024) f(NormShape<512, 2, true>());
+    else if (vectors <= 2048) f(NormShape<1024, 2, true>());
+    else f(NormShape<1024, 0, true>());
 }
 
 }  // namespace fc
@@ -386,13 +437,13 @@ int rms_norm_fwd(fc_dense* d, const void* x_dev, int32_t type, int64_t x_stride,
                     weight_type == FC_TYPE_F32, group, eps};
     return with_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        norm_shape(cdiv(dim, VECTOR<T>), [&](auto s) {
+        norm_shape(cdiv(dim, VECTOR<T>), dim % VECTOR<T> == 0, n < NORM_FEW, [&](auto s) {
             using S = decltype(s);
             constexpr int NT = norm_threads(S::TPR);
             const unsigned blocks = (unsigned)cdiv(n, NT / S::TPR);
-            if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, T, F8><<<blocks, NT, 0, d->stream>>>(a);
-            else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
-            else k_norm_fwd<S::TPR, S::KEEP, T, T><<<blocks, NT, 0, d->stream>>>(a);
+            if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, S::WHOLE, T, F8><<<blocks, NT, 0, d->stream>>>(a);
+            else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, S::WHOLE, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
+            else k_norm_fwd<S::TPR, S::KEEP, S::WHOLE, T, T><<<blocks, NT, 0, d->stream>>>(a);
         });
         FC_HIP(hipGetLastError());
         return FC_OK;
@@ -414,11 +465,11 @@ int rms_norm_bwd(fc_dense* d, const void* grad_y_dev, int64_t grad_y_stride, con
     int64_t blocks = 0;
     const int rc = with_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        if (n > 0) norm_shape(cdiv(dim, VECTOR<T>), [&](auto s) {
+        if (n > 0) norm_bwd_shape(cdiv(dim, VECTOR<T>), dim % VECTOR<T> == 0, [&](auto s) {
             using S = decltype(s);
             constexpr int NT = norm_threads(S::TPR);
             blocks = std::min<int64_t>(cdiv(n, NT / S::TPR), NORM_BWD_BLOCKS);
-            k_norm_bwd<S::TPR, S::KEEP, T><<<(unsigned)blocks, NT, 0, d->stream>>>(a);
+            k_norm_bwd<S::TPR, S::KEEP, S::WHOLE, T><<<(unsigned)blocks, NT, 0, d->stream>>>(a);
         });
         FC_HIP(hipGetLastError());
         return FC_OK;

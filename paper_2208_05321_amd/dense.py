@@ -32,9 +32,12 @@ class DenseOps:
         self._type = {getattr(torch, name): k for name, k in _TYPE_NAMES.items()}
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.device = self.stream.device
+        self._index, self._raw = self.device.index, self.stream.cuda_stream
+        # the current stream as a number: a tenth of a microsecond, where torch.cuda.current_stream takes two
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            rc = self._L.dense_create(ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h))
+            rc = self._L.dense_create(ctypes.c_void_p(self._raw), ctypes.byref(h))
         self._h = h if rc == 0 else None
         self._check(rc, "dense_create")
 
@@ -63,48 +66,48 @@ class DenseOps:
     # ---- arguments ----
     def _rows(self, t, what: str):
         """(type, rows, columns, distance of rows in elements) of a tensor whose leading dimensions have one distance between rows."""
-        if t.device != self.device:
+        if t.get_device() != self._index:
             _refuse(f"{what} is on {t.device}, the handle on {self.device}")
         k = self._type.get(t.dtype)
         if k is None:
             _refuse(f"{what}: type {t.dtype}")
-        shape, stride = t.shape, t.stride()
-        if t.dim() == 0 or shape[-1] == 0:
+        shape = t.shape
+        if not shape or shape[-1] == 0:
             _refuse(f"{what}: shape {tuple(shape)}")
         d = shape[-1]
         n = t.numel() // d
+        if t.is_contiguous() or n == 0:
+            return k, n, d, d
+        stride = t.stride()
         if d > 1 and stride[-1] != 1:
             _refuse(f"{what}: the elements of a row have to be neighbours")
-        if t.dim() == 2 and n > 1:
-            step = stride[0]
-        elif n <= 1:
+        step, size = None, 1            # leading dimensions, innermost first
+        for length, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+            if length == 1:
+                continue
+            if step is None:
+                step = st
+            elif st != step * size:
+                _refuse(f"{what}: rows have to be one distance apart")
+            size *= length
+        if step is None:
             step = d
-        else:
-            step, size = None, 1            # leading dimensions, innermost first
-            for length, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
-                if length == 1:
-                    continue
-                if step is None:
-                    step = st
-                elif st != step * size:
-                    _refuse(f"{what}: rows have to be one distance apart")
-                size *= length
         if step < d:
             _refuse(f"{what}: rows overlap")
         return k, n, d, step
 
     def _ids(self, ids):
-        if ids.device != self.device:
+        if ids.get_device() != self._index:
             _refuse(f"ids are on {ids.device}, the handle on {self.device}")
         k = self._type.get(ids.dtype)
-        if k not in (5, 6):
+        if k != 6 and k != 5:
             _refuse(f"ids: type {ids.dtype}")
         if not ids.is_contiguous():
             _refuse("ids have to be contiguous")
         return k
 
     def _vector(self, t, d: int, what: str, types):
-        if t.device != self.device:
+        if t.get_device() != self._index:
             _refuse(f"{what} is on {t.device}, the handle on {self.device}")
         k = self._type.get(t.dtype)
         if k not in types:
@@ -115,10 +118,10 @@ class DenseOps:
 
     def _run(self, what: str, call, tensors, *args):
         """The call, in order with the current stream where that is another one than the handle's."""
-        cur = self._torch.cuda.current_stream(self.device)
-        if cur == self.stream:
+        if self._current(self._index) == self._raw:
             rc = call(self._h, *args)
         else:
+            cur = self._torch.cuda.current_stream(self.device)
             self.stream.wait_stream(cur)
             rc = call(self._h, *args)
             for t in tensors:
@@ -138,9 +141,11 @@ class DenseOps:
         ik, n = self._ids(ids), ids.numel()
         if out is None:
             out = torch.empty((*ids.shape, d), dtype=out_dtype or table.dtype, device=self.device)
-        elif out.shape != (*ids.shape, d) or (out_dtype is not None and out.dtype != out_dtype):
-            _refuse("out: another shape or type")
-        ok, _, _, os = self._rows(out, "out")
+            ok, os = self._type.get(out.dtype), d
+        else:
+            if out.shape != (*ids.shape, d) or (out_dtype is not None and out.dtype != out_dtype):
+                _refuse("out: another shape or type")
+            ok, _, _, os = self._rows(out, "out")
         if tk not in _FLOATS or ok not in _FLOATS:
             _refuse(f"types {table.dtype} -> {out.dtype}")
         self._run("token_embed_fwd", self._L.token_embed_fwd, (table, ids, out), table.data_ptr(), tk, ts, rows, d, ids.data_ptr(), ik, n, scale,
@@ -160,9 +165,11 @@ class DenseOps:
             if accumulate:
                 _refuse("accumulate needs grad")
             grad = torch.empty((num_rows, d), dtype=grad_dtype or torch.float32, device=self.device)
-        elif grad.shape != (num_rows, d) or (grad_dtype is not None and grad.dtype != grad_dtype):
-            _refuse("grad: another shape or type")
-        tk, _, _, ts = self._rows(grad, "grad")
+            tk, ts = self._type.get(grad.dtype), d
+        else:
+            if grad.shape != (num_rows, d) or (grad_dtype is not None and grad.dtype != grad_dtype):
+                _refuse("grad: another shape or type")
+            tk, _, _, ts = self._rows(grad, "grad")
         if tk != 0 and tk != gk:
             _refuse(f"types {grad_out.dtype} -> {grad.dtype}")
         self._run("token_embed_bwd", self._L.token_embed_bwd, (grad_out, ids, grad), grad_out.data_ptr(), gk, gs, ids.data_ptr(), ik, n, num_rows, d,
@@ -186,15 +193,22 @@ class DenseOps:
             if rk != k or residual.shape != x.shape:
                 _refuse("residual: another shape or type than x")
             rp = residual.data_ptr()
-            h = h_out if h_out is not None else torch.empty(x.shape, dtype=x.dtype, device=self.device)
-            hk, _, _, hs = self._rows(h, "h_out")
-            if hk != k or h.shape != x.shape:
-                _refuse("h_out: another shape or type than x")
+            if h_out is None:
+                h = torch.empty(x.shape, dtype=x.dtype, device=self.device)
+            else:
+                h = h_out
+                hk, _, _, hs = self._rows(h, "h_out")
+                if hk != k or h.shape != x.shape:
+                    _refuse("h_out: another shape or type than x")
             hp = h.data_ptr()
         elif h_out is not None:
             _refuse("h_out without residual: h is x")
-        y = out if out is not None else torch.empty(x.shape, dtype=out_dtype or x.dtype, device=self.device)
-        yk, _, _, ys = self._rows(y, "out")
+        if out is None:
+            y = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=self.device)
+            yk, ys = self._type.get(y.dtype), d
+        else:
+            y = out
+            yk, _, _, ys = self._rows(y, "out")
         if y.shape != x.shape or (out_dtype is not None and y.dtype != out_dtype) or yk not in (k, 3, 4):
             _refuse(f"out: {tuple(y.shape)} {y.dtype}")
         scales = None
@@ -223,10 +237,13 @@ class DenseOps:
             if gk != k or grad_h.shape != h.shape:
                 _refuse("grad_h: another shape or type than h")
             gp = grad_h.data_ptr()
-        dx = out if out is not None else torch.empty(h.shape, dtype=h.dtype, device=self.device)
-        dk, _, _, ds = self._rows(dx, "out")
-        if dk != k or dx.shape != h.shape:
-            _refuse("out: another shape or type than h")
+        if out is None:
+            dx, ds = torch.empty(h.shape, dtype=h.dtype, device=self.device), d
+        else:
+            dx = out
+            dk, _, _, ds = self._rows(dx, "out")
+            if dk != k or dx.shape != h.shape:
+                _refuse("out: another shape or type than h")
         dw = torch.empty(d, dtype=grad_weight_dtype or weight.dtype, device=self.device)
         wt = self._type.get(dw.dtype)
         if wt not in _FLOATS:
@@ -236,34 +253,32 @@ class DenseOps:
         return dx, dw
 
     # ---- clipping ----
-    def _dense_tensors(self, tensors, what: str):
-        types = self._type
-        for t in tensors:
-            if types.get(t.dtype) not in _FLOATS or t.device != self.device:
-                _refuse(f"{what}: {t.dtype} on {t.device}")
-            if not t.is_contiguous():
-                _refuse(f"{what}: tensors have to be contiguous")
+    def _tensors(self, tensors, what: str):
+        """(addresses, sizes, types) of contiguous tensors, as lists."""
+        T = self._torch.Tensor
+        kinds = [self._type.get(t.dtype, -1) for t in tensors]
+        if not all(map(T.is_contiguous, tensors)):
+            _refuse(f"{what}: tensors have to be contiguous")
+        if set(kinds) - {0, 1, 2} or set(map(T.get_device, tensors)) - {self._index}:
+            _refuse(f"{what}: f32, bf16 or f16 on {self.device} is wanted")
+        return list(map(T.data_ptr, tensors)), list(map(T.numel, tensors)), kinds
 
     def grad_norm_clip(self, grads, max_norm: float, out=None):
         """Global norm of the tensors (f32 [1]), which are scaled by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
         torch = self._torch
         grads = list(grads)
-        self._dense_tensors(grads, "grads")
-        n = len(grads)
-        outs = None
+        src, sizes, kinds = self._tensors(grads, "grads")
+        dst = None
         if out is not None:
             out = list(out)
-            self._dense_tensors(out, "out")
-            if len(out) != n or any(a.dtype != b.dtype or a.numel() != b.numel() for a, b in zip(grads, out)):
+            dst, out_sizes, out_kinds = self._tensors(out, "out")
+            if out_sizes != sizes or out_kinds != kinds:
                 _refuse("out: other sizes or types than grads")
-            outs = array("Q", [t.data_ptr() for t in out])
+            dst = array("Q", dst)
         if not max_norm > 0:
             _refuse(f"max_norm {max_norm}")
-        types = self._type
-        src = array("Q", [t.data_ptr() for t in grads])
-        sizes = array("q", [t.numel() for t in grads])
-        kinds = array("i", [types[t.dtype] for t in grads])
+        src, sizes, kinds = array("Q", src), array("q", sizes), array("i", kinds)
         norm = torch.empty(1, dtype=torch.float32, device=self.device)
         self._run("grad_norm_clip", self._L.grad_norm_clip, (*grads, *(out or ()), norm), src.buffer_info()[0],
-                  outs.buffer_info()[0] if outs is not None else None, sizes.buffer_info()[0], kinds.buffer_info()[0], n, max_norm, norm.data_ptr())
+                  dst.buffer_info()[0] if dst is not None else None, sizes.buffer_info()[0], kinds.buffer_info()[0], len(grads), max_norm, norm.data_ptr())
         return norm
