@@ -350,7 +350,8 @@ typedef struct fc_dense fc_dense; /* opaque: stream, workspace, sticky error; on
 int dense_create(void* hip_stream, fc_dense** out);
 /* Allocate now what calls up to these sizes need beyond the caller's memory (token_embed_bwd: max_tokens ids of a table of max_rows rows;
  * max_dim columns; grad_norm_clip: max_tensors tensors).  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
- * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured.  Synchronous.  Errors: INVALID_ARG, OOM_DEVICE, HIP. */
+ * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured into a graph; buffers that a captured call uses stay
+ * until dense_destroy.  Synchronous.  Errors: INVALID_ARG, OOM_DEVICE, HIP. */
 int dense_reserve(fc_dense* d, int64_t max_tokens, int64_t max_rows, int32_t max_dim, int32_t max_tensors);
 /* Wait for the handle's stream and return the sticky error, if any (then clears it): FC_ERR_ID_OUT_OF_RANGE. */
 int dense_check(fc_dense* d);

@@ -12,6 +12,11 @@ struct fc_dense {
     fc::SortBufs sort;                  // token_embed_bwd
     char* work = nullptr;               // what one call needs beyond that, laid out by the call
     size_t work_cap = 0;
+    // A graph that was captured from calls of this handle holds addresses of its buffers: from the first capture on, buffers that are replaced by
+    // larger ones are kept until the handle goes.
+    bool captured = false;
+    struct Kept { void* p; Kept* next; };
+    Kept* kept = nullptr;
 };
 
 namespace fc {
@@ -93,6 +98,8 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
 inline int pow2_from(int64_t x, int most) { int p = 1; while (p < x && p < most) p <<= 1; return p; }
 
 int dense_work(fc_dense* d, size_t bytes);     // d->work holds that many bytes
+int dense_sort(fc_dense* d, int64_t n);        // d->sort holds n pairs
+int dense_capturing(fc_dense* d, bool* now);   // whether the handle's stream is being captured
 size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim);
 size_t norm_work_bytes(int64_t dim);
 size_t clip_work_bytes(int64_t tensors);

@@ -526,7 +526,14 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
     SortJob j;
     j.src = SORT_SRC_SLOTS; j.keys_in = keys; j.n = (int)n; j.num_bags = (int)n; j.one_per_bag = true; j.limit = (int)rows; j.bits = bits;
     const int32_t *ks, *vs;
-    FC_TRY(sort_in(j, d->sort, st, &ks, &vs));
+    bool captured;
+    FC_TRY(dense_capturing(d, &captured));
+    if (captured) {
+        // which of the sort's two tables is clean is known for work in order, not for a graph that is replayed: one without tables
+        SortBufs& b = d->sort;
+        j.keysA = b.keysA; j.valsA = b.valsA; j.keysB = b.keysB; j.valsB = b.valsB; j.ghist = b.ghist; j.dtot = b.dtot;
+        FC_TRY(sort_small_fits(j) ? sort_small(j, st, &ks, &vs) : radix_sort(j, st, &ks, &vs));
+    } else FC_TRY(sort_in(j, d->sort, st, &ks, &vs));
     float* part = reinterpret_cast<float*>(d->work + w.part);
     float* far = reinterpret_cast<float*>(d->work + w.far);
     float* miles = n >= TOK_MILES_FROM ? reinterpret_cast<float*>(d->work + w.miles) : nullptr;
@@ -646,7 +653,7 @@ int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type
     int32_t* keys = nullptr;
     TokenRun* runs = nullptr;
     if (n > TOK_FEW) {
-        FC_TRY(ensure_sort(d->sort, n));
+        FC_TRY(dense_sort(d, n));
         FC_TRY(dense_work(d, w.bytes));
         keys = reinterpret_cast<int32_t*>(d->work + w.keys);
         if (every_row) runs = reinterpret_cast<TokenRun*>(d->work + w.runs);
