@@ -24,35 +24,47 @@ constexpr int TOK_STRETCH = TOK_CHUNK * TOK_CHUNK, TOK_MILE = TOK_CHUNK * TOK_ST
 constexpr int64_t TOK_MILES_FROM = 8 * TOK_MILE;  // tokens from which on miles are added up: fewer cost a row less than the launch
 constexpr int TOK_BLOCK = 64;                     // sorted tokens whose run heads are one word
 
-// ---- forward ----
-// Rows are walked in vectors of N columns; the columns left over at the end (fewer than N) are taken by a lane each, in code of their own:
-// with a partial vector handled wherever one is loaded or stored, the backward pass's kernels grew to 1200 branches and waited for their
-// own instructions (dense gradient of 131,072 rows of 2048 columns: 380 us).
-template <int ROWS, int N, class S, class D>
-__device__ __forceinline__ void token_columns(const S* const (&row)[ROWS], float scale, D* __restrict__ out, int64_t out_stride, int64_t rows, int col, int end, int step) {
-    for (; col < end; col += step) {
-        float v[ROWS][N];
+// ---- columns ----
+// A row is walked in vectors of N columns, a lane each.  The last one ends with the row: where the width is no multiple of N it overlaps the one
+// before it, and both lanes work out, and store, the same values in the columns that they share.  (With a partial vector handled wherever one is loaded or
+// stored the backward pass's kernels grew to 1200 branches and waited for their own instructions: dense gradient of 131,072 rows of 2048 columns 380
+// us; with the columns left over done after the others every row took its chain of loads twice: 1.8 M rows of 55, 436 k tokens 191.)  Rows
+// narrower than a vector have kernels with N = 1.
+// Cols: first columns of the U vectors that a lane takes of a row, -1 where it has none.
+template <int U> struct Cols { int at[U]; };
+// Workgroups that share a row's columns are neighbours; each has `per_tile` vectors.
+struct Tiles { int dim, lpr_shift, per_tile, tiles; };
+template <int U, int N>
+__device__ __forceinline__ Cols<U> my_cols(const Tiles& q, int tile) {
+    const int lane = threadIdx.x & ((1 << q.lpr_shift) - 1), end = min((q.dim + N - 1) / N, (tile + 1) * q.per_tile);
+    Cols<U> c;
 #pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            if (row[k]) load_vector(v[k], row[k] + col);
-        }
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            if (k >= rows) break;
-            // (a row of an id outside stays zero even where the scale is infinite)
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[k][e] = row[k] ? v[k][e] * scale : 0.f;
-            store_vector(out + k * out_stride + col, v[k]);
-        }
+    for (int u = 0; u < U; ++u) {
+        const int v = tile * q.per_tile + (u << q.lpr_shift) + lane;
+        c.at[u] = v < end ? min(v * N, q.dim - N) : -1;
     }
+    return c;
+}
+struct Tile { unsigned block; int tile; };
+__device__ __forceinline__ Tile my_tile(const Tiles& q) {
+    const unsigned b = blockIdx.x / (unsigned)q.tiles;
+    return Tile{b, (int)(blockIdx.x - b * (unsigned)q.tiles)};
+}
+static Tiles tiles_of(int dim, int per_lane, int vectors) {
+    const int nv = (int)cdiv(dim, per_lane), sh = __builtin_ctz(pow2_from(nv, 64));
+    Tiles q{dim, sh, 0, (int)cdiv(nv, vectors << sh)};
+    q.per_tile = (int)cdiv(nv, q.tiles);
+    // two vectors that overlap belong to one wavefront: it reads what it adds to before it stores anything
+    while (q.tiles > 1 && dim % per_lane && (nv - 1) % q.per_tile == 0) { --q.per_tile; q.tiles = (int)cdiv(nv, q.per_tile); }
+    return q;
 }
 
-template <int ROWS, class S, class D, class I>
+// ---- forward ----
+template <int ROWS, int N, class S, class D, class I>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_fwd(const S* __restrict__ table, int64_t table_stride, int rows, int dim, int lpr_shift,
                                                            const I* __restrict__ ids, int64_t n, float scale, D* __restrict__ out,
                                                            int64_t out_stride, uint32_t* flags) {
-    constexpr int N = VECTOR<S>;
-    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1);
+    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1), vectors = (dim + N - 1) / N;
     const int64_t first = (((int64_t)blockIdx.x * TOK_THREADS + threadIdx.x) >> lpr_shift) * ROWS;
     const S* row[ROWS];
     bool bad = false;
@@ -64,21 +76,24 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_fwd(const S* __restrict__
         row[k] = ok ? table + (size_t)id * table_stride : nullptr;
     }
     if (bad && lane == 0 && first < n) atomicOr(flags, EF_ID_RANGE);
-    const int whole = dim & -N;
-    D* const o = out + first * out_stride;
-    token_columns<ROWS, N>(row, scale, o, out_stride, n - first, lane * N, whole, lpr * N);
-    if (whole != dim) token_columns<ROWS, 1>(row, scale, o, out_stride, n - first, whole + lane, dim, lpr);
+    for (int c = lane; c < vectors; c += lpr) {
+        const int col = min(c * N, dim - N);
+        float v[ROWS][N];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k)
+            if (row[k]) load_vector(v[k], row[k] + col);
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            if (first + k >= n) break;
+            // (a row of an id outside stays zero even where the scale is infinite)
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[k][e] = row[k] ? v[k][e] * scale : 0.f;
+            store_vector(out + (first + k) * out_stride + col, v[k]);
+        }
+    }
 }
 
 // ---- backward ----
-// Workgroups that share a row's columns are neighbours.
-struct Tile { unsigned block; int tile; bool last; };
-__device__ __forceinline__ Tile my_tile(int tiles) {
-    const unsigned b = blockIdx.x / (unsigned)tiles;
-    const int t = (int)(blockIdx.x - b * (unsigned)tiles);
-    return Tile{b, t, t == tiles - 1};
-}
-
 // Where an id's tokens begin and end among the sorted ones; begin < 0: it has none.
 struct TokenRun { int begin, end; };
 
@@ -99,10 +114,10 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_keys(const I* __restrict_
     if (bad) atomicOr(flags, EF_ID_RANGE);
 }
 
-// acc += the rows at(a) .. at(b - 1) of src, in order: U vectors of N columns, `step` columns apart, those before `end`.  AT rows' loads are on
-// their way together; the last ones that do not make AT go in halves of it, with rows beyond the last read again and not counted.
+// acc += the rows at(a) .. at(b - 1) of src, in order.  AT rows' loads are on their way together; the last ones that do not make AT go in halves
+// of it, with the last row read again in the place of rows beyond it, and not counted.
 template <int AT, int U, int N, class S, class F>
-__device__ __forceinline__ void add_rows(float (&acc)[U][N], const S* __restrict__ src, int64_t stride, F at, int a, int b, int col, int end, int step) {
+__device__ __forceinline__ void add_rows(float (&acc)[U][N], const S* __restrict__ src, int64_t stride, F at, int a, int b, const Cols<U>& c) {
     auto batch = [&](auto size, bool whole) {
         constexpr int B = decltype(size)::value;
         int p[B];
@@ -111,9 +126,9 @@ __device__ __forceinline__ void add_rows(float (&acc)[U][N], const S* __restrict
         float v[B][U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (col + u * step < end)
+            if (c.at[u] >= 0)
 #pragma unroll
-                for (int k = 0; k < B; ++k) load_vector(v[k][u], src + (size_t)p[k] * stride + col + u * step);
+                for (int k = 0; k < B; ++k) load_vector(v[k][u], src + (size_t)p[k] * stride + c.at[u]);
 #pragma unroll
         for (int k = 0; k < B; ++k)
             if (whole || a + k < b)
@@ -174,109 +189,91 @@ __device__ __forceinline__ bool one_row(const int32_t* __restrict__ keys, int n,
 }
 
 // Chunks and stretches inside one run: a row-group to a chunk, 16 neighbouring ones to a stretch, whose sum they work out together; the
-// chunks of such a stretch are not asked for.  Columns first .. end of the row, N to a lane.
+// chunks of such a stretch are not asked for.  Threads: 16 row-groups, or 256.
 template <int N, class S>
-__device__ __forceinline__ void chunk_sum(const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ vals, bool chunk, bool stretch, bool any_stretch,
-                                          int64_t c, float* __restrict__ part, float* __restrict__ far, int dim, int first, int end, int lpr_shift, float* lds) {
-    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1), col = first + lane * N, row0 = (int)c * TOK_CHUNK;
-    float acc[1][N] = {};
-    if (chunk && col < end) {
-        add_rows<8>(acc, grad_out, stride, [=](int i) { return vals[i]; }, row0, row0 + TOK_CHUNK, col, end, 0);
-        if (!stretch) store_vector(part + c * dim + col, acc[0]);
-    }
-    if (!any_stretch) return;
-    const int nt = blockDim.x;
-#pragma unroll
-    for (int e = 0; e < N; ++e) lds[e * nt + threadIdx.x] = acc[0][e];
-    __syncthreads();
-    if (stretch) {
-        // element j of the stretch's lpr * N columns: e = j / lpr, lane = j % lpr
-        const int base = threadIdx.x & ~((TOK_CHUNK << lpr_shift) - 1), t = threadIdx.x - base;
-        for (int j = t; j < lpr * N; j += TOK_CHUNK << lpr_shift) {
-            const int e = j >> lpr_shift, l = j & (lpr - 1), at = first + l * N + e;
-            if (at >= end) continue;
-            float s = 0.f;
-#pragma unroll
-            for (int k = 0; k < TOK_CHUNK; ++k) s += lds[e * nt + base + (k << lpr_shift) + l];
-            far[c / TOK_CHUNK * dim + at] = s;
-        }
-    }
-    __syncthreads();
-}
-
-// threads: 16 row-groups, or 256
-template <class S>
-__global__ __launch_bounds__(1024) void k_token_chunks(const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys,
-                                                       const int32_t* __restrict__ vals, int n, int rows, int dim, int lpr_shift, int tiles,
-                                                       float* __restrict__ part, float* __restrict__ far, TokenRun* __restrict__ runs,
-                                                       uint64_t* __restrict__ heads, int32_t* __restrict__ ends) {
-    constexpr int N = VECTOR<S>;
+__global__ __launch_bounds__(1024) void k_token_chunks(Tiles q, const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys,
+                                                       const int32_t* __restrict__ vals, int n, int rows, float* __restrict__ part, float* __restrict__ far,
+                                                       TokenRun* __restrict__ runs, uint64_t* __restrict__ heads, int32_t* __restrict__ ends) {
     extern __shared__ float chunk_lds[];
-    const int groups = blockDim.x >> lpr_shift;
-    const Tile t = my_tile(tiles);
-    const int64_t c = (int64_t)t.block * groups + (threadIdx.x >> lpr_shift);
+    const int groups = blockDim.x >> q.lpr_shift, lpr = 1 << q.lpr_shift;
+    const Tile t = my_tile(q);
+    const int64_t c = (int64_t)t.block * groups + (threadIdx.x >> q.lpr_shift);
     if (t.tile == 0) mark_runs(keys, n, rows, (int64_t)t.block * groups * TOK_CHUNK, groups * TOK_CHUNK, runs, heads, ends);
     const bool chunk = one_row(keys, n, rows, c * TOK_CHUNK, TOK_CHUNK);
     const bool stretch = chunk && one_row(keys, n, rows, c / TOK_CHUNK * TOK_STRETCH, TOK_STRETCH);
     const bool any = __syncthreads_or(stretch);
-    const int whole = dim & -N;
-    chunk_sum<N>(grad_out, stride, vals, chunk, stretch, any, c, part, far, dim, t.tile * (N << lpr_shift), whole, lpr_shift, chunk_lds);
-    if (whole != dim && t.last)
-        chunk_sum<1>(grad_out, stride, vals, chunk, stretch, any, c, part, far, dim, whole, dim, lpr_shift, chunk_lds);
+    const Cols<1> cols = my_cols<1, N>(q, t.tile);
+    const int row0 = (int)c * TOK_CHUNK;
+    float acc[1][N] = {};
+    if (chunk && cols.at[0] >= 0) {
+        add_rows<8>(acc, grad_out, stride, [=](int i) { return vals[i]; }, row0, row0 + TOK_CHUNK, cols);
+        if (!stretch) store_vector(part + c * q.dim + cols.at[0], acc[0]);
+    }
+    if (!any) return;
+    const int nt = blockDim.x;
+#pragma unroll
+    for (int e = 0; e < N; ++e) chunk_lds[e * nt + threadIdx.x] = acc[0][e];
+    __syncthreads();
+    if (!stretch) return;
+    // element j of the stretch's lpr * N columns: the e-th, e = j / lpr, of lane j % lpr
+    const int base = threadIdx.x & ~((TOK_CHUNK << q.lpr_shift) - 1), end = min((q.dim + N - 1) / N, (t.tile + 1) * q.per_tile);
+    for (int j = threadIdx.x - base; j < lpr * N; j += TOK_CHUNK << q.lpr_shift) {
+        const int e = j >> q.lpr_shift, l = j & (lpr - 1), v = t.tile * q.per_tile + l;
+        if (v >= end) continue;
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < TOK_CHUNK; ++k) s += chunk_lds[e * nt + base + (k << q.lpr_shift) + l];
+        far[c / TOK_CHUNK * q.dim + min(v * N, q.dim - N) + e] = s;
+    }
 }
 
 // Miles inside one run, out of the stretches' sums: a row-group each.
-__global__ __launch_bounds__(TOK_THREADS) void k_token_miles(const int32_t* __restrict__ keys, int n, int rows, int dim, int lpr_shift, int tiles,
-                                                             const float* __restrict__ far, float* __restrict__ miles) {
-    const int lpr = 1 << lpr_shift, lane = threadIdx.x & (lpr - 1);
-    const Tile t = my_tile(tiles);
-    const int64_t m = ((int64_t)t.block * TOK_THREADS + threadIdx.x) >> lpr_shift;
+template <int N>
+__global__ __launch_bounds__(TOK_THREADS) void k_token_miles(Tiles q, const int32_t* __restrict__ keys, int n, int rows, const float* __restrict__ far,
+                                                             float* __restrict__ miles) {
+    const Tile t = my_tile(q);
+    const int64_t m = ((int64_t)t.block * TOK_THREADS + threadIdx.x) >> q.lpr_shift;
     if (!one_row(keys, n, rows, m * TOK_MILE, TOK_MILE)) return;
-    auto columns = [&](auto w, int col, int end) {
-        float acc[1][decltype(w)::value] = {};
-        if (col >= end) return;
-        add_rows<TOK_CHUNK>(acc, far, dim, [](int i) { return i; }, (int)m * TOK_CHUNK, ((int)m + 1) * TOK_CHUNK, col, end, 0);
-        store_vector(miles + m * dim + col, acc[0]);
-    };
-    const int whole = dim & -4;
-    columns(std::integral_constant<int, 4>(), (t.tile * lpr + lane) * 4, whole);
-    if (whole != dim && t.last) columns(std::integral_constant<int, 1>(), whole + lane, dim);
+    const Cols<1> cols = my_cols<1, N>(q, t.tile);
+    if (cols.at[0] < 0) return;
+    float acc[1][N] = {};
+    add_rows<TOK_CHUNK>(acc, far, q.dim, [](int i) { return i; }, (int)m * TOK_CHUNK, ((int)m + 1) * TOK_CHUNK, cols);
+    store_vector(miles + m * q.dim + cols.at[0], acc[0]);
 }
 
 struct TokenRows {
+    Tiles t;
     const int32_t* vals;
     const float *part, *far, *miles;              // sums of chunks, stretches, miles (null: none are there)
-    int dim, lpr_shift, tiles;
     float scale;
 };
 
 // U vectors of a lane in one row of the gradient: the sum of rows, scaled, stored or added.
 template <bool ADD, int U, int N, class G, class F>
-__device__ __forceinline__ void token_row(float scale, G* __restrict__ out, int col, int end, int step, F sum) {
+__device__ __forceinline__ void token_row(float scale, G* __restrict__ out, const Cols<U>& c, F sum) {
     float acc[U][N] = {}, old[U][N];
     if (ADD) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) if (col + u * step < end) load_vector(old[u], out + col + u * step);
+        for (int u = 0; u < U; ++u) if (c.at[u] >= 0) load_vector(old[u], out + c.at[u]);
     }
     sum(acc);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (col + u * step >= end) break;
+        if (c.at[u] < 0) break;
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[u][e] = ADD ? fmaf(acc[u][e], scale, old[u][e]) : acc[u][e] * scale;
-        store_vector(out + col + u * step, acc[u]);
+        store_vector(out + c.at[u], acc[u]);
     }
 }
 
 // Sorted tokens a .. b - 1, with the chunks, stretches and miles among them already summed.  token(i): the i-th sorted token.
 template <int U, int N, class S, class F>
-__device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, const S* __restrict__ grad_out, int64_t stride, F token, int a, int b, int col, int end,
-                                        int step) {
+__device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, const S* __restrict__ grad_out, int64_t stride, F token, int a, int b, const Cols<U>& c) {
     constexpr int AT = U > 1 ? 4 : 8;             // loads of a lane on their way together: more cost wavefronts
     int c0 = (a + TOK_CHUNK - 1) / TOK_CHUNK, c1 = b / TOK_CHUNK;
     const bool parts = c0 < c1;
     for (int k = 0; k < (parts ? 2 : 1); ++k)     // before the first chunk, after the last
-        add_rows<AT>(acc, grad_out, stride, token, k ? c1 * TOK_CHUNK : a, parts && !k ? c0 * TOK_CHUNK : b, col, end, step);
+        add_rows<AT>(acc, grad_out, stride, token, k ? c1 * TOK_CHUNK : a, parts && !k ? c0 * TOK_CHUNK : b, c);
     if (!parts) return;
     const float* src = q.part;
     for (int level = 0; level < 3; ++level) {     // chunks before the first stretch and after the last; and so on
@@ -284,109 +281,100 @@ __device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, 
         const int s0 = (c0 + TOK_CHUNK - 1) / TOK_CHUNK, s1 = c1 / TOK_CHUNK;
         const bool more = next && s0 < s1;
         for (int k = 0; k < (more ? 2 : 1); ++k)
-            add_rows<AT>(acc, src, q.dim, [](int i) { return i; }, k ? s1 * TOK_CHUNK : c0, more && !k ? s0 * TOK_CHUNK : c1, col, end, step);
+            add_rows<AT>(acc, src, q.t.dim, [](int i) { return i; }, k ? s1 * TOK_CHUNK : c0, more && !k ? s0 * TOK_CHUNK : c1, c);
         if (!more) return;
         src = next; c0 = s0; c1 = s1;
     }
 }
 
-// f(vectors of a lane, their columns, first column, end): a workgroup's columns of a row, and in the last workgroup of a row what is left over
-template <int U, int N, class F>
-__device__ __forceinline__ void token_tile(int dim, int lpr_shift, const Tile& t, F f) {
-    const int lane = threadIdx.x & ((1 << lpr_shift) - 1), step = N << lpr_shift, whole = dim & -N;
-    f(std::integral_constant<int, U>(), std::integral_constant<int, N>(), t.tile * step * U + lane * N, whole, step);
-    if (whole != dim && t.last) f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>(), whole + lane, dim, 0);
-}
-
 // Every row of the gradient; a row-group takes PER of them, whose runs it reads together, and a workgroup's groups neighbours at a time.
-template <int PER, int U, class S, class G>
+template <int PER, int U, int N, class S, class G>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_rows(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const TokenRun* __restrict__ runs,
                                                             int rows, G* __restrict__ grad, int64_t grad_stride) {
-    const Tile tile = my_tile(q.tiles);
-    const int groups = TOK_THREADS >> q.lpr_shift;
-    const int64_t at = (int64_t)tile.block * groups * PER + (threadIdx.x >> q.lpr_shift);
+    const Tile tile = my_tile(q.t);
+    const Cols<U> cols = my_cols<U, N>(q.t, tile.tile);
+    const int groups = TOK_THREADS >> q.t.lpr_shift;
+    const int64_t at = (int64_t)tile.block * groups * PER + (threadIdx.x >> q.t.lpr_shift);
     TokenRun run[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) run[k] = runs[min(at + k * groups, (int64_t)rows - 1)];
-    token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto w, int col, int end, int step) {
-        constexpr int UU = decltype(u)::value, NN = decltype(w)::value;
-        const float none[NN] = {};
+    const float none[N] = {};
 #pragma unroll
-        for (int k = 0; k < PER; ++k)
-            if (at + k * groups < rows && run[k].begin < 0)
+    for (int k = 0; k < PER; ++k)
+        if (at + k * groups < rows && run[k].begin < 0)
 #pragma unroll
-                for (int v = 0; v < UU; ++v) if (col + v * step < end) store_vector(grad + (at + k * groups) * grad_stride + col + v * step, none);
+            for (int u = 0; u < U; ++u) if (cols.at[u] >= 0) store_vector(grad + (at + k * groups) * grad_stride + cols.at[u], none);
 #pragma unroll 1
-        for (int k = 0; k < PER; ++k) {
-            if (at + k * groups >= rows) break;
-            const TokenRun r = runs[at + k * groups];
-            if (r.begin >= 0)
-                token_row<false, UU, NN>(q.scale, grad + (at + k * groups) * grad_stride, col, end, step,
-                                         [&](float (&acc)[UU][NN]) {
-                                             add_run(acc, q, grad_out, stride, [&](int i) { return q.vals[i]; }, r.begin, r.end, col, end, step);
-                                         });
-        }
-    });
+    for (int k = 0; k < PER; ++k) {
+        if (at + k * groups >= rows) break;
+        const TokenRun r = runs[at + k * groups];
+        if (r.begin >= 0)
+            token_row<false, U, N>(q.scale, grad + (at + k * groups) * grad_stride, cols, [&](float (&acc)[U][N]) {
+                add_run(acc, q, grad_out, stride, [&](int i) { return q.vals[i]; }, r.begin, r.end, cols);
+            });
+    }
 }
 
 // Rows with tokens, stored or (ADD) added to what the gradient holds: a row-group takes the runs that begin at its PER positions.
-template <bool ADD, int PER, int U, class S, class G>
+template <bool ADD, int PER, int U, int N, class S, class G>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_runs(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys, int n,
                                                             int rows, const uint64_t* __restrict__ heads, const int32_t* __restrict__ ends,
                                                             G* __restrict__ grad, int64_t grad_stride) {
     static_assert(TOK_BLOCK % PER == 0 && PER < 64, "positions of one block");
-    const Tile tile = my_tile(q.tiles);
-    const int64_t at = (((int64_t)tile.block * TOK_THREADS + threadIdx.x) >> q.lpr_shift) * PER;
+    const Tile tile = my_tile(q.t);
+    const Cols<U> cols = my_cols<U, N>(q.t, tile.tile);
+    const int64_t at = (((int64_t)tile.block * TOK_THREADS + threadIdx.x) >> q.t.lpr_shift) * PER;
     if (at >= n) return;
     const int64_t c = at / TOK_BLOCK;
     const int bit = (int)(at % TOK_BLOCK);
     const uint64_t all = heads[c];
     const int last = ends[c];
     // the positions' keys and tokens, one to a lane: read for each run as it comes up, they cost it two loads one after the other
-    const int lpr = 1 << q.lpr_shift, lane = threadIdx.x & (lpr - 1);
+    const int lpr = 1 << q.t.lpr_shift, lane = threadIdx.x & (lpr - 1);
     const bool held = lpr >= PER;
     const int64_t i = min(at + min(lane, PER - 1), (int64_t)n - 1);
     const int my_key = held ? keys[i] : 0, my_token = held ? q.vals[i] : 0;
-    token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto w, int col, int end, int step) {
-        constexpr int UU = decltype(u)::value, NN = decltype(w)::value;
-        for (uint64_t mine = all >> bit & (((uint64_t)1 << PER) - 1); mine; mine &= mine - 1) {
-            const int j = bit + __builtin_ctzll(mine);
-            const uint64_t later = j < 63 ? all >> (j + 1) : 0;
-            const int a = (int)(c * TOK_BLOCK) + j, b = later ? a + 1 + __builtin_ctzll(later) : last;
-            const int key = held ? __shfl(my_key, a - (int)at, lpr) : keys[a];
-            if (key >= rows) break;
-            token_row<ADD, UU, NN>(q.scale, grad + (size_t)key * grad_stride, col, end, step,
-                                   [&](float (&acc)[UU][NN]) {
-                                       add_run(acc, q, grad_out, stride, [&](int i) {
-                                           const int k = i - (int)at;
-                                           const int t = __shfl(my_token, k & (PER - 1), lpr);
-                                           return held && k < PER ? t : q.vals[i];
-                                       }, a, b, col, end, step);
-                                   });
-        }
-    });
+    for (uint64_t mine = all >> bit & (((uint64_t)1 << PER) - 1); mine; mine &= mine - 1) {
+        const int j = bit + __builtin_ctzll(mine);
+        const uint64_t later = j < 63 ? all >> (j + 1) : 0;
+        const int a = (int)(c * TOK_BLOCK) + j, b = later ? a + 1 + __builtin_ctzll(later) : last;
+        const int key = held ? __shfl(my_key, a - (int)at, lpr) : keys[a];
+        if (key >= rows) break;
+        token_row<ADD, U, N>(q.scale, grad + (size_t)key * grad_stride, cols, [&](float (&acc)[U][N]) {
+            add_run(acc, q, grad_out, stride, [&](int i) {
+                const int k = i - (int)at;
+                const int t = __shfl(my_token, k & (PER - 1), lpr);
+                return held && k < PER ? t : q.vals[i];
+            }, a, b, cols);
+        });
+    }
 }
 
 // Few tokens: no sort.  Every workgroup reads all ids and lists, in order, the tokens whose rows are its own: with `per_block` neighbouring rows
 // to a workgroup, which also writes the zeros among them, or without (0: the gradient accumulates, or holds zeros already) as a hash of the id says.
-// A row-group then goes through the list's tokens that are the first of their row, puts the row's tokens together in LDS and adds them up.
-constexpr int TOK_FEW = 1024, TOK_FEW_ROWS = 1024;
-template <bool ADD, int U, class S, class G, class I>
+// A row-group then goes through the list's tokens that are the first of their row, puts the row's tokens together in LDS and adds them up; the rows
+// of TOK_HEAVY tokens or more are left to all row-groups together.
+constexpr int TOK_FEW = 1024, TOK_FEW_ROWS = 1024, TOK_HEAVY = 32;
+template <bool ADD, int U, int N, class S, class G, class I>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const I* __restrict__ ids, int n, int rows,
                                                            int64_t padding_id, int per_block, unsigned blocks, G* __restrict__ grad, int64_t grad_stride,
                                                            uint32_t* flags) {
     constexpr int PER = TOK_FEW / TOK_THREADS, WAVES = TOK_THREADS / 64;
     __shared__ int list_key[TOK_FEW], list_pos[TOK_FEW], order[TOK_FEW], counts[PER * WAVES];
     __shared__ uint32_t used[TOK_FEW_ROWS / 32];
-    const int lpr = 1 << q.lpr_shift, lane = threadIdx.x & (lpr - 1), groups = TOK_THREADS >> q.lpr_shift, g = threadIdx.x >> q.lpr_shift;
+    __shared__ int heavy_row[TOK_FEW / TOK_HEAVY], heavy_from[TOK_FEW / TOK_HEAVY], heavy_count[TOK_FEW / TOK_HEAVY], heavies;
+    __shared__ float sums[U * N][TOK_THREADS];
+    const int lpr = 1 << q.t.lpr_shift, lane = threadIdx.x & (lpr - 1), groups = TOK_THREADS >> q.t.lpr_shift, g = threadIdx.x >> q.t.lpr_shift;
     const int w = threadIdx.x >> 6, wl = threadIdx.x & 63;
-    const Tile tile = my_tile(q.tiles);
+    const Tile tile = my_tile(q.t);
+    const Cols<U> cols = my_cols<U, N>(q.t, tile.tile);
     const int64_t row0 = (int64_t)tile.block * per_block;
     bool bad = false;
     I id[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) id[k] = ids[min(k * TOK_THREADS + (int)threadIdx.x, n - 1)];
     if (threadIdx.x < TOK_FEW_ROWS / 32) used[threadIdx.x] = 0;
+    if (threadIdx.x == 0) heavies = 0;
     int key[PER];
     uint64_t mask[PER];
 #pragma unroll
@@ -418,17 +406,15 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
     __syncthreads();
     if (per_block) {
         const int here = (int)min((int64_t)per_block, rows - row0);
+        const float none[N] = {};
         for (int r = g; r < here; r += groups) {
             if (used[r / 32] >> r % 32 & 1) continue;
-            token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto v, int col, int end, int step) {
-                const float none[decltype(v)::value] = {};
 #pragma unroll
-                for (int k = 0; k < decltype(u)::value; ++k) if (col + k * step < end) store_vector(grad + (row0 + r) * grad_stride + col + k * step, none);
-            });
+            for (int u = 0; u < U; ++u) if (cols.at[u] >= 0) store_vector(grad + (row0 + r) * grad_stride + cols.at[u], none);
         }
     }
     // a lane looks at `per` neighbouring tokens of the list (an odd number, so that lanes are in different banks)
-    const int per = ((m + lpr - 1) >> q.lpr_shift) | 1, e0 = min(m, lane * per), e1 = min(m, e0 + per);
+    const int per = ((m + lpr - 1) >> q.t.lpr_shift) | 1, e0 = min(m, lane * per), e1 = min(m, e0 + per);
     for (int j0 = 0; j0 < m; j0 += groups) {
         const int j = min(j0 + g, m - 1), mine = list_key[j];
         int less = 0, equal = 0, earlier = 0;
@@ -456,12 +442,37 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
         }
         __syncthreads();
         if (!owner) continue;
-        token_tile<U, VECTOR<G>>(q.dim, q.lpr_shift, tile, [&](auto u, auto v, int col, int end, int step) {
-            constexpr int UU = decltype(u)::value, NN = decltype(v)::value;
-            token_row<ADD, UU, NN>(q.scale, grad + (size_t)mine * grad_stride, col, end, step, [&](float (&acc)[UU][NN]) {
-                add_rows<(UU > 1 ? 4 : 8)>(acc, grad_out, stride, [&](int i) { return order[i]; }, less, less + equal, col, end, step);
-            });
+        if (equal >= TOK_HEAVY && groups > 1) {
+            if (lane == 0) {
+                const int k = atomicAdd(&heavies, 1);
+                heavy_row[k] = mine; heavy_from[k] = less; heavy_count[k] = equal;
+            }
+            continue;
+        }
+        token_row<ADD, U, N>(q.scale, grad + (size_t)mine * grad_stride, cols, [&](float (&acc)[U][N]) {
+            add_rows<(U > 1 ? 4 : 8)>(acc, grad_out, stride, [&](int i) { return order[i]; }, less, less + equal, cols);
         });
+    }
+    __syncthreads();
+    for (int k = 0; k < heavies; ++k) {
+        const int from = heavy_from[k], end = from + heavy_count[k], share = (heavy_count[k] + groups - 1) >> (8 - q.t.lpr_shift);
+        static_assert(TOK_THREADS == 256, "groups = 256 / lanes of a row");
+        float acc[U][N] = {};
+        add_rows<(U > 1 ? 4 : 8)>(acc, grad_out, stride, [&](int i) { return order[i]; }, min(end, from + g * share), min(end, from + (g + 1) * share), cols);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e) sums[u * N + e][threadIdx.x] = acc[u][e];
+        __syncthreads();
+        if (g == 0)
+            token_row<ADD, U, N>(q.scale, grad + (size_t)heavy_row[k] * grad_stride, cols, [&](float (&total)[U][N]) {
+                for (int j = 0; j < groups; ++j)
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) total[u][e] += sums[u * N + e][(j << q.t.lpr_shift) + lane];
+            });
+        __syncthreads();
     }
 }
 
@@ -470,9 +481,9 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
 template <class G>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_zero(G* __restrict__ grad, int64_t stride, int64_t rows, int64_t dim, int lpr_shift, int tiles) {
     constexpr int N = VECTOR<G>;
-    const Tile t = my_tile(tiles);
-    const int64_t row = ((int64_t)t.block * TOK_THREADS + threadIdx.x) >> lpr_shift;
-    const int64_t col = (((int64_t)t.tile << lpr_shift) + (threadIdx.x & ((1 << lpr_shift) - 1))) * N;
+    const unsigned block = blockIdx.x / (unsigned)tiles, tile = blockIdx.x - block * (unsigned)tiles;
+    const int64_t row = ((int64_t)block * TOK_THREADS + threadIdx.x) >> lpr_shift;
+    const int64_t col = (((int64_t)tile << lpr_shift) + (threadIdx.x & ((1 << lpr_shift) - 1))) * N;
     if (row >= rows || col >= dim) return;
     const float none[N] = {};
     store_from_float(grad + row * stride + col, none, (int)min((int64_t)N, dim - col));
@@ -502,19 +513,19 @@ static TokenWork token_work(int64_t n, int64_t rows, int64_t dim) {
 }
 size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim) { return token_work(n, rows, dim).bytes; }
 
-// log2 of the lanes of a row whose vectors have `per_lane` columns; enough of them for the columns left over to have a lane each
-static int shift_for(int dim, int per_lane, int most = 64) {
-    const int sh = __builtin_ctz(pow2_from(dim / per_lane, most));
-    return dim % per_lane && 1 << sh < per_lane ? __builtin_ctz(per_lane) : sh;
-}
-// workgroups beside one another on a row, at `columns` of its whole vectors each
-static int tiles_of(int dim, int per_lane, int64_t columns) { return (int)std::max<int64_t>(1, cdiv(dim / per_lane * per_lane, columns)); }
-
-// f(vectors that a lane takes of a row, as an integral constant); wider rows go to several workgroups
+// f(vectors that a lane takes of a row, columns of a vector) as integral constants; wider rows go to several workgroups
 template <int N, class F>
-static void by_vectors(int dim, int lpr_shift, F f) {
-    if (tiles_of(dim, N, (int64_t)N << lpr_shift) <= 1) f(std::integral_constant<int, 1>());
-    else f(std::integral_constant<int, 2>());
+static void by_width(int dim, F f) {
+    using One = std::integral_constant<int, 1>;
+    if (dim < N) f(One(), One());
+    else if (dim <= 64 * N) f(One(), std::integral_constant<int, N>());
+    else f(std::integral_constant<int, 2>(), std::integral_constant<int, N>());
+}
+// the same for kernels whose lanes take one vector
+template <int N, class F>
+static void by_vector(int dim, F f) {
+    if (dim < N) f(std::integral_constant<int, 1>());
+    else f(std::integral_constant<int, N>());
 }
 
 template <class S, class G>
@@ -539,36 +550,35 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
     float* miles = n >= TOK_MILES_FROM ? reinterpret_cast<float*>(d->work + w.miles) : nullptr;
     uint64_t* heads = reinterpret_cast<uint64_t*>(d->work + w.heads);
     int32_t* ends = reinterpret_cast<int32_t*>(d->work + w.ends);
-    {
-        const int sh = shift_for(dim, VECTOR<S>), threads = std::max(256, TOK_CHUNK << sh);
-        const int tiles = tiles_of(dim, VECTOR<S>, (int64_t)VECTOR<S> << sh);
-        k_token_chunks<<<(unsigned)(cdiv(cdiv(n, TOK_CHUNK), threads >> sh) * tiles), threads, (size_t)threads * VECTOR<S> * 4, st>>>(
-            grad_out, stride, ks, vs, (int)n, (int)rows, dim, sh, tiles, part, far, runs, heads, ends);
-    }
-    if (miles) {
-        const int sh = shift_for(dim, 4), tiles = tiles_of(dim, 4, (int64_t)4 << sh);
-        k_token_miles<<<(unsigned)(cdiv((n / TOK_MILE) << sh, TOK_THREADS) * tiles), TOK_THREADS, 0, st>>>(ks, (int)n, (int)rows, dim, sh, tiles, far, miles);
-    }
-    constexpr int N = VECTOR<G>;
-    TokenRows q{vs, part, far, miles, dim, shift_for(dim, N), 1, scale};
-    auto rows_of = [&](auto u) {
-        constexpr int U = decltype(u)::value;
-        q.tiles = tiles_of(dim, N, (int64_t)N * U << q.lpr_shift);
+    by_vector<VECTOR<S>>(dim, [&](auto v) {
+        constexpr int N = decltype(v)::value;
+        const Tiles t = tiles_of(dim, N, 1);
+        const int threads = std::max(256, TOK_CHUNK << t.lpr_shift);
+        k_token_chunks<N><<<(unsigned)(cdiv(cdiv(n, TOK_CHUNK), threads >> t.lpr_shift) * t.tiles), threads, (size_t)threads * N * 4, st>>>(
+            t, grad_out, stride, ks, vs, (int)n, (int)rows, part, far, runs, heads, ends);
+    });
+    if (miles) by_vector<4>(dim, [&](auto v) {
+        constexpr int N = decltype(v)::value;
+        const Tiles t = tiles_of(dim, N, 1);
+        k_token_miles<N><<<(unsigned)(cdiv((n / TOK_MILE) << t.lpr_shift, TOK_THREADS) * t.tiles), TOK_THREADS, 0, st>>>(t, ks, (int)n, (int)rows, far, miles);
+    });
+    by_width<VECTOR<G>>(dim, [&](auto u, auto v) {
+        constexpr int U = decltype(u)::value, N = decltype(v)::value;
+        const TokenRows q{tiles_of(dim, N, U), vs, part, far, miles, scale};
         auto by_runs = [&](auto a) {
             constexpr bool ADD = decltype(a)::value;
             constexpr int PER = 8;                        // us a call, 2 / 4 / 8: 426 k tokens of 128 columns added to 1 M rows 113 / 107 / 105
-            k_token_runs<ADD, PER, U><<<(unsigned)(cdiv(cdiv(n, PER) << q.lpr_shift, TOK_THREADS) * q.tiles), TOK_THREADS, 0, st>>>(
+            k_token_runs<ADD, PER, U, N><<<(unsigned)(cdiv(cdiv(n, PER) << q.t.lpr_shift, TOK_THREADS) * q.t.tiles), TOK_THREADS, 0, st>>>(
                 q, grad_out, stride, ks, (int)n, (int)rows, heads, ends, grad, grad_stride);
         };
         if (add) by_runs(std::true_type());
         else if (!runs) by_runs(std::false_type());
         else {
             constexpr int PER = 4;
-            k_token_rows<PER, U><<<(unsigned)(cdiv(cdiv(rows, PER) << q.lpr_shift, TOK_THREADS) * q.tiles), TOK_THREADS, 0, st>>>(q, grad_out, stride, runs, (int)rows, grad,
-                                                                                                                                 grad_stride);
+            k_token_rows<PER, U, N><<<(unsigned)(cdiv(cdiv(rows, PER) << q.t.lpr_shift, TOK_THREADS) * q.t.tiles), TOK_THREADS, 0, st>>>(q, grad_out, stride, runs, (int)rows, grad,
+                                                                                                                                        grad_stride);
         }
-    };
-    by_vectors<N>(dim, q.lpr_shift, rows_of);
+    });
     FC_HIP(hipGetLastError());
     return FC_OK;
 }
@@ -576,21 +586,19 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
 template <class S, class G, class I>
 static int token_bwd_few(fc_dense* d, const S* grad_out, int64_t stride, const I* ids, int64_t n, int64_t rows, int dim, float scale, int64_t padding_id,
                          G* grad, int64_t grad_stride, bool add, bool zeros) {
-    constexpr int N = VECTOR<G>;
-    TokenRows q{nullptr, nullptr, nullptr, nullptr, dim, shift_for(dim, N), 1, scale};
-    by_vectors<N>(dim, q.lpr_shift, [&](auto u) {
-        constexpr int U = decltype(u)::value;
-        q.tiles = tiles_of(dim, N, (int64_t)N * U << q.lpr_shift);
-        const int groups = TOK_THREADS >> q.lpr_shift;
+    by_width<VECTOR<G>>(dim, [&](auto u, auto v) {
+        constexpr int U = decltype(u)::value, N = decltype(v)::value;
+        const TokenRows q{tiles_of(dim, N, U), nullptr, nullptr, nullptr, nullptr, scale};
+        const int groups = TOK_THREADS >> q.t.lpr_shift;
         int per_block = 0;
         int64_t blocks = cdiv(n, 16);                 // lists of some 16 tokens
         if (zeros) {
-            per_block = groups * (int)std::max<int64_t>(1, std::min<int64_t>(TOK_FEW_ROWS / groups, rows * q.tiles / (groups * 4096)));
+            per_block = groups * (int)std::max<int64_t>(1, std::min<int64_t>(TOK_FEW_ROWS / groups, rows * q.t.tiles / (groups * 4096)));
             blocks = cdiv(rows, per_block);
         }
-        const unsigned grid = (unsigned)(blocks * q.tiles);
-        if (add) k_token_few<true, U><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, 0, (unsigned)blocks, grad, grad_stride, d->flags);
-        else k_token_few<false, U><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, per_block, (unsigned)blocks, grad, grad_stride, d->flags);
+        const unsigned grid = (unsigned)(blocks * q.t.tiles);
+        if (add) k_token_few<true, U, N><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, 0, (unsigned)blocks, grad, grad_stride, d->flags);
+        else k_token_few<false, U, N><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, per_block, (unsigned)blocks, grad, grad_stride, d->flags);
     });
     FC_HIP(hipGetLastError());
     return FC_OK;
@@ -625,11 +633,14 @@ int token_embed_fwd(fc_dense* d, const void* table_dev, int32_t table_type, int6
         return with_type(out_type, [&](auto o) -> int {
             using S = decltype(s);
             using D = decltype(o);
-            const int sh = shift_for(dim, VECTOR<S>, TOK_THREADS);
             auto run = [&](auto id) {
                 using I = decltype(id);
-                k_token_fwd<1><<<(unsigned)cdiv(n << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
-                    (const S*)table_dev, table_stride, (int)num_rows, dim, sh, (const I*)ids_dev, n, scale, (D*)out_dev, out_stride, d->flags);
+                by_vector<VECTOR<S>>(dim, [&](auto v) {
+                    constexpr int N = decltype(v)::value;
+                    const int sh = __builtin_ctz(pow2_from(cdiv(dim, N), TOK_THREADS));
+                    k_token_fwd<1, N><<<(unsigned)cdiv(n << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
+                        (const S*)table_dev, table_stride, (int)num_rows, dim, sh, (const I*)ids_dev, n, scale, (D*)out_dev, out_stride, d->flags);
+                });
             };
             if (id_type == FC_TYPE_I32) run(int32_t()); else run(int64_t());
             FC_HIP(hipGetLastError());
