@@ -46,7 +46,8 @@ __device__ __forceinline__ void store_vector(T* __restrict__ p, const float (&v)
     *reinterpret_cast<typename Pack<T, N>::V*>(p) = x;
 }
 
-// The same for the `live` first of N elements.
+// The same for the `live` first of N elements, one at least.  (The last one is read in the place of those beyond it, so that all loads are on their way
+// together: in branches of their own each is waited for.)
 template <int N, class T>
 __device__ __forceinline__ void load_as_float(float (&v)[N], const T* __restrict__ p, int live) {
     if (live >= N) {
@@ -55,7 +56,9 @@ __device__ __forceinline__ void load_as_float(float (&v)[N], const T* __restrict
         for (int k = 0; k < N; ++k) v[k] = (float)x[k];
     } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = k < live ? (float)p[k] : 0.f;
+        for (int k = 0; k < N; ++k) v[k] = (float)p[k < live ? k : live - 1];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = k < live ? v[k] : 0.f;
     }
 }
 template <int N, class T>

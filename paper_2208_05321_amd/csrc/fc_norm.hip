@@ -13,6 +13,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 namespace fc {
 
 struct F8 { uint8_t b; };                          // FC_TYPE_F8E4M3
@@ -23,21 +25,33 @@ template <> constexpr float QMAX<int8_t> = 127.f;
 // the larger one, or not a number if either is none
 __device__ __forceinline__ float nan_max(float a, float b) { return a > b || a != a ? a : b; }
 
-// lanes_of: lanes that hold one row; a workgroup has `threads` of them, 256 or one row's
+// threads of a workgroup: 256, or the TPR lanes of one row
 constexpr int norm_threads(int tpr) { return tpr < 256 ? 256 : tpr; }
 
-// Rows of whole vectors (WHOLE) need no code for partial ones, which is four fifths of a kernel that has it: 9 KB of instructions for 4096 16-bit
-// columns, fetched once a launch, and 4.1 us for a single row.
-template <bool WHOLE, int N, class T>
+// What a row's last vector is.  WHOLE: the width is a multiple of N.  OVER: the vector ends with the row and overlaps the one before; its lane leaves the
+// first `skip` elements out of every sum, and stores for them what the lane before stores.  That needs all of a row to be read before any of
+// it is written (results may take the place of inputs), and rows of a vector at least; otherwise PART: the vector is loaded and stored element by
+// element, in code that is four fifths of a kernel that has it (9 KB of instructions for 4096 16-bit columns, fetched once a launch: 4.1 us for a
+// single row, 3.1 without) and takes registers: backward pass, 7227 rows of 2249 columns 65 us, of 2248 29; 31 this way.
+enum NormEnd { WHOLE, OVER, PART };
+template <int END, int N, class T>
 __device__ __forceinline__ void load_some(float (&v)[N], const T* __restrict__ p, int live) {
-    if constexpr (WHOLE) load_vector(v, p);
+    if constexpr (END != PART) load_vector(v, p);
     else load_as_float(v, p, live);
 }
-template <bool WHOLE, int N, class T>
+template <int END, int N, class T>
 __device__ __forceinline__ void store_some(T* __restrict__ p, const float (&v)[N], int live) {
-    if constexpr (WHOLE) store_vector(p, v);
+    if constexpr (END != PART) store_vector(p, v);
     else store_from_float(p, v, live);
 }
+// The vector that begins at column `v`: is it there, where does it begin, how many of its elements belong to the one before.
+struct NormVector { bool in; int col, skip; };
+template <int END, int N>
+__device__ __forceinline__ NormVector norm_vector(int v, int dim) {
+    if constexpr (END == OVER) { const int col = min(v, dim - N); return NormVector{v < dim, col, v - col}; }
+    else return NormVector{v < dim, v, 0};
+}
+template <int END> __device__ __forceinline__ bool counts(const NormVector& q, int e) { return END != OVER || e >= q.skip; }
 
 // Sum of x over the TPR lanes of a row, in each of them.  lds: TPR / 64 words for each of the two turns that alternate, so that one barrier a
 // sum is enough.
@@ -55,6 +69,18 @@ __device__ __forceinline__ float row_sum(float x, float* lds) {
     }
 }
 template <int TPR>
+__device__ __forceinline__ void row_sums(float& x, float& y, float (*lds)[TPR > 64 ? TPR / 64 : 1]) {
+    if constexpr (TPR <= 64) { x = lanes_sum<TPR>(x); y = lanes_sum<TPR>(y); }
+    else {
+        x = wave_sum(x); y = wave_sum(y);
+        if ((threadIdx.x & 63) == 0) { lds[0][threadIdx.x >> 6] = x; lds[1][threadIdx.x >> 6] = y; }
+        __syncthreads();
+        x = y = 0.f;
+#pragma unroll
+        for (int k = 0; k < TPR / 64; ++k) { x += lds[0][k]; y += lds[1][k]; }
+    }
+}
+template <int TPR>
 __device__ __forceinline__ float row_max(float x, float* lds) {
 #pragma unroll
     for (int o = 1; o < (TPR < 64 ? TPR : 64); o <<= 1) x = nan_max(x, __shfl_xor(x, o));
@@ -68,14 +94,15 @@ __device__ __forceinline__ float row_max(float x, float* lds) {
     return x;
 }
 
-template <bool WHOLE, class T, int N>
+template <int END, class T, int N>
 __device__ __forceinline__ void load_weight(float (&v)[N], const void* w, bool f32, int col, int live) {
-    if (f32) load_some<WHOLE>(v, (const float*)w + col, live);
-    else load_some<WHOLE>(v, (const T*)w + col, live);
+    if (f32) load_some<END>(v, (const float*)w + col, live);
+    else load_some<END>(v, (const T*)w + col, live);
 }
 
-template <bool WHOLE, int N>
-__device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], float inv, int live) {
+// (elements skip .. live - 1)
+template <bool ALL, int N>
+__device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], float inv, int skip, int live) {
     uint32_t word[N / 4];
 #pragma unroll
     for (int k = 0; k < N; k += 4) {
@@ -88,7 +115,7 @@ __device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], floa
         int x = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
         word[k / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], x, true);
     }
-    if (WHOLE || live >= N) {
+    if (ALL || (skip == 0 && live >= N)) {
         typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
         V x;
 #pragma unroll
@@ -96,11 +123,11 @@ __device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], floa
         *reinterpret_cast<V*>(p) = x;
     } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) if (k < live) p[k].b = (uint8_t)(word[k / 4] >> (k % 4 * 8));
+        for (int k = 0; k < N; ++k) if (k >= skip && k < live) p[k].b = (uint8_t)(word[k / 4] >> (k % 4 * 8));
     }
 }
-template <bool WHOLE, int N>
-__device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], float inv, int live) {
+template <bool ALL, int N>
+__device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], float inv, int skip, int live) {
     typedef int8_t V __attribute__((ext_vector_type(N), aligned(1)));
     V x;
 #pragma unroll
@@ -108,10 +135,10 @@ __device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], 
         const float t = rintf(v[k] * inv);
         x[k] = (int8_t)(t > 127.f ? 127.f : t < -127.f ? -127.f : t == t ? t : 0.f);
     }
-    if (WHOLE || live >= N) *reinterpret_cast<V*>(p) = x;
+    if (ALL || (skip == 0 && live >= N)) *reinterpret_cast<V*>(p) = x;
     else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) if (k < live) p[k] = x[k];
+        for (int k = 0; k < N; ++k) if (k >= skip && k < live) p[k] = x[k];
     }
 }
 
@@ -124,11 +151,12 @@ struct NormFwd {
     float eps;
 };
 
-// KEEP: vectors of a row that a lane keeps in registers, 0: rows too wide for that, h is worked out again for each of the three steps
-template <int TPR, int KEEP, bool WHOLE, class T, class Q>
+// KEEP: vectors of a row that a lane keeps in registers, 0: rows too wide for that, h is worked out again for each of the steps (with END PART)
+template <int TPR, int KEEP, int END, class T, class Q>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     constexpr int N = VECTOR<T>, NT = norm_threads(TPR), K = KEEP ? KEEP : 1;
     constexpr bool QUANT = QMAX<Q> > 0.f;
+    static_assert(KEEP > 0 || END == PART, "lanes that share columns read them before they write");
     __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
     const int lane = threadIdx.x & (TPR - 1);
     const int64_t row = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
@@ -139,12 +167,13 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     Q* const y = (Q*)a.y + row * a.y_stride;
     const int vectors = KEEP ? KEEP : (a.dim + TPR * N - 1) / (TPR * N);
     float v[K][N];
+    auto vector = [&](int k) { return norm_vector<END, N>((k * TPR + lane) * N, a.dim); };
     auto fetch = [&](float (&t)[N], int col) {
         const int live = a.dim - col;
-        load_some<WHOLE>(t, x + col, live);
+        load_some<END>(t, x + col, live);
         if (r) {
             float s[N];
-            load_some<WHOLE>(s, r + col, live);
+            load_some<END>(s, r + col, live);
 #pragma unroll
             for (int e = 0; e < N; ++e) t[e] = (float)(T)(t[e] + s[e]);
         }
@@ -152,44 +181,43 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     float s = 0.f;
 #pragma unroll K
     for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
-        const int col = (k * TPR + lane) * N;
+        const NormVector q = vector(k);
         float (&t)[N] = v[KEEP ? k : 0];
-        if (col < a.dim) fetch(t, col);
+        if (q.in) fetch(t, q.col);
         else
 #pragma unroll
             for (int e = 0; e < N; ++e) t[e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) s = fmaf(t[e], t[e], s);
+        for (int e = 0; e < N; ++e) s = counts<END>(q, e) ? fmaf(t[e], t[e], s) : s;
     }
     const float rho = rsqrtf(row_sum<TPR>(s, lds[0]) / (float)a.dim + a.eps);
-    auto result = [&](float (&t)[N], int col) {                      // h -> y, and h stored on the way
-        const int live = a.dim - col;
+    auto result = [&](float (&t)[N], int col) {                      // h -> y
         float w[N];
-        load_weight<WHOLE, T>(w, a.weight, a.weight_f32, col, live);
+        load_weight<END, T>(w, a.weight, a.weight_f32, col, a.dim - col);
 #pragma unroll
         for (int e = 0; e < N; ++e) t[e] = t[e] * rho * w[e];
+    };
+    auto store_h = [&](int col) {                                    // KEEP 0: h once more, when it is read no more
+        if (KEEP || !h) return;
+        float t[N];
+        fetch(t, col);
+        store_some<END>(h + col, t, a.dim - col);
     };
     float most = 0.f;
 #pragma unroll K
     for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
-        const int col = (k * TPR + lane) * N;
+        const NormVector q = vector(k);
         float (&t)[N] = v[KEEP ? k : 0];
-        if (col < a.dim) {
-            if (!KEEP) fetch(t, col);
-            if (KEEP && h) store_some<WHOLE>(h + col, t, a.dim - col);
-            result(t, col);
-            if (!QUANT) {
-                if constexpr (!QUANT) {
-                    if (!KEEP && h) {
-                        float t0[N];
-                        fetch(t0, col);
-                        store_some<WHOLE>(h + col, t0, a.dim - col);
-                    }
-                    store_some<WHOLE>(y + col, t, a.dim - col);
-                }
+        if (q.in) {
+            if (!KEEP) fetch(t, q.col);
+            if (KEEP && h) store_some<END>(h + q.col, t, a.dim - q.col);
+            result(t, q.col);
+            if constexpr (!QUANT) {
+                store_h(q.col);
+                store_some<END>(y + q.col, t, a.dim - q.col);
             } else
 #pragma unroll
-                for (int e = 0; e < N; ++e) most = nan_max(fabsf(t[e]), most);
+                for (int e = 0; e < N; ++e) most = counts<END>(q, e) ? nan_max(fabsf(t[e]), most) : most;
         }
         if constexpr (QUANT) {
             if (a.group) {                                           // neighbouring lanes hold a group's columns
@@ -197,15 +225,12 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
                 const int lanes = min(a.group / N, TPR < 64 ? TPR : 64);
                 for (int o = 1; o < lanes; o <<= 1) m = nan_max(m, __shfl_xor(m, o));
                 most = 0.f;
-                if (col < a.dim) {
+                if (q.in) {
                     const float scale = m * (1.f / QMAX<Q>);
-                    if (col % a.group == 0) a.scales[row * ((a.dim + a.group - 1) / a.group) + col / a.group] = scale;
-                    if (!KEEP && h) {
-                        float t0[N];
-                        fetch(t0, col);
-                        store_some<WHOLE>(h + col, t0, a.dim - col);
-                    }
-                    store_quantised<WHOLE>(y + col, t, scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f, a.dim - col);
+                    const int at = q.col + q.skip;
+                    if (at % a.group == 0) a.scales[row * ((a.dim + a.group - 1) / a.group) + at / a.group] = scale;
+                    store_h(q.col);
+                    store_quantised<END == WHOLE>(y + q.col, t, scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f, q.skip, a.dim - q.col);
                 }
             }
         }
@@ -217,20 +242,12 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
         if (lane == 0) a.scales[row] = scale;
 #pragma unroll K
         for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
-            const int col = (k * TPR + lane) * N;
+            const NormVector q = vector(k);
             float (&t)[N] = v[KEEP ? k : 0];
-            if (col >= a.dim) continue;
-            if (!KEEP) {
-                fetch(t, col);
-                if (h) {
-                    float t0[N];
-#pragma unroll
-                    for (int e = 0; e < N; ++e) t0[e] = t[e];
-                    result(t, col);
-                    store_some<WHOLE>(h + col, t0, a.dim - col);
-                } else result(t, col);
-            }
-            store_quantised<WHOLE>(y + col, t, inv, a.dim - col);
+            if (!q.in) continue;
+            if (!KEEP) { fetch(t, q.col); result(t, q.col); }
+            store_h(q.col);
+            store_quantised<END != PART>(y + q.col, t, inv, 0, a.dim - q.col);
         }
     }
 }
@@ -245,22 +262,24 @@ struct NormBwd {
 };
 
 // KEEP as above; with 0 a workgroup adds to its row of `part` in memory
-template <int TPR, int KEEP, bool WHOLE, class T>
+template <int TPR, int KEEP, int END, class T>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
     constexpr int N = VECTOR<T>, NT = norm_threads(TPR), GROUPS = NT / TPR, K = KEEP ? KEEP : 1;
+    static_assert(KEEP > 0 || END == PART, "lanes that share columns read them before they write");
     __shared__ float lds[4][TPR > 64 ? TPR / 64 : 1];
     __shared__ float cols[GROUPS > 1 ? GROUPS * TPR * K * N : 1];
     const int lane = threadIdx.x & (TPR - 1);
     const int vectors = KEEP ? KEEP : (a.dim + TPR * N - 1) / (TPR * N);
     float* const part = a.part + (size_t)blockIdx.x * a.dim;
+    auto vector = [&](int k) { return norm_vector<END, N>((k * TPR + lane) * N, a.dim); };
     float w[K][N], dw[K][N];
     if (KEEP) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int col = (k * TPR + lane) * N;
-            if (col < a.dim) load_weight<WHOLE, T>(w[k], a.weight, a.weight_f32, col, a.dim - col);
+            const NormVector q = vector(k);
+            if (q.in) load_weight<END, T>(w[k], a.weight, a.weight_f32, q.col, a.dim - q.col);
 #pragma unroll
-            for (int e = 0; e < N; ++e) { if (col >= a.dim) w[k][e] = 0.f; dw[k][e] = 0.f; }
+            for (int e = 0; e < N; ++e) { if (!q.in) w[k][e] = 0.f; dw[k][e] = 0.f; }
         }
     } else
         for (int col = threadIdx.x; col < a.dim; col += NT) part[col] = 0.f;
@@ -273,61 +292,62 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
         const T* const in = a.dh_in ? (const T*)a.dh_in + row * a.dh_in_stride : nullptr;
         T* const dx = (T*)a.dx + row * a.dx_stride;
         float g[K][N], x[K][N];
+        typename Pack<T, N>::V more[K];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll K
         for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
-            const int col = (k * TPR + lane) * N, b = KEEP ? k : 0;
-            if (col < a.dim) {
-                load_some<WHOLE>(g[b], dy + col, a.dim - col);
-                load_some<WHOLE>(x[b], h + col, a.dim - col);
-                if (!KEEP) load_weight<WHOLE, T>(w[0], a.weight, a.weight_f32, col, a.dim - col);
+            const NormVector q = vector(k);
+            const int b = KEEP ? k : 0;
+            if (q.in) {
+                load_some<END>(g[b], dy + q.col, a.dim - q.col);
+                load_some<END>(x[b], h + q.col, a.dim - q.col);
+                if (END == OVER && in) more[b] = *reinterpret_cast<const typename Pack<T, N>::V*>(in + q.col);
+                if (!KEEP) load_weight<END, T>(w[0], a.weight, a.weight_f32, q.col, a.dim - q.col);
             } else
 #pragma unroll
                 for (int e = 0; e < N; ++e) g[b][e] = x[b][e] = 0.f;
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                s1 = fmaf(g[b][e] * w[b][e], x[b][e], s1);
-                s2 = fmaf(x[b][e], x[b][e], s2);
+                s1 = counts<END>(q, e) ? fmaf(g[b][e] * w[b][e], x[b][e], s1) : s1;
+                s2 = counts<END>(q, e) ? fmaf(x[b][e], x[b][e], s2) : s2;
             }
         }
-        s1 = row_sum<TPR>(s1, lds[turn]);
-        s2 = row_sum<TPR>(s2, lds[turn + 1]);
+        row_sums<TPR>(s1, s2, lds + turn);
         const float rho = rsqrtf(s2 / (float)a.dim + a.eps), m = rho * rho * (s1 / (float)a.dim);
 #pragma unroll K
         for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
-            const int col = (k * TPR + lane) * N, b = KEEP ? k : 0;
-            if (col >= a.dim) continue;
-            const int live = a.dim - col;
+            const NormVector q = vector(k);
+            const int b = KEEP ? k : 0, live = a.dim - q.col;
+            if (!q.in) continue;
             if (!KEEP) {
-                load_some<WHOLE>(g[0], dy + col, live);
-                load_some<WHOLE>(x[0], h + col, live);
-                load_weight<WHOLE, T>(w[0], a.weight, a.weight_f32, col, live);
-                load_some<WHOLE>(dw[0], part + col, live);
+                load_some<END>(g[0], dy + q.col, live);
+                load_some<END>(x[0], h + q.col, live);
+                load_weight<END, T>(w[0], a.weight, a.weight_f32, q.col, live);
+                load_some<END>(dw[0], part + q.col, live);
             }
             float o[N];
-            if (in) load_some<WHOLE>(o, in + col, live);
+            if (END != OVER && in) load_some<END>(o, in + q.col, live);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 dw[b][e] = fmaf(g[b][e], x[b][e] * rho, dw[b][e]);
                 const float t = rho * (g[b][e] * w[b][e] - x[b][e] * m);
-                o[e] = in ? o[e] + t : t;
+                o[e] = in ? (END == OVER ? (float)more[b][e] : o[e]) + t : t;
             }
-            store_some<WHOLE>(dx + col, o, live);
-            if (!KEEP) store_some<WHOLE>(part + col, dw[0], live);
+            store_some<END>(dx + q.col, o, live);
+            if (!KEEP) store_some<END>(part + q.col, dw[0], live);
         }
     }
+    // (columns that two lanes have: both have added the same numbers up, in the same order)
     if constexpr (KEEP > 0) {
-        if constexpr (GROUPS == 1) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int col = (k * TPR + lane) * N;
-                if (col < a.dim) store_some<WHOLE>(part + col, dw[k], a.dim - col);
-            }
-        } else {
+        for (int k = 0; k < K; ++k) {
+            const NormVector q = vector(k);
+            if constexpr (GROUPS == 1) { if (q.in) store_some<END>(part + q.col, dw[k], a.dim - q.col); }
+            else if (q.in)
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int e = 0; e < N; ++e) cols[threadIdx.x / TPR * (TPR * K * N) + (k * TPR + lane) * N + e] = dw[k][e];
+                for (int e = 0; e < N; ++e) cols[threadIdx.x / TPR * (TPR * K * N) + q.col + e] = dw[k][e];
+        }
+        if constexpr (GROUPS > 1) {
             __syncthreads();
             for (int col = threadIdx.x; col < a.dim; col += NT) {
                 float s = 0.f;
@@ -362,58 +382,55 @@ __global__ __launch_bounds__(DW_COLS * DW_PARTS) void k_norm_dw(const float* __r
 constexpr int NORM_BWD_BLOCKS = 1024;
 size_t norm_work_bytes(int64_t dim) { return (size_t)NORM_BWD_BLOCKS * dim * 4; }
 
-// f(shape): lanes of a row, vectors a lane keeps, whether rows are whole vectors.  Up to a wavefront a row's lanes are as many as its vectors.
+// f(shape): lanes of a row, vectors a lane keeps, what its last vector is.  Up to a wavefront a row's lanes are as many as its vectors.
 // Wider rows: a vector to a lane where there are few of them (`few`), which then wait for nothing but one round of loads; else more of them to a
-// lane, and fewer lanes.  Rows that end in a partial vector have six shapes.
-template <int TPR_, int KEEP_, bool WHOLE_> struct NormShape { static constexpr int TPR = TPR_, KEEP = KEEP_; static constexpr bool WHOLE = WHOLE_; };
-template <class F>
-static void norm_shape(int64_t vectors, bool whole, bool few, F f) {
-    if (!whole) {
-        if (vectors <= 16) f(NormShape<16, 1, false>());
-        else if (vectors <= 64) f(NormShape<64, 1, false>());
-        else if (vectors <= 256) f(NormShape<256, 1, false>());
-        else if (vectors <= 1024) f(NormShape<256, 4, false>());
-        else if (vectors <= 4096) f(NormShape<1024, 4, false>());
-        else f(NormShape<1024, 0, false>());
-        return;
-    }
-    if (vectors <= 8) f(NormShape<8, 1, true>());
-    else if (vectors <= 16) f(NormShape<16, 1, true>());
-    else if (vectors <= 32) f(NormShape<32, 1, true>());
-    else if (vectors <= 64) f(NormShape<64, 1, true>());
-    else if (vectors <= 128 && !few) f(NormShape<64, 2, true>());
-    else if (vectors <= 256) f(NormShape<256, 1, true>());
-    else if (vectors <= 512 && few) f(NormShape<512, 1, true>());
-    else if (vectors <= 1024 && few) f(NormShape<1024, 1, true>());
-    else if (vectors <= 512) f(NormShape<256, 2, true>());
-    else if (vectors <= 1024) f(NormShape<256, 4, true>());
-    else if (vectors <= 4096) f(NormShape<1024, 4, true>());
-    else f(NormShape<1024, 0, true>());
-}
+// lane, and fewer lanes.
+template <int TPR_, int KEEP_, int END_> struct NormShape { static constexpr int TPR = TPR_, KEEP = KEEP_, END = END_; };
 constexpr int64_t NORM_FEW = 512;                  // rows
+template <int N, class F>
+static void norm_shape(int dim, bool few, F f) {
+    const int64_t vectors = cdiv(dim, N);
+    auto kept = [&](auto end) {
+        constexpr int E = decltype(end)::value;
+        if (vectors <= 8) f(NormShape<8, 1, E>());
+        else if (vectors <= 16) f(NormShape<16, 1, E>());
+        else if (vectors <= 32) f(NormShape<32, 1, E>());
+        else if (vectors <= 64) f(NormShape<64, 1, E>());
+        else if (vectors <= 128 && !few) f(NormShape<64, 2, E>());
+        else if (vectors <= 256) f(NormShape<256, 1, E>());
+        else if (vectors <= 512 && few) f(NormShape<512, 1, E>());
+        else if (vectors <= 1024 && few) f(NormShape<1024, 1, E>());
+        else if (vectors <= 512) f(NormShape<256, 2, E>());
+        else if (vectors <= 1024) f(NormShape<256, 4, E>());
+        else f(NormShape<1024, 4, E>());
+    };
+    if (dim < N) f(NormShape<8, 1, PART>());
+    else if (vectors > 4096) f(NormShape<1024, 0, PART>());
+    else if (dim % N) kept(std::integral_constant<int, OVER>());
+    else kept(std::integral_constant<int, WHOLE>());
+}
 
-// The backward pass keeps two rows, the weights and the weights' gradient: half as many vectors a lane (four: 202 registers, and with 1024 threads
+// The backward pass keeps three rows, the weights and the weights' gradient: half as many vectors a lane (four: 202 registers, and with 1024 threads
 // they spill).
-template <class F>
-static void norm_bwd_shape(int64_t vectors, bool whole, F f) {
-    if (!whole) {
-        if (vectors <= 16) f(NormShape<16, 1, false>());
-        else if (vectors <= 64) f(NormShape<64, 1, false>());
-        else if (vectors <= 256) f(NormShape<256, 1, false>());
-        else if (vectors <= 1024) f(NormShape<512, 2, false>());
-        else f(NormShape<1024, 0, false>());
-        return;
-    }
-    if (vectors <= 8) f(NormShape<8, 1, true>());
-    else if (vectors <= 16) f(NormShape<16, 1, true>());
-    else if (vectors <= 32) f(NormShape<32, 1, true>());
-    else if (vectors <= 64) f(NormShape<64, 1, true>());
-    else if (vectors <= 128) f(NormShape<64, 2, true>());
-    else if (vectors <= 256) f(NormShape<256, 1, true>());
-    else if (vectors <= 512) f(NormShape<256, 2, true>());
-    else if (vectors <= 1024) f(NormShape<512, 2, true>());
-    else if (vectors <= 2048) f(NormShape<1024, 2, true>());
-    else f(NormShape<1024, 0, true>());
+template <int N, class F>
+static void norm_bwd_shape(int dim, F f) {
+    const int64_t vectors = cdiv(dim, N);
+    auto kept = [&](auto end) {
+        constexpr int E = decltype(end)::value;
+        if (vectors <= 8) f(NormShape<8, 1, E>());
+        else if (vectors <= 16) f(NormShape<16, 1, E>());
+        else if (vectors <= 32) f(NormShape<32, 1, E>());
+        else if (vectors <= 64) f(NormShape<64, 1, E>());
+        else if (vectors <= 128) f(NormShape<64, 2, E>());
+        else if (vectors <= 256) f(NormShape<256, 1, E>());
+        else if (vectors <= 512) f(NormShape<256, 2, E>());
+        else if (vectors <= 1024) f(NormShape<512, 2, E>());
+        else f(NormShape<1024, 2, E>());
+    };
+    if (dim < N) f(NormShape<8, 1, PART>());
+    else if (vectors > 2048) f(NormShape<1024, 0, PART>());
+    else if (dim % N) kept(std::integral_constant<int, OVER>());
+    else kept(std::integral_constant<int, WHOLE>());
 }
 
 }  // namespace fc
@@ -437,13 +454,13 @@ int rms_norm_fwd(fc_dense* d, const void* x_dev, int32_t type, int64_t x_stride,
                     weight_type == FC_TYPE_F32, group, eps};
     return with_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        norm_shape(cdiv(dim, VECTOR<T>), dim % VECTOR<T> == 0, n < NORM_FEW, [&](auto s) {
+        norm_shape<VECTOR<T>>(dim, n < NORM_FEW, [&](auto s) {
             using S = decltype(s);
             constexpr int NT = norm_threads(S::TPR);
             const unsigned blocks = (unsigned)cdiv(n, NT / S::TPR);
-            if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, S::WHOLE, T, F8><<<blocks, NT, 0, d->stream>>>(a);
-            else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, S::WHOLE, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
-            else k_norm_fwd<S::TPR, S::KEEP, S::WHOLE, T, T><<<blocks, NT, 0, d->stream>>>(a);
+            if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, S::END, T, F8><<<blocks, NT, 0, d->stream>>>(a);
+            else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, S::END, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
+            else k_norm_fwd<S::TPR, S::KEEP, S::END, T, T><<<blocks, NT, 0, d->stream>>>(a);
         });
         FC_HIP(hipGetLastError());
         return FC_OK;
@@ -465,11 +482,11 @@ int rms_norm_bwd(fc_dense* d, const void* grad_y_dev, int64_t grad_y_stride, con
     int64_t blocks = 0;
     const int rc = with_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        if (n > 0) norm_bwd_shape(cdiv(dim, VECTOR<T>), dim % VECTOR<T> == 0, [&](auto s) {
+        if (n > 0) norm_bwd_shape<VECTOR<T>>(dim, [&](auto s) {
             using S = decltype(s);
             constexpr int NT = norm_threads(S::TPR);
             blocks = std::min<int64_t>(cdiv(n, NT / S::TPR), NORM_BWD_BLOCKS);
-            k_norm_bwd<S::TPR, S::KEEP, S::WHOLE, T><<<(unsigned)blocks, NT, 0, d->stream>>>(a);
+            k_norm_bwd<S::TPR, S::KEEP, S::END, T><<<(unsigned)blocks, NT, 0, d->stream>>>(a);
         });
         FC_HIP(hipGetLastError());
         return FC_OK;

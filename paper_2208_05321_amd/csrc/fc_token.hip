@@ -114,6 +114,10 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_keys(const I* __restrict_
     if (bad) atomicOr(flags, EF_ID_RANGE);
 }
 
+// Rows that a lane has on their way together: 32 sums' worth.  More of them, or two vectors of eight columns to a lane, cost wavefronts.
+// us a call, 8 rows and two vectors / 4 and one: 37 k tokens added to 137 k rows of 2048 16-bit columns 114 / 101, 426 k to 1 M of 128 107.5 / 97.
+template <int U, int N> constexpr int token_loads = 32 / (U * N) < 8 ? 32 / (U * N) : 8;
+
 // acc += the rows at(a) .. at(b - 1) of src, in order.  AT rows' loads are on their way together; the last ones that do not make AT go in halves
 // of it, with the last row read again in the place of rows beyond it, and not counted.
 template <int AT, int U, int N, class S, class F>
@@ -269,7 +273,7 @@ __device__ __forceinline__ void token_row(float scale, G* __restrict__ out, cons
 // Sorted tokens a .. b - 1, with the chunks, stretches and miles among them already summed.  token(i): the i-th sorted token.
 template <int U, int N, class S, class F>
 __device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, const S* __restrict__ grad_out, int64_t stride, F token, int a, int b, const Cols<U>& c) {
-    constexpr int AT = U > 1 ? 4 : 8;             // loads of a lane on their way together: more cost wavefronts
+    constexpr int AT = token_loads<U, N>;
     int c0 = (a + TOK_CHUNK - 1) / TOK_CHUNK, c1 = b / TOK_CHUNK;
     const bool parts = c0 < c1;
     for (int k = 0; k < (parts ? 2 : 1); ++k)     // before the first chunk, after the last
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
             continue;
         }
         token_row<ADD, U, N>(q.scale, grad + (size_t)mine * grad_stride, cols, [&](float (&acc)[U][N]) {
-            add_rows<(U > 1 ? 4 : 8)>(acc, grad_out, stride, [&](int i) { return order[i]; }, less, less + equal, cols);
+            add_rows<token_loads<U, N>>(acc, grad_out, stride, [&](int i) { return order[i]; }, less, less + equal, cols);
         });
     }
     __syncthreads();
@@ -458,7 +462,7 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
         const int from = heavy_from[k], end = from + heavy_count[k], share = (heavy_count[k] + groups - 1) >> (8 - q.t.lpr_shift);
         static_assert(TOK_THREADS == 256, "groups = 256 / lanes of a row");
         float acc[U][N] = {};
-        add_rows<(U > 1 ? 4 : 8)>(acc, grad_out, stride, [&](int i) { return order[i]; }, min(end, from + g * share), min(end, from + (g + 1) * share), cols);
+        add_rows<token_loads<U, N>>(acc, grad_out, stride, [&](int i) { return order[i]; }, min(end, from + g * share), min(end, from + (g + 1) * share), cols);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -518,7 +522,7 @@ template <int N, class F>
 static void by_width(int dim, F f) {
     using One = std::integral_constant<int, 1>;
     if (dim < N) f(One(), One());
-    else if (dim <= 64 * N) f(One(), std::integral_constant<int, N>());
+    else if (dim <= 64 * N || N > 4) f(One(), std::integral_constant<int, N>());
     else f(std::integral_constant<int, 2>(), std::integral_constant<int, N>());
 }
 // the same for kernels whose lanes take one vector
@@ -637,9 +641,17 @@ int token_embed_fwd(fc_dense* d, const void* table_dev, int32_t table_type, int6
                 using I = decltype(id);
                 by_vector<VECTOR<S>>(dim, [&](auto v) {
                     constexpr int N = decltype(v)::value;
-                    const int sh = __builtin_ctz(pow2_from(cdiv(dim, N), TOK_THREADS));
-                    k_token_fwd<1, N><<<(unsigned)cdiv(n << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
-                        (const S*)table_dev, table_stride, (int)num_rows, dim, sh, (const I*)ids_dev, n, scale, (D*)out_dev, out_stride, d->flags);
+                    // Lanes of a row: a wavefront, or a workgroup where rows are that wide, or few.  us a call, 256 lanes / 64: 85 k rows of 206 vectors
+                    // 113 / 95, 8 k of 512 18.1 / 20.7, 16 k of 1024 171 / 180.
+                    // Two narrow rows to a group where there are many: one / two, 426 k of 16 vectors 21.0 / 19.5, 1 M of 16 94 / 88, 65 k of 64 16.2 / 17.1.
+                    const int64_t nv = cdiv(dim, N);
+                    const int sh = __builtin_ctz(pow2_from(nv, nv >= 512 || n < 2048 ? TOK_THREADS : 64));
+                    auto go = [&](auto r) {
+                        constexpr int ROWS = decltype(r)::value;
+                        k_token_fwd<ROWS, N><<<(unsigned)cdiv(cdiv(n, ROWS) << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
+                            (const S*)table_dev, table_stride, (int)num_rows, dim, sh, (const I*)ids_dev, n, scale, (D*)out_dev, out_stride, d->flags);
+                    };
+                    if (nv <= 32 && n >= 1 << 17) go(std::integral_constant<int, 2>()); else go(std::integral_constant<int, 1>());
                 });
             };
             if (id_type == FC_TYPE_I32) run(int32_t()); else run(int64_t());

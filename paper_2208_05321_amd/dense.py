@@ -4,11 +4,13 @@ from __future__ import annotations
 
 import ctypes
 from array import array
+from operator import attrgetter
 
 from .binding import FreqCacheError, load_library
 
 _TYPE_NAMES = {"float32": 0, "bfloat16": 1, "float16": 2, "float8_e4m3fn": 3, "int8": 4, "int32": 5, "int64": 6}
 _FLOATS = (0, 1, 2)
+_dtype = attrgetter("dtype")
 
 
 def _refuse(what: str):
@@ -125,8 +127,9 @@ class DenseOps:
             self.stream.wait_stream(cur)
             rc = call(self._h, *args)
             for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+                for x in (t if isinstance(t, (list, tuple)) else (t,)):
+                    if x is not None:
+                        x.record_stream(self.stream)
             cur.wait_stream(self.stream)
         if rc != 0:
             raise FreqCacheError(rc, what)
@@ -255,13 +258,13 @@ class DenseOps:
     # ---- clipping ----
     def _tensors(self, tensors, what: str):
         """(addresses, sizes, types) of contiguous tensors, as lists."""
-        T = self._torch.Tensor
-        kinds = [self._type.get(t.dtype, -1) for t in tensors]
+        T = self._torch.Tensor                  # (one pass of C code for each question: a model has hundreds of tensors)
+        kinds = list(map(self._type.get, map(_dtype, tensors)))
         if not all(map(T.is_contiguous, tensors)):
             _refuse(f"{what}: tensors have to be contiguous")
-        if set(kinds) - {0, 1, 2} or set(map(T.get_device, tensors)) - {self._index}:
+        if not {0, 1, 2}.issuperset(kinds) or not {self._index}.issuperset(map(T.get_device, tensors)):
             _refuse(f"{what}: f32, bf16 or f16 on {self.device} is wanted")
-        return list(map(T.data_ptr, tensors)), list(map(T.numel, tensors)), kinds
+        return array("Q", map(T.data_ptr, tensors)), array("q", map(T.numel, tensors)), kinds
 
     def grad_norm_clip(self, grads, max_norm: float, out=None):
         """Global norm of the tensors (f32 [1]), which are scaled by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`."""
@@ -274,11 +277,10 @@ class DenseOps:
             dst, out_sizes, out_kinds = self._tensors(out, "out")
             if out_sizes != sizes or out_kinds != kinds:
                 _refuse("out: other sizes or types than grads")
-            dst = array("Q", dst)
         if not max_norm > 0:
             _refuse(f"max_norm {max_norm}")
-        src, sizes, kinds = array("Q", src), array("q", sizes), array("i", kinds)
+        kinds = array("i", kinds)
         norm = torch.empty(1, dtype=torch.float32, device=self.device)
-        self._run("grad_norm_clip", self._L.grad_norm_clip, (*grads, *(out or ()), norm), src.buffer_info()[0],
+        self._run("grad_norm_clip", self._L.grad_norm_clip, (grads, out or (), (norm,)), src.buffer_info()[0],
                   dst.buffer_info()[0] if dst is not None else None, sizes.buffer_info()[0], kinds.buffer_info()[0], len(grads), max_norm, norm.data_ptr())
         return norm
