@@ -291,32 +291,26 @@ __device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, 
     }
 }
 
-// Every row of the gradient; a row-group takes PER of them, whose runs it reads together, and a workgroup's groups neighbours at a time.
-template <int PER, int U, int N, class S, class G>
+// Every row of the gradient, a row-group each.  (Four rows to a group, their runs read together: 595 rows of 1024 columns, 137 k tokens 106 -> 139 us, 100 k
+// of 16, 65 k tokens 41 -> 47, 32,768 of 4096, 65 k tokens 343 -> 340.)
+template <int U, int N, class S, class G>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_rows(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const TokenRun* __restrict__ runs,
                                                             int rows, G* __restrict__ grad, int64_t grad_stride) {
     const Tile tile = my_tile(q.t);
     const Cols<U> cols = my_cols<U, N>(q.t, tile.tile);
-    const int groups = TOK_THREADS >> q.t.lpr_shift;
-    const int64_t at = (int64_t)tile.block * groups * PER + (threadIdx.x >> q.t.lpr_shift);
-    TokenRun run[PER];
+    const int64_t row = ((int64_t)tile.block * TOK_THREADS + threadIdx.x) >> q.t.lpr_shift;
+    if (row >= rows) return;
+    const TokenRun r = runs[row];
+    G* const out = grad + row * grad_stride;
+    if (r.begin < 0) {
+        const float none[N] = {};
 #pragma unroll
-    for (int k = 0; k < PER; ++k) run[k] = runs[min(at + k * groups, (int64_t)rows - 1)];
-    const float none[N] = {};
-#pragma unroll
-    for (int k = 0; k < PER; ++k)
-        if (at + k * groups < rows && run[k].begin < 0)
-#pragma unroll
-            for (int u = 0; u < U; ++u) if (cols.at[u] >= 0) store_vector(grad + (at + k * groups) * grad_stride + cols.at[u], none);
-#pragma unroll 1
-    for (int k = 0; k < PER; ++k) {
-        if (at + k * groups >= rows) break;
-        const TokenRun r = runs[at + k * groups];
-        if (r.begin >= 0)
-            token_row<false, U, N>(q.scale, grad + (at + k * groups) * grad_stride, cols, [&](float (&acc)[U][N]) {
-                add_run(acc, q, grad_out, stride, [&](int i) { return q.vals[i]; }, r.begin, r.end, cols);
-            });
+        for (int u = 0; u < U; ++u) if (cols.at[u] >= 0) store_vector(out + cols.at[u], none);
+        return;
     }
+    token_row<false, U, N>(q.scale, out, cols, [&](float (&acc)[U][N]) {
+        add_run(acc, q, grad_out, stride, [&](int i) { return q.vals[i]; }, r.begin, r.end, cols);
+    });
 }
 
 // Rows with tokens, stored or (ADD) added to what the gradient holds: a row-group takes the runs that begin at its PER positions.
@@ -577,11 +571,7 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
         };
         if (add) by_runs(std::true_type());
         else if (!runs) by_runs(std::false_type());
-        else {
-            constexpr int PER = 4;
-            k_token_rows<PER, U, N><<<(unsigned)(cdiv(cdiv(rows, PER) << q.t.lpr_shift, TOK_THREADS) * q.t.tiles), TOK_THREADS, 0, st>>>(q, grad_out, stride, runs, (int)rows, grad,
-                                                                                                                                        grad_stride);
-        }
+        else k_token_rows<U, N><<<(unsigned)(cdiv(rows << q.t.lpr_shift, TOK_THREADS) * q.t.tiles), TOK_THREADS, 0, st>>>(q, grad_out, stride, runs, (int)rows, grad, grad_stride);
     });
     FC_HIP(hipGetLastError());
     return FC_OK;
