@@ -21,7 +21,7 @@ namespace fc {
 constexpr int TOK_THREADS = 256;
 constexpr int TOK_CHUNK = 16;                     // sorted tokens to a chunk, chunks to a stretch, stretches to a mile
 constexpr int TOK_STRETCH = TOK_CHUNK * TOK_CHUNK, TOK_MILE = TOK_CHUNK * TOK_STRETCH;
-constexpr int64_t TOK_MILES_FROM = 8 * TOK_MILE;  // tokens from which on miles are added up: fewer cost a row less than the launch
+constexpr int64_t TOK_MILES_FROM = 16 * TOK_MILE;  // tokens from which on miles are added up: fewer cost a row less than the launch
 constexpr int TOK_BLOCK = 64;                     // sorted tokens whose run heads are one word
 
 // ---- columns ----
@@ -271,21 +271,24 @@ __device__ __forceinline__ void token_row(float scale, G* __restrict__ out, cons
 }
 
 // Sorted tokens a .. b - 1, with the chunks, stretches and miles among them already summed.  token(i): the i-th sorted token.
+// What lies before the first chunk and after the last is one list (two of up to 15 take a round of loads or two more), and so on upwards.
 template <int U, int N, class S, class F>
 __device__ __forceinline__ void add_run(float (&acc)[U][N], const TokenRows& q, const S* __restrict__ grad_out, int64_t stride, F token, int a, int b, const Cols<U>& c) {
     constexpr int AT = token_loads<U, N>;
     int c0 = (a + TOK_CHUNK - 1) / TOK_CHUNK, c1 = b / TOK_CHUNK;
     const bool parts = c0 < c1;
-    for (int k = 0; k < (parts ? 2 : 1); ++k)     // before the first chunk, after the last
-        add_rows<AT>(acc, grad_out, stride, token, k ? c1 * TOK_CHUNK : a, parts && !k ? c0 * TOK_CHUNK : b, c);
+    {
+        const int before = parts ? c0 * TOK_CHUNK - a : b - a, skip = parts ? (c1 - c0) * TOK_CHUNK : 0;
+        add_rows<AT>(acc, grad_out, stride, [=](int i) { return token(a + i + (i < before ? 0 : skip)); }, 0, b - a - skip, c);
+    }
     if (!parts) return;
     const float* src = q.part;
-    for (int level = 0; level < 3; ++level) {     // chunks before the first stretch and after the last; and so on
+    for (int level = 0; level < 3; ++level) {
         const float* const next = level == 0 ? q.far : level == 1 ? q.miles : nullptr;
         const int s0 = (c0 + TOK_CHUNK - 1) / TOK_CHUNK, s1 = c1 / TOK_CHUNK;
         const bool more = next && s0 < s1;
-        for (int k = 0; k < (more ? 2 : 1); ++k)
-            add_rows<AT>(acc, src, q.t.dim, [](int i) { return i; }, k ? s1 * TOK_CHUNK : c0, more && !k ? s0 * TOK_CHUNK : c1, c);
+        const int from = c0, before = more ? s0 * TOK_CHUNK - c0 : c1 - c0, skip = more ? (s1 - s0) * TOK_CHUNK : 0;
+        add_rows<AT>(acc, src, q.t.dim, [=](int i) { return from + i + (i < before ? 0 : skip); }, 0, c1 - c0 - skip, c);
         if (!more) return;
         src = next; c0 = s0; c1 = s1;
     }
