@@ -419,6 +419,7 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
     for (int j0 = 0; j0 < m; j0 += groups) {
         const int j = min(j0 + g, m - 1), mine = list_key[j];
         int less = 0, equal = 0, earlier = 0;
+#pragma unroll 8
         for (int e = e0; e < e1; ++e) {
             const int k = list_key[e];
             less += k < mine;
@@ -438,8 +439,11 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
         const bool owner = j0 + g < m && earlier == 0;
         if (owner && own) {
             rank += less - own;
-            for (int e = e0; e < e1; ++e)
-                if (list_key[e] == mine) order[rank++] = list_pos[e];
+            if (equal == 1) order[rank] = list_pos[j];
+            else
+#pragma unroll 8
+                for (int e = e0; e < e1; ++e)
+                    if (list_key[e] == mine) order[rank++] = list_pos[e];
         }
         __syncthreads();
         if (!owner) continue;
