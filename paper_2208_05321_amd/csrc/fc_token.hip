@@ -185,6 +185,20 @@ __device__ __forceinline__ void mark_runs(const int32_t* __restrict__ keys, int 
     }
 }
 
+// Zeros, one 16-byte store to a lane: of what was tried (1, 2, 4, 8 stores of a lane to a row, contiguous or not, 1 to 8 rows, workgroups that go
+// round) it fills memory fastest (1 GB: 151 us, 170 to 270 us the others).  Rows of `bytes` (contiguous ones are one row); 1 << shift lanes beside one another.
+struct Zeros { char* at; int64_t stride, rows, bytes; unsigned tiles; int shift; unsigned blocks; };
+__device__ __forceinline__ void zero_block(const Zeros& z, unsigned block) {
+    const unsigned group = block / z.tiles, tile = block - group * z.tiles;
+    const int64_t row = ((int64_t)group * blockDim.x + threadIdx.x) >> z.shift, from = (((int64_t)tile << z.shift) + (threadIdx.x & ((1 << z.shift) - 1))) * 16;
+    if (row >= z.rows || from >= z.bytes) return;
+    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+    char* const p = z.at + row * z.stride + from;
+    if (from + 16 <= z.bytes) { *reinterpret_cast<V*>(p) = V{0, 0, 0, 0}; return; }
+    for (int64_t k = 0; k < z.bytes - from; k += 2) *reinterpret_cast<uint16_t*>(p + k) = 0;
+}
+__global__ __launch_bounds__(TOK_THREADS) void k_token_zero(Zeros z) { zero_block(z, blockIdx.x); }
+
 // all of `count` sorted positions from i are there and have one row
 __device__ __forceinline__ bool one_row(const int32_t* __restrict__ keys, int n, int rows, int64_t i, int count) {
     if (i + count > n) return false;
@@ -193,12 +207,14 @@ __device__ __forceinline__ bool one_row(const int32_t* __restrict__ keys, int n,
 }
 
 // Chunks and stretches inside one run: a row-group to a chunk, 16 neighbouring ones to a stretch, whose sum they work out together; the
-// chunks of such a stretch are not asked for.  Threads: 16 row-groups, or 256.
+// chunks of such a stretch are not asked for.  Threads: 16 row-groups, or 256.  Workgroups from `blocks` on fill the gradient with zeros meanwhile.
 template <int N, class S>
 __global__ __launch_bounds__(1024) void k_token_chunks(Tiles q, const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys,
                                                        const int32_t* __restrict__ vals, int n, int rows, float* __restrict__ part, float* __restrict__ far,
-                                                       TokenRun* __restrict__ runs, uint64_t* __restrict__ heads, int32_t* __restrict__ ends) {
+                                                       TokenRun* __restrict__ runs, uint64_t* __restrict__ heads, int32_t* __restrict__ ends,
+                                                       unsigned blocks, Zeros z) {
     extern __shared__ float chunk_lds[];
+    if (blockIdx.x >= blocks) { zero_block(z, blockIdx.x - blocks); return; }
     const int groups = blockDim.x >> q.lpr_shift, lpr = 1 << q.lpr_shift;
     const Tile t = my_tile(q);
     const int64_t c = (int64_t)t.block * groups + (threadIdx.x >> q.lpr_shift);
@@ -481,19 +497,6 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
     }
 }
 
-// Zeros, one store to a lane: of what was tried (1, 2, 4, 8 stores of a lane to a row, contiguous or not, 1 to 8 rows, workgroups that go round) it
-// fills memory fastest (1 GB: 151 us, 170 to 270 us the others).
-template <class G>
-__global__ __launch_bounds__(TOK_THREADS) void k_token_zero(G* __restrict__ grad, int64_t stride, int64_t rows, int64_t dim, int lpr_shift, int tiles) {
-    constexpr int N = VECTOR<G>;
-    const unsigned block = blockIdx.x / (unsigned)tiles, tile = blockIdx.x - block * (unsigned)tiles;
-    const int64_t row = ((int64_t)block * TOK_THREADS + threadIdx.x) >> lpr_shift;
-    const int64_t col = (((int64_t)tile << lpr_shift) + (threadIdx.x & ((1 << lpr_shift) - 1))) * N;
-    if (row >= rows || col >= dim) return;
-    const float none[N] = {};
-    store_from_float(grad + row * stride + col, none, (int)min((int64_t)N, dim - col));
-}
-
 // A gradient is written row by row, each once, where most rows may be in use or where it fits the memory-side cache (256 MB, with what is read);
 // else zeros go everywhere first, at the rate at which memory can be filled, and the rows in use are written again.
 // us a call, row by row / zeros first (16-bit rows in, f32 out; rows, columns, tokens): 131,072 x 64, 1024 19 / 23; 131,072 x 256, 16 k 51 / 56;
@@ -517,6 +520,16 @@ static TokenWork token_work(int64_t n, int64_t rows, int64_t dim) {
     return w;
 }
 size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim) { return token_work(n, rows, dim).bytes; }
+
+constexpr int64_t ZEROS_BESIDE = (int64_t)512 << 20;           // bytes
+static Zeros zeros_of(void* at, int64_t stride, int64_t rows, int64_t dim, int element, int threads) {
+    Zeros z{(char*)at, stride * element, rows, dim * element, 1, 0, 0};
+    if (stride == dim) { z.bytes *= rows; z.rows = 1; }
+    z.shift = __builtin_ctz(pow2_from(cdiv(z.bytes, 16), threads));
+    z.tiles = (unsigned)cdiv(z.bytes, (int64_t)16 << z.shift);
+    z.blocks = (unsigned)cdiv(z.rows << z.shift, threads) * z.tiles;
+    return z;
+}
 
 // f(vectors that a lane takes of a row, columns of a vector) as integral constants; wider rows go to several workgroups
 template <int N, class F>
@@ -559,8 +572,16 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
         constexpr int N = decltype(v)::value;
         const Tiles t = tiles_of(dim, N, 1);
         const int threads = std::max(256, TOK_CHUNK << t.lpr_shift);
-        k_token_chunks<N><<<(unsigned)(cdiv(cdiv(n, TOK_CHUNK), threads >> t.lpr_shift) * t.tiles), threads, (size_t)threads * N * 4, st>>>(
-            t, grad_out, stride, ks, vs, (int)n, (int)rows, part, far, runs, heads, ends);
+        const unsigned blocks = (unsigned)(cdiv(cdiv(n, TOK_CHUNK), threads >> t.lpr_shift) * t.tiles);
+        // Zeros are filled in beside the chunks' sums, or, with workgroups of 1024 threads, which fill memory more slowly, by a launch of their own
+        // where they take long.  us a call, own launch / beside: 131,072 x 512 (f32), 16 k tokens 92 / 85, 1 M x 64, 65 k 91 / 84, 131,072 x 2048, 16 k 227 / 234.
+        Zeros z{.tiles = 1};
+        if (!add && !runs) {
+            const bool own = threads > 256 && rows * dim * (int64_t)sizeof(G) > ZEROS_BESIDE;
+            z = zeros_of(grad, grad_stride, rows, dim, sizeof(G), own ? TOK_THREADS : threads);
+            if (own) { k_token_zero<<<z.blocks, TOK_THREADS, 0, st>>>(z); z = Zeros{.tiles = 1}; }
+        }
+        k_token_chunks<N><<<blocks + z.blocks, threads, (size_t)threads * N * 4, st>>>(t, grad_out, stride, ks, vs, (int)n, (int)rows, part, far, runs, heads, ends, blocks, z);
     });
     if (miles) by_vector<4>(dim, [&](auto v) {
         constexpr int N = decltype(v)::value;
@@ -601,17 +622,6 @@ static int token_bwd_few(fc_dense* d, const S* grad_out, int64_t stride, const I
         if (add) k_token_few<true, U, N><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, 0, (unsigned)blocks, grad, grad_stride, d->flags);
         else k_token_few<false, U, N><<<grid, TOK_THREADS, 0, d->stream>>>(q, grad_out, stride, ids, (int)n, (int)rows, padding_id, per_block, (unsigned)blocks, grad, grad_stride, d->flags);
     });
-    FC_HIP(hipGetLastError());
-    return FC_OK;
-}
-
-template <class G>
-static int token_zero(fc_dense* d, G* grad, int64_t stride, int64_t rows, int64_t dim) {
-    constexpr int N = VECTOR<G>;
-    if (stride == dim) { dim *= rows; stride = dim; rows = 1; }
-    const int sh = __builtin_ctz(pow2_from(cdiv(dim, N), TOK_THREADS));
-    const int64_t tiles = cdiv(dim, (int64_t)N << sh);
-    k_token_zero<<<(unsigned)(cdiv(rows << sh, TOK_THREADS) * tiles), TOK_THREADS, 0, d->stream>>>(grad, stride, rows, dim, sh, (int)tiles);
     FC_HIP(hipGetLastError());
     return FC_OK;
 }
@@ -686,7 +696,11 @@ int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type
         using S = decltype(s);
         const S* grad_out = (const S*)grad_out_dev;
         auto go = [&](auto* grad) -> int {
-            if (!add && (!every_row || n == 0)) FC_TRY(token_zero(d, grad, grad_table_stride, num_rows, dim));
+            if (!add && (n == 0 || (n <= TOK_FEW && !every_row))) {
+                const Zeros z = zeros_of(grad, grad_table_stride, num_rows, dim, sizeof(*grad), TOK_THREADS);
+                k_token_zero<<<z.blocks, TOK_THREADS, 0, st>>>(z);
+                FC_HIP(hipGetLastError());
+            }
             if (n > TOK_FEW) return token_bwd(d, grad_out, grad_out_stride, keys, n, num_rows, dim, scale, w, runs, grad, grad_table_stride, add);
             if (n > 0 && id_type == FC_TYPE_I32)
                 return token_bwd_few(d, grad_out, grad_out_stride, (const int32_t*)ids_dev, n, num_rows, dim, scale, padding_id, grad, grad_table_stride, add, every_row);
