@@ -107,6 +107,8 @@ size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim);
 size_t norm_work_bytes(int64_t dim);
 size_t clip_work_bytes(int64_t tensors);
 
+// Threads of one launch: the runtime takes fewer than 2^32.  Rows that need more go in several.
+constexpr int64_t LAUNCH_THREADS = (int64_t)1 << 31;
 constexpr int64_t DENSE_LIMIT = ((int64_t)1 << 31) - 65536;    // tokens, rows
 constexpr int64_t DENSE_MAX_DIM = 1 << 20;
 

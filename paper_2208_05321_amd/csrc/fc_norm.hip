@@ -146,7 +146,7 @@ struct NormFwd {
     const void *x, *residual, *weight;
     void *h, *y;
     float* scales;
-    int64_t x_stride, residual_stride, h_stride, y_stride, n;
+    int64_t x_stride, residual_stride, h_stride, y_stride, first, n;      // rows first .. n - 1
     int dim, weight_f32, group;          // group: columns of a scale, 0 = the row
     float eps;
 };
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
     static_assert(KEEP > 0 || END == PART, "lanes that share columns read them before they write");
     __shared__ float lds[2][TPR > 64 ? TPR / 64 : 1];
     const int lane = threadIdx.x & (TPR - 1);
-    const int64_t row = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
+    const int64_t row = a.first + (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     if (TPR <= 64 && row >= a.n) return;          // (whole rows of lanes; a workgroup with one row always has it)
     const T* const x = (const T*)a.x + row * a.x_stride;
     const T* const r = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
@@ -450,17 +450,20 @@ int rms_norm_fwd(fc_dense* d, const void* x_dev, int32_t type, int64_t x_stride,
         return FC_ERR_INVALID_ARG;
     if (n == 0) return FC_OK;
     FC_HIP(hipSetDevice(d->device));
-    const NormFwd a{x_dev, residual_dev, weight_dev, h_dev, y_dev, scales_dev, x_stride, residual_stride, h_stride, y_stride, n, dim,
+    NormFwd a{x_dev, residual_dev, weight_dev, h_dev, y_dev, scales_dev, x_stride, residual_stride, h_stride, y_stride, 0, n, dim,
                     weight_type == FC_TYPE_F32, group, eps};
     return with_type(type, [&](auto t) -> int {
         using T = decltype(t);
         norm_shape<VECTOR<T>>(dim, n < NORM_FEW, [&](auto s) {
             using S = decltype(s);
             constexpr int NT = norm_threads(S::TPR);
-            const unsigned blocks = (unsigned)cdiv(n, NT / S::TPR);
-            if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, S::END, T, F8><<<blocks, NT, 0, d->stream>>>(a);
-            else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, S::END, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
-            else k_norm_fwd<S::TPR, S::KEEP, S::END, T, T><<<blocks, NT, 0, d->stream>>>(a);
+            constexpr int64_t MOST = LAUNCH_THREADS / S::TPR;             // (a multiple of a workgroup's rows)
+            for (; a.first < n; a.first += MOST) {
+                const unsigned blocks = (unsigned)cdiv(std::min(MOST, n - a.first), NT / S::TPR);
+                if (y_type == FC_TYPE_F8E4M3) k_norm_fwd<S::TPR, S::KEEP, S::END, T, F8><<<blocks, NT, 0, d->stream>>>(a);
+                else if (y_type == FC_TYPE_I8) k_norm_fwd<S::TPR, S::KEEP, S::END, T, int8_t><<<blocks, NT, 0, d->stream>>>(a);
+                else k_norm_fwd<S::TPR, S::KEEP, S::END, T, T><<<blocks, NT, 0, d->stream>>>(a);
+            }
         });
         FC_HIP(hipGetLastError());
         return FC_OK;

@@ -22,6 +22,7 @@ constexpr int TOK_THREADS = 256;
 constexpr int TOK_CHUNK = 16;                     // sorted tokens to a chunk, chunks to a stretch, stretches to a mile
 constexpr int TOK_STRETCH = TOK_CHUNK * TOK_CHUNK, TOK_MILE = TOK_CHUNK * TOK_STRETCH;
 constexpr int64_t TOK_MILES_FROM = 16 * TOK_MILE;  // tokens from which on miles are added up: fewer cost a row less than the launch
+constexpr int64_t TOK_MOST = (int64_t)1 << 36;    // tokens x columns of a gradient: the lanes of its runs fit a launch
 constexpr int TOK_BLOCK = 64;                     // sorted tokens whose run heads are one word
 
 // ---- columns ----
@@ -197,7 +198,11 @@ __device__ __forceinline__ void zero_block(const Zeros& z, unsigned block) {
     if (from + 16 <= z.bytes) { *reinterpret_cast<V*>(p) = V{0, 0, 0, 0}; return; }
     for (int64_t k = 0; k < z.bytes - from; k += 2) *reinterpret_cast<uint16_t*>(p + k) = 0;
 }
-__global__ __launch_bounds__(TOK_THREADS) void k_token_zero(Zeros z) { zero_block(z, blockIdx.x); }
+__global__ __launch_bounds__(TOK_THREADS) void k_token_zero(Zeros z, unsigned first) { zero_block(z, first + blockIdx.x); }
+static void fill_zeros(const Zeros& z, hipStream_t st) {         // (z for TOK_THREADS)
+    constexpr unsigned MOST = (unsigned)(LAUNCH_THREADS / TOK_THREADS);
+    for (unsigned at = 0; at < z.blocks; at += MOST) k_token_zero<<<std::min(MOST, z.blocks - at), TOK_THREADS, 0, st>>>(z, at);
+}
 
 // all of `count` sorted positions from i are there and have one row
 __device__ __forceinline__ bool one_row(const int32_t* __restrict__ keys, int n, int rows, int64_t i, int count) {
@@ -499,10 +504,17 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_few(TokenRows q, const S*
 
 // A gradient is written row by row, each once, where most rows may be in use or where it fits the memory-side cache (256 MB, with what is read);
 // else zeros go everywhere first, at the rate at which memory can be filled, and the rows in use are written again.
-// us a call, row by row / zeros first (16-bit rows in, f32 out; rows, columns, tokens): 131,072 x 64, 1024 19 / 23; 131,072 x 256, 16 k 51 / 56;
-// 131,072 x 384 (201 MB), 16 k 61 / 69; x 512 (268 MB) 105 / 90; x 2048, 16 k 313 / 240; 1 M x 64, 65 k 109 / 88; 131,072 x 1024, 131 k 285 / 269;
-// 32,768 x 4096, 65 k 340 / 373; 16,384 x 4096, 65 k 250 / 313; 1 M x 64, 1.7 M 265 / 278.
-static bool writes_every_row(int64_t n, int64_t rows, int64_t bytes) { return n >= rows || bytes < (int64_t)224 << 20; }
+// us a call, row by row / zeros first (16-bit rows in, f32 out; rows, columns, tokens): 131,072 x 64, 16 k 37 / 43; x 256 48 / 50; x 384 (201 MB) 60 / 65;
+// x 512 (268 MB) 100 / 85; x 2048 295 / 234; 1 M x 64, 65 k 106 / 84; 1 M x 64, 1.7 M 255 / 248; 131,072 x 1024, 100 k 247 / 219; 131 k 263 / 241;
+// 32,768 x 4096, 65 k 301 / 330; 16,384 x 4096, 65 k 225 / 272.  (Elements: the rows' lanes, at most two an element, fit a launch.)
+static bool writes_every_row(int64_t n, int64_t rows, int64_t dim, int64_t bytes) {
+    return (n >= 2 * rows && rows * dim < LAUNCH_THREADS) || bytes < (int64_t)224 << 20;
+}
+// Few tokens go without the sort: every row-group works out its part of the list by itself, which costs the more the wider a row is (lanes to a row-group).
+// us a call, sorted / not, ids of popularity 1.05, 1.2 (16-bit rows in, f32 out): gradient of 100 k x 16, 1000 tokens 23 / 10, 22 / 13, 2000 26 / 17, 26 / 28;
+// x 128, 1000 28 / 19, 28 / 28; 50 k x 512, 200 29 / 20, 31 / 22, 600 33 / 25, 34 / 35, 1000 34 / 31, 36 / 50; 8192 x 2048, 300 27 / 20, 28 / 24, 1000 30 / 35, 32 / 53;
+// added to 50 k x 512, 200 22 / 19, 23 / 19, 400 24 / 20, 23 / 30.
+static bool goes_unsorted(int64_t n, int dim) { return n <= TOK_FEW && n * std::min(dim, 512) <= TOK_FEW * 128; }
 
 struct TokenWork { size_t keys, runs, heads, ends, part, far, miles, bytes; };
 static TokenWork token_work(int64_t n, int64_t rows, int64_t dim) {
@@ -577,9 +589,11 @@ static int token_bwd(fc_dense* d, const S* grad_out, int64_t stride, const int32
         // where they take long.  us a call, own launch / beside: 131,072 x 512 (f32), 16 k tokens 92 / 85, 1 M x 64, 65 k 91 / 84, 131,072 x 2048, 16 k 227 / 234.
         Zeros z{.tiles = 1};
         if (!add && !runs) {
-            const bool own = threads > 256 && rows * dim * (int64_t)sizeof(G) > ZEROS_BESIDE;
-            z = zeros_of(grad, grad_stride, rows, dim, sizeof(G), own ? TOK_THREADS : threads);
-            if (own) { k_token_zero<<<z.blocks, TOK_THREADS, 0, st>>>(z); z = Zeros{.tiles = 1}; }
+            z = zeros_of(grad, grad_stride, rows, dim, sizeof(G), threads);
+            if ((threads > 256 && rows * dim * (int64_t)sizeof(G) > ZEROS_BESIDE) || ((int64_t)blocks + z.blocks) * threads > LAUNCH_THREADS) {
+                fill_zeros(zeros_of(grad, grad_stride, rows, dim, sizeof(G), TOK_THREADS), st);
+                z = Zeros{.tiles = 1};
+            }
         }
         k_token_chunks<N><<<blocks + z.blocks, threads, (size_t)threads * N * 4, st>>>(t, grad_out, stride, ks, vs, (int)n, (int)rows, part, far, runs, heads, ends, blocks, z);
     });
@@ -655,8 +669,12 @@ int token_embed_fwd(fc_dense* d, const void* table_dev, int32_t table_type, int6
                     const int sh = __builtin_ctz(pow2_from(nv, nv >= 512 || n < 2048 ? TOK_THREADS : 64));
                     auto go = [&](auto r) {
                         constexpr int ROWS = decltype(r)::value;
-                        k_token_fwd<ROWS, N><<<(unsigned)cdiv(cdiv(n, ROWS) << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
-                            (const S*)table_dev, table_stride, (int)num_rows, dim, sh, (const I*)ids_dev, n, scale, (D*)out_dev, out_stride, d->flags);
+                        for (int64_t at = 0, most = (LAUNCH_THREADS >> sh) * ROWS; at < n; at += most) {
+                            const int64_t part = std::min(most, n - at);
+                            k_token_fwd<ROWS, N><<<(unsigned)cdiv(cdiv(part, ROWS) << sh, TOK_THREADS), TOK_THREADS, 0, d->stream>>>(
+                                (const S*)table_dev, table_stride, (int)num_rows, dim, sh, (const I*)ids_dev + at, part, scale, (D*)out_dev + at * out_stride,
+                                out_stride, d->flags);
+                        }
                     };
                     if (nv <= 32 && n >= 1 << 17) go(std::integral_constant<int, 2>()); else go(std::integral_constant<int, 1>());
                 });
@@ -673,16 +691,16 @@ int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type
                     int64_t grad_table_stride, int32_t accumulate) {
     if (!d || n < 0 || n >= DENSE_LIMIT || num_rows <= 0 || num_rows >= DENSE_LIMIT || dim <= 0 || dim > DENSE_MAX_DIM || grad_out_stride < dim ||
         grad_table_stride < dim || !is_float_type(grad_out_type) || (grad_table_type != FC_TYPE_F32 && grad_table_type != grad_out_type) ||
-        (id_type != FC_TYPE_I32 && id_type != FC_TYPE_I64) || !grad_table_dev || (n > 0 && (!grad_out_dev || !ids_dev)))
+        n * dim >= TOK_MOST || (id_type != FC_TYPE_I32 && id_type != FC_TYPE_I64) || !grad_table_dev || (n > 0 && (!grad_out_dev || !ids_dev)))
         return FC_ERR_INVALID_ARG;
     if (n == 0 && accumulate) return FC_OK;
     FC_HIP(hipSetDevice(d->device));
     const hipStream_t st = d->stream;
-    const bool add = accumulate != 0, every_row = !add && writes_every_row(n, num_rows, num_rows * dim * type_bytes(grad_table_type));
+    const bool add = accumulate != 0, every_row = !add && writes_every_row(n, num_rows, dim, num_rows * dim * type_bytes(grad_table_type)), few = goes_unsorted(n, dim);
     const TokenWork w = token_work(n, every_row ? num_rows : 0, dim);
     int32_t* keys = nullptr;
     TokenRun* runs = nullptr;
-    if (n > TOK_FEW) {
+    if (!few) {
         FC_TRY(dense_sort(d, n));
         FC_TRY(dense_work(d, w.bytes));
         keys = reinterpret_cast<int32_t*>(d->work + w.keys);
@@ -696,12 +714,11 @@ int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type
         using S = decltype(s);
         const S* grad_out = (const S*)grad_out_dev;
         auto go = [&](auto* grad) -> int {
-            if (!add && (n == 0 || (n <= TOK_FEW && !every_row))) {
-                const Zeros z = zeros_of(grad, grad_table_stride, num_rows, dim, sizeof(*grad), TOK_THREADS);
-                k_token_zero<<<z.blocks, TOK_THREADS, 0, st>>>(z);
+            if (!add && (n == 0 || (few && !every_row))) {
+                fill_zeros(zeros_of(grad, grad_table_stride, num_rows, dim, sizeof(*grad), TOK_THREADS), st);
                 FC_HIP(hipGetLastError());
             }
-            if (n > TOK_FEW) return token_bwd(d, grad_out, grad_out_stride, keys, n, num_rows, dim, scale, w, runs, grad, grad_table_stride, add);
+            if (!few) return token_bwd(d, grad_out, grad_out_stride, keys, n, num_rows, dim, scale, w, runs, grad, grad_table_stride, add);
             if (n > 0 && id_type == FC_TYPE_I32)
                 return token_bwd_few(d, grad_out, grad_out_stride, (const int32_t*)ids_dev, n, num_rows, dim, scale, padding_id, grad, grad_table_stride, add, every_row);
             if (n > 0) return token_bwd_few(d, grad_out, grad_out_stride, (const int64_t*)ids_dev, n, num_rows, dim, scale, padding_id, grad, grad_table_stride, add, every_row);
