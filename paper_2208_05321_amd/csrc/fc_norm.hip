@@ -151,6 +151,7 @@ struct NormFwd {
     float eps;
 };
 
+// 8192 rows of 8192 bf16 columns with residual, to 8 bits by groups of 128: 98 to 101 us (472 MB, 4.7 TB/s); one row of 4096 3.1 us; 777 of 1111 f16 3.
 // KEEP: vectors of a row that a lane keeps in registers, 0: rows too wide for that, h is worked out again for each of the steps (with END PART)
 template <int TPR, int KEEP, int END, class T, class Q>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
@@ -261,6 +262,8 @@ struct NormBwd {
     float eps;
 };
 
+// The weight's gradient is summed over the workgroup's rows in registers and then over the workgroups by k_norm_dw: no atomics, the same order always.
+// 16,384 rows of 4096 bf16 columns 97 to 100 us (537 MB, 5.4 TB/s), and 6 for k_norm_dw.
 // KEEP as above; with 0 a workgroup adds to its row of `part` in memory
 template <int TPR, int KEEP, int END, class T>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
