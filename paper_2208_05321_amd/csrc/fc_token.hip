@@ -10,7 +10,7 @@
 // in a row (a stretch) and 16 stretches (a mile).  A row then adds at most 30 tokens, 30 chunks, 30 stretches and n / 4096 miles, whatever the
 // ids.  All sums are in 32 bits and in an order that depends on the ids alone: results are reproducible.
 // HBM bounds the large calls (the zeros of the dense gradient alone are 142 us of the 226 that one of 131,072 rows of 2048 columns takes with 16 k tokens),
-// the chain sort - chunks - rows the others: 426 k tokens of 128 columns added to 1 M rows 103 us, 32 of them the sort and 28 the chunks.
+// the chain sort - chunks - rows the others: 426 k tokens of 128 columns added to 1 M rows 98 us, 32 of them the sort and 28 the chunks.
 // (With chunks of 64 a popular row's 126 tokens, one after the other, were the kernel's duration: dense gradient of 131,072 rows of 2048
 // columns, 16,384 tokens, 330 us.)
 #include "dense_device.h"
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_rows(TokenRows q, const S
     });
 }
 
-// 47 k rows of 128 columns added to, 426 k tokens 38 to 39 us; 4.7 k rows of 2048 stored, 16 k tokens 34 to 36: bound by the longest chains of loads (token, row, then up to
+// 47 k rows of 128 columns added to, 426 k tokens 31 to 33 us; 4.7 k rows of 2048 stored, 16 k tokens 34 to 36: bound by the longest chains of loads (token, row, then up to
 // 30 of each level), which is why levels are sixteen apart and a group's tokens are in its lanes before it needs them.
 // Rows with tokens, stored or (ADD) added to what the gradient holds: a row-group takes the runs that begin at its PER positions.
 template <bool ADD, int PER, int U, int N, class S, class G>
@@ -363,7 +363,46 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_runs(TokenRows q, const S
     const bool held = lpr >= PER;
     const int64_t i = min(at + min(lane, PER - 1), (int64_t)n - 1);
     const int my_key = held ? keys[i] : 0, my_token = held ? q.vals[i] : 0;
-    for (uint64_t mine = all >> bit & (((uint64_t)1 << PER) - 1); mine; mine &= mine - 1) {
+    uint64_t mine = all >> bit & (((uint64_t)1 << PER) - 1);
+    // Rows with one token: up to four at a time.  us a call, one by one / so: 426 k tokens of 128 added to 1 M rows 104 / 98 (popularity 1.2), 120 / 111 (1.05),
+    // of 16 77 / 73, 37 k of 2048 118 / 114, 65 k of 64 59 / 55.  (Up to eight at a time: 103, 120, 72.5, 117, 55.)
+    if (mine) {
+        constexpr int SB = 16 / (U * N) < 2 ? 2 : 16 / (U * N) > 4 ? 4 : 16 / (U * N);
+        const int head = 63 - __builtin_clzll(all);
+        const uint64_t ones = (all & all >> 1) | (uint64_t)(last == (int)(c * TOK_BLOCK) + head + 1) << head;
+        uint64_t left = ones >> bit & mine;
+        mine &= ~left;
+        while (left) {
+            int key[SB], token[SB];
+#pragma unroll
+            for (int k = 0; k < SB; ++k) {
+                const int j = left ? __builtin_ctzll(left) : 0;
+                token[k] = held ? __shfl(my_token, j, lpr) : q.vals[min(at + j, (int64_t)n - 1)];
+                key[k] = held ? __shfl(my_key, j, lpr) : keys[min(at + j, (int64_t)n - 1)];
+                if (!left) key[k] = rows;
+                left &= left - 1;
+            }
+            float v[SB][U][N], old[SB][U][N];
+#pragma unroll
+            for (int k = 0; k < SB; ++k)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (key[k] < rows && cols.at[u] >= 0) {
+                        load_vector(v[k][u], grad_out + (size_t)token[k] * stride + cols.at[u]);
+                        if (ADD) load_vector(old[k][u], grad + (size_t)key[k] * grad_stride + cols.at[u]);
+                    }
+#pragma unroll
+            for (int k = 0; k < SB; ++k)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (key[k] < rows && cols.at[u] >= 0) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) v[k][u][e] = ADD ? fmaf(v[k][u][e], q.scale, old[k][u][e]) : v[k][u][e] * q.scale;
+                        store_vector(grad + (size_t)key[k] * grad_stride + cols.at[u], v[k][u]);
+                    }
+        }
+    }
+    for (; mine; mine &= mine - 1) {
         const int j = bit + __builtin_ctzll(mine);
         const uint64_t later = j < 63 ? all >> (j + 1) : 0;
         const int a = (int)(c * TOK_BLOCK) + j, b = later ? a + 1 + __builtin_ctzll(later) : last;
