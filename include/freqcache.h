@@ -366,7 +366,8 @@ int token_embed_fwd(fc_dense* d, const void* table_dev, int32_t table_type, int6
 /* Its gradient: grad_table[v, :] = scale * sum of grad_out[i, :] over the tokens i with ids[i] == v, for every row v of the table (zeros for one
  * without tokens); with accumulate != 0 that is added to grad_table, and rows without tokens are not touched.
  *   grad_out F32, BF16 or F16; grad_table F32 or grad_out's type; n * dim below 2^36.
- * Tokens with padding_id (-1: none) and, with the sticky error, ids outside the table contribute nothing. */
+ * Tokens with padding_id and, with the sticky error, ids outside the table contribute nothing.  A padding_id of -1 means that there is none: ids of -1
+ * are then outside, too.  Another padding_id may lie outside the table, without the error. */
 int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type, int64_t grad_out_stride, const void* ids_dev, int32_t id_type, int64_t n,
                     int64_t num_rows, int32_t dim, float scale, int64_t padding_id, void* grad_table_dev, int32_t grad_table_type,
                     int64_t grad_table_stride, int32_t accumulate);

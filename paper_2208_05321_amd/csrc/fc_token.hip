@@ -102,10 +102,11 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_fwd(const S* __restrict__
 // Where an id's tokens begin and end among the sorted ones; begin < 0: it has none.
 struct TokenRun { int begin, end; };
 
-// Sort keys: the id, or `rows` for the padding id and for ids outside.  runs: one per table row, without tokens to begin with.
+// Sort keys: the id, or `rows` for the padding id and for ids outside.  (-1 says that there is no padding id: as an id it is one outside, as in the
+// forward pass.)  runs: one per table row, without tokens to begin with.
 template <class I>
 __device__ __forceinline__ int token_key(I id, int rows, int64_t padding_id, bool& bad) {
-    const bool ok = id >= 0 && id < (I)rows, pad = (int64_t)id == padding_id;
+    const bool ok = id >= 0 && id < (I)rows, pad = padding_id != -1 && (int64_t)id == padding_id;
     bad |= !ok && !pad;
     return ok && !pad ? (int)id : rows;
 }
