@@ -348,8 +348,10 @@ typedef struct fc_dense fc_dense; /* opaque: stream, workspace, sticky error; on
 
 /* On the current device; hip_stream: hipStream_t (NULL = default stream) of all its calls. */
 int dense_create(void* hip_stream, fc_dense** out);
-/* Allocate now what calls up to these sizes need beyond the caller's memory (token_embed_bwd: max_tokens ids of a table of max_rows rows;
- * max_dim columns; grad_norm_clip: max_tensors tensors).  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
+/* Allocate now what calls up to these sizes need beyond the caller's memory: token_embed_bwd of max_tokens ids and a table of max_rows rows of max_dim
+ * columns, rms_norm_bwd of any number of rows of max_dim columns, grad_norm_clip of max_tensors tensors.  What token_embed_bwd needs grows with
+ * max_tokens * max_dim: a wide norm beside a narrow table is better reserved by a call of its own (max_tokens 0), as the workspace keeps the larger of
+ * the two.  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
  * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured into a graph; buffers that a captured call uses stay
  * until dense_destroy.  Synchronous.  Errors: INVALID_ARG, OOM_DEVICE, HIP. */
 int dense_reserve(fc_dense* d, int64_t max_tokens, int64_t max_rows, int32_t max_dim, int32_t max_tensors);

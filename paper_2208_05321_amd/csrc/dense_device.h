@@ -104,7 +104,7 @@ int dense_work(fc_dense* d, size_t bytes);     // d->work holds that many bytes
 int dense_sort(fc_dense* d, int64_t n);        // d->sort holds n pairs
 int dense_capturing(fc_dense* d, bool* now);   // whether the handle's stream is being captured
 size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim);
-size_t norm_work_bytes(int64_t dim);
+size_t norm_work_bytes(int64_t n, int64_t dim);
 size_t clip_work_bytes(int64_t tensors);
 
 // Threads of one launch: the runtime takes fewer than 2^32.  Rows that need more go in several.

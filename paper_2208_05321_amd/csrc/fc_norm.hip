@@ -383,7 +383,12 @@ __global__ __launch_bounds__(DW_COLS * DW_PARTS) void k_norm_dw(const float* __r
 }
 
 constexpr int NORM_BWD_BLOCKS = 1024;
-size_t norm_work_bytes(int64_t dim) { return (size_t)NORM_BWD_BLOCKS * dim * 4; }
+// Rows of sums: one a workgroup, of which there are no more than rows.  Up to 32 MB (8192 columns) there is room for all of them, so that the workspace does
+// not grow, and the call that grows it does not wait, each time a call has more rows than those before.
+size_t norm_work_bytes(int64_t n, int64_t dim) {
+    const size_t row = (size_t)dim * 4;
+    return std::max(std::min(NORM_BWD_BLOCKS * row, (size_t)32 << 20), (size_t)std::min<int64_t>(n, NORM_BWD_BLOCKS) * row);
+}
 
 // f(shape): lanes of a row, vectors a lane keeps, what its last vector is.  Up to a wavefront a row's lanes are as many as its vectors.
 // Wider rows: a vector to a lane where there are few of them (`few`), which then wait for nothing but one round of loads; else more of them to a
@@ -481,7 +486,7 @@ int rms_norm_bwd(fc_dense* d, const void* grad_y_dev, int64_t grad_y_stride, con
         grad_x_stride < dim || !weight_dev || !grad_weight_dev || (n > 0 && (!grad_y_dev || !h_dev || !grad_x_dev)))
         return FC_ERR_INVALID_ARG;
     FC_HIP(hipSetDevice(d->device));
-    FC_TRY(dense_work(d, norm_work_bytes(dim)));
+    FC_TRY(dense_work(d, norm_work_bytes(n, dim)));
     float* part = reinterpret_cast<float*>(d->work);
     const NormBwd a{grad_y_dev, h_dev, weight_dev, grad_h_dev, grad_x_dev, part, grad_y_stride, h_stride, grad_h_stride, grad_x_stride, n, dim,
                     weight_type == FC_TYPE_F32, eps};
