@@ -10,6 +10,7 @@ from .binding import FreqCacheError, load_library
 
 _TYPE_NAMES = {"float32": 0, "bfloat16": 1, "float16": 2, "float8_e4m3fn": 3, "int8": 4, "int32": 5, "int64": 6}
 _FLOATS = (0, 1, 2)
+_MOST_DIM = 1 << 20              # columns of a row (the C ABI takes 32 bits of their number)
 _dtype = attrgetter("dtype")
 
 
@@ -59,6 +60,8 @@ class DenseOps:
             pass
 
     def reserve(self, max_tokens: int = 0, max_rows: int = 0, max_dim: int = 0, max_tensors: int = 0):
+        if not 0 <= max_dim <= _MOST_DIM or not 0 <= max_tensors < 1 << 31:
+            _refuse(f"max_dim {max_dim}, max_tensors {max_tensors}")
         self._check(self._L.dense_reserve(self._h, int(max_tokens), int(max_rows), int(max_dim), int(max_tensors)), "dense_reserve")
 
     def check(self):
@@ -74,7 +77,7 @@ class DenseOps:
         if k is None:
             _refuse(f"{what}: type {t.dtype}")
         shape = t.shape
-        if not shape or shape[-1] == 0:
+        if not shape or not 0 < shape[-1] <= _MOST_DIM:
             _refuse(f"{what}: shape {tuple(shape)}")
         d = shape[-1]
         n = t.numel() // d
