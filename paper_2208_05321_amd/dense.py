@@ -11,6 +11,7 @@ from .binding import FreqCacheError, load_library
 _TYPE_NAMES = {"float32": 0, "bfloat16": 1, "float16": 2, "float8_e4m3fn": 3, "int8": 4, "int32": 5, "int64": 6}
 _FLOATS = (0, 1, 2)
 _MOST_DIM = 1 << 20              # columns of a row (the C ABI takes 32 bits of their number)
+_INF = float("inf")
 _dtype = attrgetter("dtype")
 
 
@@ -23,7 +24,11 @@ class DenseOps:
 
     The work runs on `stream` (the current stream of the constructor's call if not given).  A method called while another stream is current
     waits for that stream, and that stream waits for the method's work, so that tensors may come from, and go to, either.
-    Rows are the last dimension of a tensor; its elements have to be neighbours, rows may be any distance apart."""
+    Rows are the last dimension of a tensor; its elements have to be neighbours, rows may be any distance apart.
+
+    Autograd does not record these calls: results require no gradient, whatever the inputs do, and the gradients are calls of their own.  What a call
+    writes into a tensor of the caller's (`out`, `h_out`, `grad`, clipping in place) it does see: a tensor that was saved for a backward pass and then
+    written is an error there, as after torch's own in-place operations."""
 
     def __init__(self, stream=None):
         import torch
@@ -32,6 +37,7 @@ class DenseOps:
             raise FreqCacheError(-8, "no GPU visible; this library has no CPU path")
         self._L = load_library()
         self._torch = torch
+        self._written = torch.autograd.graph.increment_version
         self._type = {getattr(torch, name): k for name, k in _TYPE_NAMES.items()}
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.device = self.stream.device
@@ -151,7 +157,8 @@ class DenseOps:
             _refuse("table: [rows, dim] is wanted")
         tk, rows, d, ts = self._rows(table, "table")
         ik, n = self._ids(ids), ids.numel()
-        if out is None:
+        given = out is not None
+        if not given:
             out = torch.empty((*ids.shape, d), dtype=out_dtype or table.dtype, device=self.device)
             ok, os = self._type.get(out.dtype), d
         else:
@@ -162,6 +169,8 @@ class DenseOps:
             _refuse(f"types {table.dtype} -> {out.dtype}")
         self._run("token_embed_fwd", self._L.token_embed_fwd, (table, ids, out), table.data_ptr(), tk, ts, rows, d, ids.data_ptr(), ik, n, scale,
                   out.data_ptr(), ok, os)
+        if given:
+            self._written(out)
         return out
 
     def token_embed_bwd(self, grad_out, ids, num_rows: int, scale: float = 1.0, padding_id: int = -1, grad=None, grad_dtype=None,
@@ -173,7 +182,8 @@ class DenseOps:
         ik = self._ids(ids)
         if n != ids.numel() or gk not in _FLOATS:
             _refuse(f"grad_out {tuple(grad_out.shape)} {grad_out.dtype} for ids {tuple(ids.shape)}")
-        if grad is None:
+        given = grad is not None
+        if not given:
             if accumulate:
                 _refuse("accumulate needs grad")
             grad = torch.empty((num_rows, d), dtype=grad_dtype or torch.float32, device=self.device)
@@ -186,6 +196,8 @@ class DenseOps:
             _refuse(f"types {grad_out.dtype} -> {grad.dtype}")
         self._run("token_embed_bwd", self._L.token_embed_bwd, (grad_out, ids, grad), grad_out.data_ptr(), gk, gs, ids.data_ptr(), ik, n, num_rows, d,
                   scale, padding_id, grad.data_ptr(), tk, ts, 1 if accumulate else 0)
+        if given:
+            self._written(grad)
         return grad
 
     # ---- root-mean-square norm ----
@@ -232,6 +244,10 @@ class DenseOps:
             _refuse("group without a result in 8 bits")
         self._run("rms_norm_fwd", self._L.rms_norm_fwd, (x, weight, residual, h, y, scales), x.data_ptr(), k, xs, rp, rs, weight.data_ptr(), wk, n, d, eps,
                   hp, hs, y.data_ptr(), yk, ys, scales.data_ptr() if scales is not None else None, group)
+        if h_out is not None:
+            self._written(h_out)
+        if out is not None:
+            self._written(out)
         return y, h, scales
 
     def rms_norm_bwd(self, grad_y, h, weight, grad_h=None, eps: float = 1e-6, grad_weight_dtype=None, out=None):
@@ -262,6 +278,8 @@ class DenseOps:
             _refuse(f"grad_weight: type {dw.dtype}")
         self._run("rms_norm_bwd", self._L.rms_norm_bwd, (grad_y, h, weight, grad_h, dx, dw), grad_y.data_ptr(), ys, h.data_ptr(), k, hs, weight.data_ptr(),
                   wk, gp, gs, n, d, eps, dx.data_ptr(), ds, dw.data_ptr(), wt)
+        if out is not None:
+            self._written(out)
         return dx, dw
 
     # ---- clipping ----
@@ -292,4 +310,8 @@ class DenseOps:
         norm = torch.empty(1, dtype=torch.float32, device=self.device)
         self._run("grad_norm_clip", self._L.grad_norm_clip, (grads, out or (), (norm,)), src.buffer_info()[0],
                   dst.buffer_info()[0] if dst is not None else None, sizes.buffer_info()[0], kinds.buffer_info()[0], len(grads), max_norm, norm.data_ptr())
+        if out is not None:
+            self._written(out)
+        elif max_norm != _INF:
+            self._written(grads)
         return norm
