@@ -100,20 +100,30 @@ __device__ __forceinline__ void load_weight(float (&v)[N], const void* w, bool f
     else load_some<END>(v, (const T*)w + col, live);
 }
 
+// v / scale, rounded as a division is, in three instructions an element: the product with the rounded reciprocal, and what that leaves over, which is
+// exact (scales from 1e-28 on), times the reciprocal again (Markstein's correction).  The product alone is off by up to 1.5 units of 32 bits, and a quotient that close to the
+// middle between two 8-bit values then goes to the wrong one.  inv, by: 0 for a scale that is too small for a reciprocal or infinite.
+// Quotients are at most QMAX and one unit of 32 bits (|v| <= m and scale = m / QMAX, rounded), which rounds to QMAX: nothing is cut off.
+struct Quotient {
+    float inv, by;
+    __device__ __forceinline__ explicit Quotient(float scale) {
+        inv = scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f;
+        by = inv > 0.f ? scale : 0.f;
+    }
+    __device__ __forceinline__ float operator()(float v) const {
+        const float t = v * inv;
+        return fmaf(-fmaf(t, by, -v), inv, t);
+    }
+};
+
 // (elements skip .. live - 1)
 template <bool ALL, int N>
-__device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], float inv, int skip, int live) {
+__device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], const Quotient& of, int skip, int live) {
     uint32_t word[N / 4];
 #pragma unroll
     for (int k = 0; k < N; k += 4) {
-        float q[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float t = v[k + e] * inv;
-            q[e] = t > 448.f ? 448.f : t < -448.f ? -448.f : t;      // (beyond its range the conversion gives no number)
-        }
-        int x = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-        word[k / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], x, true);
+        int x = __builtin_amdgcn_cvt_pk_fp8_f32(of(v[k]), of(v[k + 1]), 0, false);
+        word[k / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(of(v[k + 2]), of(v[k + 3]), x, true);
     }
     if (ALL || (skip == 0 && live >= N)) {
         typedef uint32_t V __attribute__((ext_vector_type(N / 4), aligned(1)));
@@ -127,13 +137,13 @@ __device__ __forceinline__ void store_quantised(F8* p, const float (&v)[N], floa
     }
 }
 template <bool ALL, int N>
-__device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], float inv, int skip, int live) {
+__device__ __forceinline__ void store_quantised(int8_t* p, const float (&v)[N], const Quotient& of, int skip, int live) {
     typedef int8_t V __attribute__((ext_vector_type(N), aligned(1)));
     V x;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float t = rintf(v[k] * inv);
-        x[k] = (int8_t)(t > 127.f ? 127.f : t < -127.f ? -127.f : t == t ? t : 0.f);
+        const float t = rintf(of(v[k]));
+        x[k] = (int8_t)(int)(t == t ? t : 0.f);
     }
     if (ALL || (skip == 0 && live >= N)) *reinterpret_cast<V*>(p) = x;
     else {
@@ -227,19 +237,19 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
                 for (int o = 1; o < lanes; o <<= 1) m = nan_max(m, __shfl_xor(m, o));
                 most = 0.f;
                 if (q.in) {
-                    const float scale = m * (1.f / QMAX<Q>);
+                    const float scale = m / QMAX<Q>;
                     const int at = q.col + q.skip;
                     if (at % a.group == 0) a.scales[row * ((a.dim + a.group - 1) / a.group) + at / a.group] = scale;
                     store_h(q.col);
-                    store_quantised<END == WHOLE>(y + q.col, t, scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f, q.skip, a.dim - q.col);
+                    store_quantised<END == WHOLE>(y + q.col, t, Quotient(scale), q.skip, a.dim - q.col);
                 }
             }
         }
     }
     if constexpr (QUANT) {
         if (a.group) return;
-        const float scale = row_max<TPR>(most, lds[1]) * (1.f / QMAX<Q>);
-        const float inv = scale >= FLT_MIN || scale != scale ? 1.f / scale : 0.f;
+        const float scale = row_max<TPR>(most, lds[1]) / QMAX<Q>;
+        const Quotient of(scale);
         if (lane == 0) a.scales[row] = scale;
 #pragma unroll K
         for (int k = 0; k < (KEEP ? KEEP : vectors); ++k) {
@@ -248,7 +258,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
             if (!q.in) continue;
             if (!KEEP) { fetch(t, q.col); result(t, q.col); }
             store_h(q.col);
-            store_quantised<END != PART>(y + q.col, t, inv, 0, a.dim - q.col);
+            store_quantised<END != PART>(y + q.col, t, of, 0, a.dim - q.col);
         }
     }
 }
