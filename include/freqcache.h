@@ -353,7 +353,8 @@ int dense_create(void* hip_stream, fc_dense** out);
  * max_tokens * max_dim: a wide norm beside a narrow table is better reserved by a call of its own (max_tokens 0), as the workspace keeps the larger of
  * the two.  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
  * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured into a graph; buffers that a captured call uses stay
- * until dense_destroy.  Synchronous.  Errors: INVALID_ARG, OOM_DEVICE, HIP. */
+ * until dense_destroy, and its replays have to be in order with the handle's other work, which uses the same ones.  Synchronous.
+ * Errors: INVALID_ARG, OOM_DEVICE, HIP. */
 int dense_reserve(fc_dense* d, int64_t max_tokens, int64_t max_rows, int32_t max_dim, int32_t max_tensors);
 /* Wait for the handle's stream and return the sticky error, if any (then clears it): FC_ERR_ID_OUT_OF_RANGE. */
 int dense_check(fc_dense* d);
@@ -376,10 +377,12 @@ int token_embed_bwd(fc_dense* d, const void* grad_out_dev, int32_t grad_out_type
 
 /* Root-mean-square norm of each of n rows, with the residual's addition: h = x + residual (rounded to its type; residual may be NULL),
  * y = h * (mean(h^2) + eps)^-1/2 * weight.
- *   x, residual, h: `type` (F32, BF16, F16); weight: F32 or `type`; h may be NULL (not wanted) and may be x or residual itself.
+ *   x, residual, h: `type` (F32, BF16, F16); weight: F32 or `type`; h may be NULL (not wanted) and may be x or residual itself (same stride).
  *   y: `type`, or F8E4M3 / I8 with scales: y ~ q * scale, one scale for each `group` columns (32, 64, 128, 256; the last group may be
- *   narrower) or for the row (0): scales_dev fp32[n][ceil(dim / group)] = max |y| / (448 or 127) of the group, q rounded to nearest, ties to
- *   even.  Where that is below 1.18e-38 q = 0; where y holds infinities or no numbers the scale is one. */
+ *   narrower) or for the row (0): scales_dev fp32[n][ceil(dim / group)] = max |y| / (448 or 127) of the group, q = y / scale rounded to nearest, ties to
+ *   even; both quotients are in 32 bits, rounded once.  Where the scale is below 1.18e-38 q = 0.  Where y holds an infinity the scale is infinite, and where it
+ *   holds one that is no number the scale is none either; of such a group (row) I8 stores 0 throughout, F8E4M3 0 for finite y beside an infinity and no number
+ *   for all else: it is the scale that says so for both. */
 int rms_norm_fwd(fc_dense* d, const void* x_dev, int32_t type, int64_t x_stride, const void* residual_dev, int64_t residual_stride, const void* weight_dev,
                  int32_t weight_type, int64_t n, int32_t dim, float eps, void* h_dev, int64_t h_stride, void* y_dev, int32_t y_type, int64_t y_stride,
                  float* scales_dev, int32_t group);
