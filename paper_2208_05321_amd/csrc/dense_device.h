@@ -74,6 +74,11 @@ __device__ __forceinline__ void store_from_float(T* __restrict__ p, const float 
     }
 }
 
+// Where a row's last two vectors overlap, a lane stores elements that another lane of the wavefront reads (in place, or added to): what was read
+// before this is read before what is stored after it.  A wavefront's accesses leave in the order of its instructions; this keeps the compiler, which looks at one
+// lane at a time, from changing that order, and is no instruction itself.
+__device__ __forceinline__ void read_before_stores() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Sum over the wavefront's lanes, all of them active, in every lane.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float add_lane(float x) {

@@ -325,6 +325,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_bwd(NormBwd a) {
                 s2 = counts<END>(q, e) ? fmaf(x[b][e], x[b][e], s2) : s2;
             }
         }
+        if (END == OVER && TPR <= 64) read_before_stores();
         row_sums<TPR>(s1, s2, lds + turn);
         const float rho = rsqrtf(s2 / (float)a.dim + a.eps), m = rho * rho * (s1 / (float)a.dim);
 #pragma unroll K

@@ -286,6 +286,7 @@ __device__ __forceinline__ void token_row(float scale, G* __restrict__ out, cons
     if (ADD) {
 #pragma unroll
         for (int u = 0; u < U; ++u) if (c.at[u] >= 0) load_vector(old[u], out + c.at[u]);
+        read_before_stores();
     }
     sum(acc);
 #pragma unroll
@@ -392,6 +393,7 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_runs(TokenRows q, const S
                         load_vector(v[k][u], grad_out + (size_t)token[k] * stride + cols.at[u]);
                         if (ADD) load_vector(old[k][u], grad + (size_t)key[k] * grad_stride + cols.at[u]);
                     }
+            if (ADD) read_before_stores();
 #pragma unroll
             for (int k = 0; k < SB; ++k)
 #pragma unroll
