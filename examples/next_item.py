@@ -9,7 +9,8 @@ SEQ.  Items and positions have small dense tables.
 
 The backward pass gives the norm's weight, the item table (padding left out) and the position table their gradients; they are clipped together with
 the head's and the pooled context rows' by one global norm, and stepped by plain SGD, the cached table by its fused backward pass (the update is
-linear in the pooled rows' gradient, so that clipping that clips the step).
+linear in the pooled rows' gradient, so that clipping that clips the step; its share of the norm is that of the pooled rows, which is not the table's where a
+bag or a batch has an id more than once).
 
     python examples/next_item.py [--steps 30]
 """

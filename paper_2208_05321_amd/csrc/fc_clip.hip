@@ -17,6 +17,8 @@ namespace fc {
 
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_GROUP = 120;                    // tensors that one launch's arguments can describe (a launch takes 4 KB of them)
+// us a call.  Workgroups, 1024 / 2048 / 4096 at most: 20 f32 tensors of 1 M elements 42.5 / 46.8 / 46.0, 240 of 1.9 M bf16 548 / 549 / 541, 20 of 105 k f32 13.9 / 13.7 / 13.8.
+// Elements of a tile, 4096 / 8192 / 16,384: 45.0 / 46.8 / 42.5, 562 / 549 / 546, 12.0 / 13.7 / 13.5, one of 4 M bf16 10.4 / 9.2 / 9.2.
 constexpr int CLIP_BLOCKS = 2048;                  // workgroups
 constexpr int64_t CLIP_TILE = 8192;                // elements; a tile belongs to one tensor
 

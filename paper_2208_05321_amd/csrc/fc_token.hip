@@ -7,8 +7,8 @@
 // order) and every row of the gradient is written once, by the lanes that add its tokens up; without accumulation a row without
 // tokens gets its zeros in the same pass.  Popular ids are what a sum by rows has to be protected from: the sorted tokens are cut
 // into chunks of 16, and a chunk that lies inside one id's run is added up beforehand, by lanes of its own, as are 16 such chunks
-// in a row (a stretch) and 16 stretches (a mile).  A row then adds at most 30 tokens, 30 chunks, 30 stretches and n / 4096 miles, whatever the
-// ids.  All sums are in 32 bits and in an order that depends on the ids alone: results are reproducible.
+// in a row (a stretch) and, from 65,536 tokens on, 16 stretches (a mile).  A row then adds at most 30 tokens, 30 chunks, 30 stretches and n / 4096 miles,
+// whatever the ids; with fewer tokens there are no miles, and it adds up to n / 256 stretches, 255 at most.  All sums are in 32 bits and in an order that depends on the ids alone: results are reproducible.
 // HBM bounds the large calls (the zeros of the dense gradient alone are 142 us of the 226 that one of 131,072 rows of 2048 columns takes with 16 k tokens),
 // the chain sort - chunks - rows the others: 426 k tokens of 128 columns added to 1 M rows 98 us, 32 of them the sort and 28 the chunks.
 // (With chunks of 64 a popular row's 126 tokens, one after the other, were the kernel's duration: dense gradient of 131,072 rows of 2048
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(TOK_THREADS) void k_token_rows(TokenRows q, const S
 }
 
 // 47 k rows of 128 columns added to, 426 k tokens 31 to 33 us; 4.7 k rows of 2048 stored, 16 k tokens 34 to 36: bound by the longest chains of loads (token, row, then up to
-// 30 of each level), which is why levels are sixteen apart and a group's tokens are in its lanes before it needs them.
+// 30 of each level below the last), which is why levels are sixteen apart and a group's tokens are in its lanes before it needs them.
 // Rows with tokens, stored or (ADD) added to what the gradient holds: a row-group takes the runs that begin at its PER positions.
 template <bool ADD, int PER, int U, int N, class S, class G>
 __global__ __launch_bounds__(TOK_THREADS) void k_token_runs(TokenRows q, const S* __restrict__ grad_out, int64_t stride, const int32_t* __restrict__ keys, int n,
