@@ -161,7 +161,7 @@ struct NormFwd {
     float eps;
 };
 
-// 8192 rows of 8192 bf16 columns with residual, to 8 bits by groups of 128: 98 to 101 us (472 MB, 4.7 TB/s); one row of 4096 3.1 us; 777 of 1111 f16 3.
+// 8192 rows of 8192 bf16 columns with residual, to 8 bits by groups of 128: 97 to 99 us (472 MB, 4.8 TB/s); one row of 4096 3.2 us; 777 of 1111 f16 3.
 // KEEP: vectors of a row that a lane keeps in registers, 0: rows too wide for that, h is worked out again for each of the steps (with END PART)
 template <int TPR, int KEEP, int END, class T, class Q>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_fwd(NormFwd a) {
