@@ -349,7 +349,7 @@ typedef struct fc_dense fc_dense; /* opaque: stream, workspace, sticky error; on
 /* On the current device; hip_stream: hipStream_t (NULL = default stream) of all its calls. */
 int dense_create(void* hip_stream, fc_dense** out);
 /* Allocate now what calls up to these sizes need beyond the caller's memory: token_embed_bwd of max_tokens ids and a table of max_rows rows of max_dim
- * columns, rms_norm_bwd of any number of rows of max_dim columns, grad_norm_clip of max_tensors tensors.  What token_embed_bwd needs grows with
+ * columns, rms_norm_bwd of any number of rows of max_dim columns, grad_norm_clip of max_tensors tensors; distill_* and beam_* of any sizes where max_dim > 0.  What token_embed_bwd needs grows with
  * max_tokens * max_dim: a wide norm beside a narrow table is better reserved by a call of its own (max_tokens 0), as the workspace keeps the larger of
  * the two.  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
  * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured into a graph; buffers that a captured call uses stay
@@ -401,6 +401,58 @@ int rms_norm_bwd(fc_dense* d, const void* grad_y_dev, int64_t grad_y_stride, con
  * A norm that is infinite or no number makes the factor 0 or no number, as the formula says. */
 int grad_norm_clip(fc_dense* d, const void* const* grads_dev, void* const* out_dev, const int64_t* sizes, const int32_t* types, int32_t count,
                    float max_norm, float* norm_dev);
+
+/* Distillation from a teacher's top logits, with cross entropy beside it.  Row i has logits x (of `type`, dim of them: the vocabulary), `top` entries of the teacher
+ * (ids t_k, logits z_k; an id of -1: no entry; 0 <= top <= 1024) and, if targets are given, an id y.  With T = temperature (1/1024 to 1024), a = alpha (0 to 1):
+ *   P_k = exp(z_k / T - L), where L = teacher_lse[i] is the logarithm of the sum of exp(z / T) over the teacher's whole vocabulary, and P_0 = max(0, 1 - sum P_k) is what
+ *         the entries leave over;  teacher_lse NULL: L is that of the row's entries, and P_0 = 0
+ *   Q = softmax(x / T), Q_0 = the sum of Q over the ids that no entry names
+ *   loss[i] = a T^2 (sum P_k (log P_k - log Q[t_k]) + P_0 (log P_0 - log Q_0)) + (1 - a) (-log softmax(x)[y])
+ * Sums are over the row's entries: an id that is named twice counts twice among P, and once among those that Q_0 leaves out.  Terms with P = 0, and with a factor a or 1 - a of 0, are 0.  A row without
+ * entries (or, without teacher_lse, with entries of -infinity only) has no first term (and is left out where a is 1).  A target of -1 leaves the row out: its loss and gradient are 0, whatever its
+ * logits hold; other ids outside [0, dim) raise the sticky FC_ERR_ID_OUT_OF_RANGE, an entry then does not count, and a row with such a target is left out.
+ * Logits of -infinity are ids of probability 0; rows with logits that are +infinity, no number or all -infinity have a loss and a gradient that are no numbers.  Logits
+ * over the temperature are below 2^126 in magnitude.  targets may be NULL where alpha is 1.
+ *   type, teacher_type F32, BF16, F16; id_type (teacher_ids [n][top]) and target_type I32 or I64; loss fp32[n];
+ *   stats fp32[n][12]: what distill_bwd needs of the forward pass (of no meaning otherwise). */
+int distill_fwd(fc_dense* d, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t n, int32_t dim, const void* teacher_ids_dev, int32_t id_type,
+                const void* teacher_dev, int32_t teacher_type, int32_t top, const float* teacher_lse_dev, const void* targets_dev, int32_t target_type,
+                float temperature, float alpha, float* loss_dev, float* stats_dev);
+/* Its backward pass: grad_logits[i] = grad_loss[i * grad_loss_stride] * the gradient of loss[i], of the logits' type.
+ *   grad_loss_stride 1, or 0: one number for all rows.  A row whose grad_loss is 0 gets zeros, whatever its logits hold.  The other arguments are those of the forward call;
+ *   grad_logits may be logits itself (same stride). */
+int distill_bwd(fc_dense* d, const float* grad_loss_dev, int64_t grad_loss_stride, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t n, int32_t dim,
+                const void* teacher_ids_dev, int32_t id_type, const void* teacher_dev, int32_t teacher_type, int32_t top, const void* targets_dev, int32_t target_type,
+                float temperature, float alpha, const float* stats_dev, void* grad_logits_dev, int64_t grad_logits_stride);
+/* Both in one call, where grad_loss is known beforehand (1 / n for a mean): the same loss and gradient. */
+int distill_grad(fc_dense* d, const float* grad_loss_dev, int64_t grad_loss_stride, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t n, int32_t dim,
+                 const void* teacher_ids_dev, int32_t id_type, const void* teacher_dev, int32_t teacher_type, int32_t top, const float* teacher_lse_dev,
+                 const void* targets_dev, int32_t target_type, float temperature, float alpha, float* loss_dev, void* grad_logits_dev, int64_t grad_logits_stride);
+
+/* One step of beam search: of the candidates (w, v) of each of `batch` sequences,
+ *   c = scores[w] + x[w][v] - log(sum over u of exp(x[w][u])),   of a beam with finished[w] != 0 only (w, eos_id) with c = scores[w],
+ * the `keep` largest in descending order: scores_out, parents_out (w), tokens_out (v), [batch][keep] each.  Of equal ones the lower beam comes first, then the larger
+ * logit, then the lower id.  Candidates are compared in 64 bits, scores are rounded to 32 when stored.
+ *   logits of `type` (F32, BF16, F16), batch * beams rows; scores fp32[batch][beams]; beams, keep: 1 to 64; tokens I32 or I64.
+ *   finished uint8[batch][beams], may be NULL; finished_out uint8[batch][keep] = (token == eos_id), may be NULL; eos_id -1: none, then both are NULL.
+ * A logit of -infinity is no candidate.  A beam whose score is -infinity has none (its logits are not read), nor has one whose score is +infinity or no number or whose
+ * logits hold a +infinity or one that is no number.  Where fewer than `keep` candidates are left the remaining places hold score -infinity, parent 0, token max(eos_id, 0). */
+int beam_select(fc_dense* d, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t batch, int32_t beams, int32_t dim, const float* scores_dev,
+                const uint8_t* finished_dev, int32_t eos_id, int32_t keep, float* scores_out_dev, int32_t* parents_out_dev, void* tokens_out_dev, int32_t token_type,
+                uint8_t* finished_out_dev);
+/* A tensor of beam_reorder: rows of `pieces` pieces of piece_bytes bytes each, of any type; row r begins src_row * r bytes from src, piece p of it src_piece * p bytes on
+ * (pieces of a row, and rows, do not overlap).  The same for dst. */
+typedef struct {
+    const void* src;
+    void* dst;
+    int64_t src_row, dst_row, src_piece, dst_piece;
+    int64_t piece_bytes, pieces;
+} fc_state;
+/* Reordering of the states of beams: for every tensor, row b * keep + j of dst = row b * beams + parents[b][j] of src.  parents [batch][keep], I32 or I64; beams, keep: 1 to 64.
+ * dst may be src (then keep == beams, and the strides are the same): rows that are their own parent are not touched.  Tensors do not overlap otherwise.
+ * A parent outside [0, beams) raises the sticky FC_ERR_ID_OUT_OF_RANGE; its row of dst becomes zeros, in place it stays as it was.  `states` is a host array, read before the call
+ * returns; pieces and piece_bytes below 2^31, a row below 2^35 bytes. */
+int beam_reorder(fc_dense* d, const fc_state* states, int32_t count, int64_t batch, int32_t beams, const void* parents_dev, int32_t parent_type, int32_t keep);
 
 /* ---- per-kernel timing with HIP events on the handle's own streams (for the benchmark) ----
  * Each item stands for one kind of work.  While recording, what shares a launch otherwise is launched by itself: the sort of a small batch

@@ -34,6 +34,7 @@ EXPORTS = (
     "cache_profile_get", "freq_create", "freq_add", "freq_build", "freq_destroy", "table_reorder",
     "dense_create", "dense_reserve", "dense_check", "dense_destroy", "token_embed_fwd", "token_embed_bwd",
     "rms_norm_fwd", "rms_norm_bwd", "grad_norm_clip",
+    "distill_fwd", "distill_bwd", "distill_grad", "beam_select", "beam_reorder",
 )
 
 
@@ -102,6 +103,11 @@ def load_library(path: str | None = None):
     L.rms_norm_fwd.argtypes = [vp, vp, i32, i64, vp, i64, vp, i32, i64, i32, f32, vp, i64, vp, i32, i64, vp, i32]
     L.rms_norm_bwd.argtypes = [vp, vp, i64, vp, i32, i64, vp, i32, vp, i64, i64, i32, f32, vp, i64, vp, i32]
     L.grad_norm_clip.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp]
+    L.distill_fwd.argtypes = [vp, vp, i32, i64, i64, i32, vp, i32, vp, i32, i32, vp, vp, i32, f32, f32, vp, vp]
+    L.distill_bwd.argtypes = [vp, vp, i64, vp, i32, i64, i64, i32, vp, i32, vp, i32, i32, vp, i32, f32, f32, vp, vp, i64]
+    L.distill_grad.argtypes = [vp, vp, i64, vp, i32, i64, i64, i32, vp, i32, vp, i32, i32, vp, vp, i32, f32, f32, vp, vp, i64]
+    L.beam_select.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, vp, i32, i32, vp, vp, vp, i32, vp]
+    L.beam_reorder.argtypes = [vp, vp, i32, i64, i32, vp, i32, i32]
     for name in EXPORTS:
         if name not in ("cache_host_weight", "cache_strerror", "cache_profile_name"):
             getattr(L, name).restype = ctypes.c_int

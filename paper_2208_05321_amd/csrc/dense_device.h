@@ -111,6 +111,8 @@ int dense_capturing(fc_dense* d, bool* now);   // whether the handle's stream is
 size_t token_work_bytes(int64_t n, int64_t rows, int64_t dim);
 size_t norm_work_bytes(int64_t n, int64_t dim);
 size_t clip_work_bytes(int64_t tensors);
+size_t distill_work_bytes();                   // both whatever the sizes
+size_t beam_work_bytes();
 
 // Threads of one launch: the runtime takes fewer than 2^32.  Rows that need more go in several.
 constexpr int64_t LAUNCH_THREADS = (int64_t)1 << 31;

@@ -1,0 +1,327 @@
+// Beam search: the selection over beams and vocabulary.
+//
+//   candidates (w, v) of a sequence:  c = s[w] + x[w, v] - log sum_u exp(x[w, u]);  of a beam that has ended only (w, eos) with c = s[w]
+//   the `keep` largest, in descending order; equal ones: lower beam, larger logit, lower id
+//
+// Within a beam the order is that of the logits, so a slice of a row (in registers, read once) gives its `keep` largest logits and its sum of
+// exponentials, and one workgroup for a sequence puts beams and slices together.  HBM bounds the first step: 8 bytes of lists a candidate against 32 KB read.
+// The candidates are put in order in 64 bits: sums of exponentials are added up in 64 bits over the lanes, and nothing is rounded before the scores are stored.
+//
+// The `keep` largest of a workgroup's elements: those above a bound that is no larger than the `keep`-th largest are few, and are ranked by
+// counting.  The bound is the `keep`-th largest of the lanes' largest elements.
+#include "logits_device.h"
+
+#include <algorithm>
+#include <float.h>
+
+#include <type_traits>
+
+namespace fc {
+
+constexpr int BEAM_MOST = 64;                      // beams of a sequence, and candidates kept
+constexpr int BEAM_LIST = 1024;                    // elements above the bound that are ranked by counting; with more of them one is found at a time
+
+struct BeamArgs {
+    const void* x;
+    int64_t stride;
+    const float* scores;
+    const uint8_t* finished;                       // or NULL
+    int32_t beams, dim, keep, eos, slices;
+};
+// what a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are in a list of `keep`
+struct BeamSlice { double sum; float off; int32_t count; };
+struct BeamEntry { float x; int32_t id; };
+
+// numbers in the order of unsigned integers (no distinction between zeros)
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+// larger logit first, then lower id
+__device__ __forceinline__ uint64_t entry_key(float x, int id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
+
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+// The n-th largest of the wavefront's keys, but for the 16 lower bits, which are 0.
+__device__ __forceinline__ uint32_t wave_bound(uint32_t key, int n) {
+    uint32_t bound = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t t = bound | 1u << b;
+        if (__popcll(__ballot(key >= t)) >= n) bound = t;
+    }
+    return bound;
+}
+
+template <class K>
+__device__ __forceinline__ K block_max(K x, K* lds) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) { const K y = __shfl_xor(x, o); x = y > x ? y : x; }
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+#pragma unroll
+    for (int k = 1; k < LOGIT_THREADS / 64; ++k) x = lds[k] > x ? lds[k] : x;
+    __syncthreads();
+    return x;
+}
+
+// whether the beam has candidates: one whose score is -infinity, or no finite number, has none
+__device__ __forceinline__ bool beam_lives(const BeamArgs& a, int64_t row) {
+    const float s = a.scores[row];
+    return s - s == 0.f;
+}
+
+template <class T, int PER>
+__global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_t first, BeamSlice* __restrict__ sums, BeamEntry* __restrict__ lists) {
+    using Slice = RowSlice<T, LOGIT_THREADS, PER>;
+    constexpr int N = Slice::N;
+    __shared__ uint64_t list[BEAM_LIST];
+    __shared__ uint64_t best[LOGIT_THREADS / 64];
+    __shared__ uint32_t bounds[LOGIT_THREADS / 64];
+    __shared__ float offs[LOGIT_THREADS / 64];
+    __shared__ double parts[LOGIT_THREADS / 64];
+    __shared__ int count;
+    const int lane = threadIdx.x, slice = blockIdx.x % a.slices, base = slice * Slice::COLUMNS;
+    const int64_t local = blockIdx.x / a.slices, row = first + local;
+    if (!beam_lives(a, row) || (a.finished && a.finished[row])) return;
+    const T* x = (const T*)a.x + row * a.stride;
+    Slice s;
+    s.load(x, base, lane, a.dim);
+    float most[PER], top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        most[k] = s.at(k, 0);
+#pragma unroll
+        for (int e = 1; e < N; ++e) most[k] = fmaxf(most[k], s.at(k, e));
+        top = fmaxf(top, most[k]);
+    }
+    // sum of exponentials, each lane's from its own largest element
+    const float off = top * LOG2E, by = -from_of(off);
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(s.at(k, e), LOG2E, by));
+    const float off_wave = wave_max(off);
+    const double part = wave_sum((double)(sum * __builtin_amdgcn_exp2f(off - from_of(off_wave))));
+    const uint32_t bound_wave = wave_bound(ordered(top), a.keep);
+    if (lane == 0) count = 0;
+    if ((lane & 63) == 0) { offs[lane >> 6] = off_wave; parts[lane >> 6] = part; bounds[lane >> 6] = bound_wave; }
+    __syncthreads();
+    uint32_t bound = 0x00800000u;                  // the lowest finite number: -infinity is no candidate
+#pragma unroll
+    for (int k = 0; k < LOGIT_THREADS / 64; ++k) bound = max(bound, bounds[k]);
+    const float least = unordered(bound);
+    if (top >= least) {
+        uint32_t at = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) if (most[k] >= least) at |= 1u << k;
+        while (at) {
+            const int k = __builtin_ctz(at);
+            at &= at - 1;
+            typename Slice::V v = s.x[0];
+#pragma unroll
+            for (int j = 1; j < PER; ++j) if (j == k) v = s.x[j];
+            const int col = min(Slice::column(base, lane, k), a.dim - N);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if ((float)v[e] >= least) {
+                    const int p = atomicAdd(&count, 1);
+                    if (p < BEAM_LIST) list[p] = entry_key((float)v[e], col + e);
+                }
+        }
+    }
+    __syncthreads();
+    BeamEntry* out = lists + (local * a.slices + slice) * a.keep;
+    auto put = [&](int at, uint64_t key) { out[at] = BeamEntry{unordered((uint32_t)(key >> 32)), (int32_t)~(uint32_t)key}; };
+    int got = count;
+    if (got <= BEAM_LIST) {
+        for (int i = lane; i < got; i += LOGIT_THREADS) {
+            const uint64_t key = list[i];
+            int rank = 0;
+            for (int j = 0; j < got; ++j) rank += list[j] > key;
+            if (rank < a.keep) put(rank, key);
+        }
+        got = min(got, a.keep);
+    } else {                                       // (as good as equal logits)
+        uint64_t last = ~0ull;
+        got = a.keep;
+        for (int i = 0; i < a.keep; ++i) {
+            uint64_t mine = 0;
+            for (int c = base + lane; c < min(a.dim, base + Slice::COLUMNS); c += LOGIT_THREADS) {
+                const float v = (float)x[c];
+                const uint64_t key = entry_key(v, c);
+                if (v >= least && key < last && key > mine) mine = key;
+            }
+            last = block_max(mine, best);
+            if (lane == 0) put(i, last);
+        }
+    }
+    if (lane == 0) {
+        float to = offs[0];
+        for (int k = 1; k < LOGIT_THREADS / 64; ++k) to = fmaxf(to, offs[k]);
+        double all = 0.;
+        for (int k = 0; k < LOGIT_THREADS / 64; ++k) all += parts[k] * (double)exp2f(offs[k] - from_of(to));
+        sums[local * a.slices + slice] = BeamSlice{all, to, got};
+    }
+}
+
+// A candidate in the order of the search.
+struct Candidate { double c; float x; int32_t beam, id; };
+__device__ __forceinline__ bool before(const Candidate& p, const Candidate& q) {
+    if (p.c != q.c) return p.c > q.c;
+    if (p.beam != q.beam) return p.beam < q.beam;
+    if (p.x != q.x) return p.x > q.x;
+    return p.id < q.id;
+}
+
+// One workgroup puts a sequence's beams and slices together.
+__global__ __launch_bounds__(LOGIT_THREADS) void k_beam_join(BeamArgs a, int64_t first, const BeamSlice* __restrict__ sums, const BeamEntry* __restrict__ lists,
+                                                             float* __restrict__ scores_out, int32_t* __restrict__ parents_out, void* __restrict__ tokens_out,
+                                                             int32_t token_type, uint8_t* __restrict__ finished_out) {
+    __shared__ double add[BEAM_MOST];              // what a beam's logits lack to be candidates; not finite: there are none
+    __shared__ bool ended[BEAM_MOST];
+    __shared__ double tops[LOGIT_THREADS];
+    __shared__ Candidate list[BEAM_LIST];
+    __shared__ double least;
+    __shared__ int count;
+    const int lane = threadIdx.x;
+    const int64_t seq = blockIdx.x, row0 = first + seq * a.beams;
+    for (int w = lane >> 6; w < a.beams; w += LOGIT_THREADS / 64) {
+        const int64_t row = row0 + w;
+        const bool lives = beam_lives(a, row), end = a.finished && a.finished[row];
+        double v = lives ? 0. : -INFINITY;
+        if (lives && !end) {
+            const BeamSlice* s = sums + (seq * a.beams + w) * a.slices;
+            float to = -INFINITY;
+            for (int k = lane & 63; k < a.slices; k += 64) to = fmaxf(to, s[k].off);
+            to = from_of(wave_max(to));
+            double sum = 0.;
+            for (int k = lane & 63; k < a.slices; k += 64) sum += s[k].sum * (double)exp2f(s[k].off - to);
+            v = -0.69314718055994530942 * ((double)to + log2(wave_sum(sum)));
+        }
+        if ((lane & 63) == 0) { add[w] = v + (double)a.scores[row]; ended[w] = end; }
+    }
+    if (lane == 0) { count = 0; least = -INFINITY; }
+    __syncthreads();
+    // f(candidate) for each of this lane's candidates
+    const int each = a.slices * a.keep, all = a.beams * each;       // (below 2^22)
+    auto candidates = [&](auto f) {
+        for (int i = lane; i < all; i += LOGIT_THREADS) {
+            const int w = i / each, at = i - w * each;
+            const double v = add[w];
+            if (!(v - v == 0.)) continue;
+            if (ended[w]) { if (at == 0) f(Candidate{v, 0.f, w, a.eos}); continue; }
+            const int64_t k = (seq * a.beams + w) * a.slices + at / a.keep;
+            const int j = at % a.keep;
+            if (j >= sums[k].count) continue;
+            const BeamEntry e = lists[k * a.keep + j];
+            f(Candidate{v + (double)e.x, e.x, w, e.id});
+        }
+    };
+    double top = -INFINITY;
+    candidates([&](const Candidate& q) { top = fmax(top, q.c); });
+    tops[lane] = top;
+    __syncthreads();
+    int above = 0;
+    for (int k = 0; k < LOGIT_THREADS; ++k) above += tops[k] > top || (tops[k] == top && k < lane);
+    if (above == a.keep - 1) least = top;
+    __syncthreads();
+    const double bound = least;
+    if (top >= bound)
+        candidates([&](const Candidate& q) {
+            if (q.c < bound) return;
+            const int p = atomicAdd(&count, 1);
+            if (p < BEAM_LIST) list[p] = q;
+        });
+    __syncthreads();
+    auto put = [&](int at, const Candidate& q) {
+        const int64_t o = seq * a.keep + at;
+        scores_out[o] = (float)q.c;
+        parents_out[o] = q.beam;
+        if (token_type == FC_TYPE_I64) ((int64_t*)tokens_out)[o] = q.id; else ((int32_t*)tokens_out)[o] = q.id;
+        if (finished_out) finished_out[o] = q.id == a.eos;
+    };
+    int got = count;
+    if (got <= BEAM_LIST) {
+        for (int i = lane; i < got; i += LOGIT_THREADS) {
+            const Candidate q = list[i];
+            int rank = 0;
+            for (int j = 0; j < got; ++j) rank += before(list[j], q);
+            if (rank < a.keep) put(rank, q);
+        }
+        got = min(got, a.keep);
+    } else {
+        Candidate last{INFINITY, 0.f, -1, -1};
+        got = a.keep;
+        for (int i = 0; i < a.keep; ++i) {
+            Candidate mine{-INFINITY, 0.f, 1 << 30, 0};
+            candidates([&](const Candidate& q) { if (before(last, q) && before(q, mine)) mine = q; });
+            __syncthreads();
+            list[lane] = mine;
+            for (int o = LOGIT_THREADS / 2; o > 0; o >>= 1) {
+                __syncthreads();
+                if (lane < o && before(list[lane + o], list[lane])) list[lane] = list[lane + o];
+            }
+            __syncthreads();
+            last = list[0];
+            if (lane == 0) put(i, last);
+        }
+    }
+    for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) put(i, Candidate{-INFINITY, 0.f, 0, max(a.eos, 0)});
+}
+
+constexpr size_t BEAM_WORK = (size_t)5 << 20;      // of a launch's slices (one sequence takes 4.4 MB at most); more sequences go in several
+size_t beam_work_bytes() { return BEAM_WORK; }
+
+template <class T, int PER>
+void beam_run(fc_dense* d, BeamArgs a, int64_t batch, float* scores, int32_t* parents, void* tokens, int32_t token_type, uint8_t* finished) {
+    a.slices = (int32_t)cdiv(a.dim, RowSlice<T, LOGIT_THREADS, PER>::COLUMNS);
+    const size_t of_seq = (size_t)a.beams * a.slices * (sizeof(BeamSlice) + a.keep * sizeof(BeamEntry));
+    const int64_t most = std::max<int64_t>(1, (int64_t)(BEAM_WORK / of_seq));
+    for (int64_t at = 0; at < batch; at += most) {
+        const int64_t n = std::min(most, batch - at);
+        BeamSlice* sums = reinterpret_cast<BeamSlice*>(d->work);
+        BeamEntry* lists = reinterpret_cast<BeamEntry*>(sums + n * a.beams * a.slices);
+        k_beam_slice<T, PER><<<(unsigned)(n * a.beams * a.slices), LOGIT_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists);
+        const int64_t o = at * a.keep;
+        k_beam_join<<<(unsigned)n, LOGIT_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists, scores + o, parents + o,
+                                                                  (char*)tokens + o * (token_type == FC_TYPE_I64 ? 8 : 4), token_type, finished ? finished + o : nullptr);
+    }
+}
+
+}  // namespace fc
+
+using namespace fc;
+
+extern "C" {
+
+int beam_select(fc_dense* d, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t batch, int32_t beams, int32_t dim, const float* scores_dev,
+                const uint8_t* finished_dev, int32_t eos_id, int32_t keep, float* scores_out_dev, int32_t* parents_out_dev, void* tokens_out_dev, int32_t token_type,
+                uint8_t* finished_out_dev) {
+    if (!d || batch < 0 || batch >= DENSE_LIMIT || beams <= 0 || beams > BEAM_MOST || keep <= 0 || keep > BEAM_MOST || dim <= 0 || dim > DENSE_MAX_DIM || logits_stride < dim ||
+        !is_float_type(type) || (token_type != FC_TYPE_I32 && token_type != FC_TYPE_I64) || eos_id < -1 || eos_id >= dim || (finished_dev && eos_id < 0) ||
+        (finished_out_dev && eos_id < 0) || (batch > 0 && (!logits_dev || !scores_dev || !scores_out_dev || !parents_out_dev || !tokens_out_dev)))
+        return FC_ERR_INVALID_ARG;
+    if (batch == 0) return FC_OK;
+    FC_HIP(hipSetDevice(d->device));
+    FC_TRY(dense_work(d, BEAM_WORK));
+    return with_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        const BeamArgs a{logits_dev, logits_stride, scores_dev, finished_dev, beams, dim, keep, eos_id, 1};
+        const int64_t vectors = cdiv(dim, VECTOR<T>);
+        if (vectors <= LOGIT_THREADS * 2 || batch * beams * cdiv(vectors, LOGIT_THREADS * 8) < 512)
+            beam_run<T, 2>(d, a, batch, scores_out_dev, parents_out_dev, tokens_out_dev, token_type, finished_out_dev);
+        else beam_run<T, 8>(d, a, batch, scores_out_dev, parents_out_dev, tokens_out_dev, token_type, finished_out_dev);
+        FC_HIP(hipGetLastError());
+        return FC_OK;
+    });
+}
+
+}  // extern "C"

@@ -108,7 +108,7 @@ int dense_reserve(fc_dense* d, int64_t max_tokens, int64_t max_rows, int32_t max
     FC_HIP(hipSetDevice(d->device));
     if (max_tokens > 0) FC_TRY(dense_sort(d, max_tokens));
     size_t most = clip_work_bytes(max_tensors);
-    if (max_dim > 0) most = std::max({most, token_work_bytes(max_tokens, max_rows, max_dim), norm_work_bytes(DENSE_LIMIT, max_dim)});
+    if (max_dim > 0) most = std::max({most, token_work_bytes(max_tokens, max_rows, max_dim), norm_work_bytes(DENSE_LIMIT, max_dim), distill_work_bytes(), beam_work_bytes()});
     return dense_work(d, most);
 }
 

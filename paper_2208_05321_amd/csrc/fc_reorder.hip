@@ -1,0 +1,154 @@
+// Reordering of the states of beams: row (b, j) becomes row (b, parent[b, j]), for a list of tensors, in place or into others.
+//
+// A copy, bound by HBM: what is read are the distinct parents of the rows that change, what is written those rows.  A thread owns 16 bytes of every beam's row of a
+// sequence (8 or 4 where more than 16 or 32 of them move) and reads all of them before it writes one, so that in place a row may be another's
+// source in any pattern, without a second buffer or a wait between workgroups.  Rows that stay are not touched.
+#include "dense_device.h"
+
+#include <algorithm>
+
+namespace fc {
+
+constexpr int STATE_THREADS = 256;
+constexpr int STATE_MOST_BEAMS = 64;
+constexpr int STATE_GROUP = 44;                    // tensors that one launch's arguments can describe
+constexpr int STATE_TILE = 1024;                   // vectors of 16 bytes of a row that a workgroup moves, for every beam
+struct StateRows {
+    const char* src;
+    char* dst;
+    int64_t src_row, dst_row, src_piece, dst_piece, begin;      // begin: its first workgroup
+    uint32_t piece, vectors;                       // bytes of a piece; vectors of a row (pieces * those of a piece)
+    uint32_t per, tiles;                           // vectors of a piece, workgroups of a sequence
+};
+struct StateGroup { StateRows t[STATE_GROUP]; int count; };
+static_assert(sizeof(StateGroup) + 64 <= 4096, "arguments of a launch");
+
+template <int BYTES> struct Chunk { typedef uint32_t V __attribute__((ext_vector_type(BYTES / 4), aligned(1))); };
+template <> struct Chunk<4> { typedef uint32_t V __attribute__((aligned(1))); };
+template <> struct Chunk<2> { typedef uint16_t V __attribute__((aligned(1))); };
+template <> struct Chunk<1> { typedef uint8_t V; };
+
+struct Moves { int from[STATE_MOST_BEAMS], to[STATE_MOST_BEAMS]; int count, none; };       // none: rows that become zeros, listed from the end of `to`
+
+// Every move of one chunk of the rows: all rows are read before one is written, as in place a row may be another's source.
+template <int BYTES, int MOST>
+__device__ __forceinline__ void move_chunk(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, int begin, int n) {
+    typename Chunk<BYTES>::V v[MOST];
+#pragma unroll
+    for (int i = 0; i < MOST; ++i)
+        v[i] = *reinterpret_cast<const typename Chunk<BYTES>::V*>(src + __builtin_amdgcn_readfirstlane(m.from[begin + min(i, n - 1)]) * src_row);
+#pragma unroll
+    for (int i = 0; i < MOST; ++i)
+        if (i < n) *reinterpret_cast<typename Chunk<BYTES>::V*>(dst + __builtin_amdgcn_readfirstlane(m.to[begin + i]) * dst_row) = v[i];
+}
+template <int BYTES, int MOST>
+__device__ __forceinline__ void move_rows(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m) {
+    if (m.count) move_chunk<BYTES, MOST>(src, dst, src_row, dst_row, m, 0, m.count);
+    for (int i = 0; i < m.none; ++i) *reinterpret_cast<typename Chunk<BYTES>::V*>(dst + m.to[STATE_MOST_BEAMS - 1 - i] * dst_row) = typename Chunk<BYTES>::V{};
+}
+template <int MOST>
+__device__ __forceinline__ void move_tile(const StateRows& t, const char* src, char* dst, int tile, const Moves& m) {
+    constexpr int BYTES = MOST <= 16 ? 16 : MOST <= 32 ? 8 : 4, SPLIT = 16 / BYTES;       // 64 registers of a lane at most
+    for (uint32_t i = threadIdx.x; i < STATE_TILE * SPLIT; i += STATE_THREADS) {
+        const uint32_t v = (uint32_t)tile * STATE_TILE + i / SPLIT;
+        if (v >= t.vectors) break;
+        const uint32_t piece = t.per == t.vectors ? 0 : v / t.per;
+        uint32_t at = (v - piece * t.per) * 16 + i % SPLIT * BYTES;
+        const char* s = src + piece * t.src_piece;
+        char* o = dst + piece * t.dst_piece;
+        if (at + BYTES <= t.piece) { move_rows<BYTES, MOST>(s + at, o + at, t.src_row, t.dst_row, m); continue; }
+        if (at >= t.piece) continue;
+        const uint32_t left = t.piece - at;
+        if (BYTES > 8 && left & 8) { move_rows<8, MOST>(s + at, o + at, t.src_row, t.dst_row, m); at += 8; }
+        if (BYTES > 4 && left & 4) { move_rows<4, MOST>(s + at, o + at, t.src_row, t.dst_row, m); at += 4; }
+        if (left & 2) { move_rows<2, MOST>(s + at, o + at, t.src_row, t.dst_row, m); at += 2; }
+        if (left & 1) move_rows<1, MOST>(s + at, o + at, t.src_row, t.dst_row, m);
+    }
+}
+
+__global__ __launch_bounds__(STATE_THREADS) void k_beam_reorder(StateGroup g, int64_t first, const void* __restrict__ parents, int32_t parent_type, int beams, int keep,
+                                                                uint32_t* __restrict__ flags) {
+    __shared__ Moves m;
+    const int64_t block = first + blockIdx.x;
+    int lo = 0, hi = g.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (g.t[mid].begin <= block) lo = mid; else hi = mid;
+    }
+    const StateRows& t = g.t[lo];
+    const int64_t seq = (block - t.begin) / t.tiles;
+    const int tile = (int)((block - t.begin) - seq * t.tiles);
+    const bool in_place = t.src == t.dst;
+    if (threadIdx.x < 64) {
+        const int j = threadIdx.x;
+        int64_t p = -1;
+        if (j < keep) p = parent_type == FC_TYPE_I64 ? ((const int64_t*)parents)[seq * keep + j] : (int64_t)((const int32_t*)parents)[seq * keep + j];
+        const bool known = p >= 0 && p < beams;
+        if (j < keep && !known) atomicOr(flags, (uint32_t)EF_ID_RANGE);
+        const bool moves = known && !(in_place && p == j), none = j < keep && !known && !in_place;
+        const uint64_t mm = __ballot(moves), nn = __ballot(none), below = ((uint64_t)1 << j) - 1;
+        if (moves) { const int k = __popcll(mm & below); m.from[k] = (int)p; m.to[k] = j; }
+        if (none) m.to[STATE_MOST_BEAMS - 1 - __popcll(nn & below)] = j;
+        if (j == 0) { m.count = __popcll(mm); m.none = __popcll(nn); }
+    }
+    __syncthreads();
+    const char* src = t.src + seq * beams * t.src_row;
+    char* dst = t.dst + seq * keep * t.dst_row;
+    const int n = __builtin_amdgcn_readfirstlane(m.count);
+    if (n <= 8) move_tile<8>(t, src, dst, tile, m);
+    else if (n <= 16) move_tile<16>(t, src, dst, tile, m);
+    else if (n <= 32) move_tile<32>(t, src, dst, tile, m);
+    else move_tile<64>(t, src, dst, tile, m);
+}
+
+}  // namespace fc
+
+using namespace fc;
+
+extern "C" {
+
+int beam_reorder(fc_dense* d, const fc_state* states, int32_t count, int64_t batch, int32_t beams, const void* parents_dev, int32_t parent_type, int32_t keep) {
+    if (!d || count < 0 || batch < 0 || batch >= DENSE_LIMIT || beams <= 0 || beams > STATE_MOST_BEAMS || keep <= 0 || keep > STATE_MOST_BEAMS ||
+        (parent_type != FC_TYPE_I32 && parent_type != FC_TYPE_I64) || (count > 0 && !states) || (count > 0 && batch > 0 && !parents_dev))
+        return FC_ERR_INVALID_ARG;
+    for (int32_t k = 0; k < count; ++k) {
+        const fc_state& s = states[k];
+        if (s.piece_bytes < 0 || s.pieces < 0) return FC_ERR_INVALID_ARG;
+        if (s.piece_bytes == 0 || s.pieces == 0 || batch == 0) continue;
+        if (!s.src || !s.dst || s.pieces >= (int64_t)1 << 31 || s.piece_bytes >= (int64_t)1 << 31 || cdiv(s.piece_bytes, 16) * s.pieces >= (int64_t)1 << 31 ||
+            (s.pieces > 1 && (s.src_piece < s.piece_bytes || s.dst_piece < s.piece_bytes)) ||
+            s.src_row < (s.pieces - 1) * s.src_piece + s.piece_bytes || s.dst_row < (s.pieces - 1) * s.dst_piece + s.piece_bytes ||
+            (s.src == s.dst && (keep != beams || s.src_row != s.dst_row || (s.pieces > 1 && s.src_piece != s.dst_piece))))
+            return FC_ERR_INVALID_ARG;
+    }
+    if (batch == 0) return FC_OK;
+    FC_HIP(hipSetDevice(d->device));
+    StateGroup g;
+    g.count = 0;
+    int64_t blocks = 0;
+    auto launch = [&]() {
+        const int64_t most = LAUNCH_THREADS / STATE_THREADS;
+        for (int64_t at = 0; at < blocks; at += most)
+            k_beam_reorder<<<(unsigned)std::min(most, blocks - at), STATE_THREADS, 0, d->stream>>>(g, at, parents_dev, parent_type, beams, keep, d->flags);
+        g.count = 0;
+        blocks = 0;
+    };
+    for (int32_t k = 0; k < count; ++k) {
+        fc_state s = states[k];
+        if (s.piece_bytes == 0 || s.pieces == 0) continue;
+        if (s.pieces > 1 && s.src_piece == s.piece_bytes && s.dst_piece == s.piece_bytes && s.pieces * s.piece_bytes < (int64_t)1 << 31) {
+            s.piece_bytes *= s.pieces;             // neighbours are one piece
+            s.pieces = 1;
+        }
+        if (g.count == STATE_GROUP) launch();
+        const int64_t per = cdiv(s.piece_bytes, 16), tiles = cdiv(per * s.pieces, STATE_TILE);
+        g.t[g.count++] = StateRows{(const char*)s.src, (char*)s.dst, s.src_row, s.dst_row, s.src_piece, s.dst_piece, blocks, (uint32_t)s.piece_bytes,
+                                   (uint32_t)(per * s.pieces), (uint32_t)per, (uint32_t)tiles};
+        blocks += tiles * batch;
+    }
+    launch();
+    FC_HIP(hipGetLastError());
+    return FC_OK;
+}
+
+}  // extern "C"

@@ -1,5 +1,5 @@
 """ctypes binding of the operators beside the cached table (include/freqcache.h): token embedding, root-mean-square norm, clipping by the
-global norm.  Marshalling only: shapes, types and strides are checked here, PyTorch supplies device memory and streams."""
+global norm, distillation, beam search.  Marshalling only: shapes, types and strides are checked here, PyTorch supplies device memory and streams."""
 from __future__ import annotations
 
 import ctypes
@@ -12,6 +12,8 @@ _TYPE_NAMES = {"float32": 0, "bfloat16": 1, "float16": 2, "float8_e4m3fn": 3, "i
 _FLOATS = (0, 1, 2)
 _MOST_DIM = 1 << 20              # columns of a row (the C ABI takes 32 bits of their number)
 _INF = float("inf")
+_STATS = 12                     # numbers of a row that the distillation's forward pass leaves for its backward pass
+_MOST_BEAMS = 64
 _dtype = attrgetter("dtype")
 
 
@@ -315,3 +317,207 @@ class DenseOps:
         elif max_norm != _INF:
             self._written(grads)
         return norm
+
+    # ---- distillation ----
+    def _teacher(self, logits, teacher_ids, teacher, targets, temperature: float, alpha: float):
+        """(type, rows, columns, stride) of the logits, and the arguments that describe the teacher's entries."""
+        k, n, d, xs = self._rows(logits, "logits")
+        if k not in _FLOATS:
+            _refuse(f"logits: type {logits.dtype}")
+        lead = logits.shape[:-1]
+        ik = self._ids(teacher_ids)
+        if teacher_ids.shape[:-1] != lead or teacher_ids.dim() != logits.dim() or teacher.shape != teacher_ids.shape:
+            _refuse(f"teacher_ids {tuple(teacher_ids.shape)} and teacher {tuple(teacher.shape)} for logits {tuple(logits.shape)}")
+        if teacher.get_device() != self._index or not teacher.is_contiguous():
+            _refuse(f"teacher: contiguous on {self.device} is wanted")
+        zk = self._type.get(teacher.dtype)
+        if zk not in _FLOATS:
+            _refuse(f"teacher: type {teacher.dtype}")
+        yk, yp = ik, None
+        if targets is not None:
+            yk = self._ids(targets)
+            if targets.shape != lead:
+                _refuse(f"targets {tuple(targets.shape)} for logits {tuple(logits.shape)}")
+            yp = targets.data_ptr()
+        elif alpha != 1.0:
+            _refuse(f"alpha {alpha} without targets")
+        if not 2.0 ** -10 <= temperature <= 2.0 ** 10 or not 0.0 <= alpha <= 1.0:
+            _refuse(f"temperature {temperature}, alpha {alpha}")
+        top = teacher_ids.shape[-1]
+        if top > 1024:
+            _refuse(f"teacher_ids: {top} entries of a row")
+        return (k, n, d, xs), (teacher_ids.data_ptr(), ik, teacher.data_ptr(), zk, top), (yp, yk), lead
+
+    def _of_rows(self, t, lead, what: str):
+        if t.get_device() != self._index or self._type.get(t.dtype) != 0 or not t.is_contiguous() or t.shape != lead:
+            _refuse(f"{what}: f32 {tuple(lead)} on {self.device}, contiguous, is wanted")
+        return t.data_ptr()
+
+    def _grad_loss(self, t, n: int, lead):
+        """(address, stride) of the gradients of the rows' losses: a tensor like the losses, a broadcast one, or one number."""
+        if t.get_device() != self._index or self._type.get(t.dtype) != 0:
+            _refuse(f"grad_loss: f32 on {self.device} is wanted")
+        if t.numel() == 1:
+            return t.data_ptr(), 0
+        if t.shape != lead:
+            _refuse(f"grad_loss {tuple(t.shape)} for rows {tuple(lead)}")
+        if t.is_contiguous():
+            return t.data_ptr(), 1
+        if not any(s for s, length in zip(t.stride(), t.shape) if length > 1):
+            return t.data_ptr(), 0
+        _refuse("grad_loss has to be contiguous, or one number")
+
+    def _grad_logits(self, logits, k: int, xs: int, out):
+        if out is None:
+            return self._like(logits), logits.shape[-1]
+        ok, _, _, os = self._rows(out, "out")
+        if ok != k or out.shape != logits.shape:
+            _refuse("out: another shape or type than logits")
+        if out.data_ptr() == logits.data_ptr() and os != xs:
+            _refuse("out: the logits' memory with another distance of rows")
+        return out, os
+
+    def distill_fwd(self, logits, teacher_ids, teacher, teacher_lse=None, targets=None, temperature: float = 1.0, alpha: float = 1.0):
+        """(loss, stats): of each row of logits [..., vocabulary] the divergence from a teacher's top logits, and cross entropy beside it,
+        alpha * T^2 * KL(teacher | softmax(logits / T)) + (1 - alpha) * -log softmax(logits)[target], f32 [...].
+        teacher_ids, teacher [..., top]: ids (-1: no entry) and logits.  teacher_lse [...] (f32): the log-sum of exp(z / T) over the teacher's whole vocabulary; what the entries leave
+        over is then one more category, the ids that none of them names.  Without it the entries are the whole distribution.
+        targets [...]: ids; -1 leaves the row out (loss 0).  `stats` [..., 12] is for distill_bwd."""
+        torch = self._torch
+        (k, n, d, xs), entries, target, lead = self._teacher(logits, teacher_ids, teacher, targets, temperature, alpha)
+        lse = None if teacher_lse is None else self._of_rows(teacher_lse, lead, "teacher_lse")
+        loss = torch.empty(lead, dtype=torch.float32, device=self.device)
+        stats = torch.empty((*lead, _STATS), dtype=torch.float32, device=self.device)
+        self._run("distill_fwd", self._L.distill_fwd, (logits, teacher_ids, teacher, teacher_lse, targets, loss, stats), logits.data_ptr(), k, xs, n, d,
+                  *entries, lse, *target, temperature, alpha, loss.data_ptr(), stats.data_ptr())
+        return loss, stats
+
+    def distill_bwd(self, grad_loss, logits, teacher_ids, teacher, stats, targets=None, temperature: float = 1.0, alpha: float = 1.0, out=None):
+        """Gradient of the logits, in their type: grad_loss (f32, like the losses, or one number) times that of each row's loss.  The other arguments are
+        the forward call's.  `out` may be logits."""
+        (k, n, d, xs), entries, target, lead = self._teacher(logits, teacher_ids, teacher, targets, temperature, alpha)
+        gp, gs = self._grad_loss(grad_loss, n, lead)
+        sp = self._of_rows(stats, (*lead, _STATS), "stats")
+        grad, os = self._grad_logits(logits, k, xs, out)
+        self._run("distill_bwd", self._L.distill_bwd, (grad_loss, logits, teacher_ids, teacher, stats, targets, grad), gp, gs, logits.data_ptr(), k, xs, n, d,
+                  *entries, *target, temperature, alpha, sp, grad.data_ptr(), os)
+        if out is not None:
+            self._written(out)
+        return grad
+
+    def distill_grad(self, grad_loss, logits, teacher_ids, teacher, teacher_lse=None, targets=None, temperature: float = 1.0, alpha: float = 1.0, out=None):
+        """(loss, gradient of the logits) in one call, where grad_loss is known beforehand (1 / rows for a mean).  `out` may be logits."""
+        torch = self._torch
+        (k, n, d, xs), entries, target, lead = self._teacher(logits, teacher_ids, teacher, targets, temperature, alpha)
+        lse = None if teacher_lse is None else self._of_rows(teacher_lse, lead, "teacher_lse")
+        gp, gs = self._grad_loss(grad_loss, n, lead)
+        grad, os = self._grad_logits(logits, k, xs, out)
+        loss = torch.empty(lead, dtype=torch.float32, device=self.device)
+        self._run("distill_grad", self._L.distill_grad, (grad_loss, logits, teacher_ids, teacher, teacher_lse, targets, loss, grad), gp, gs, logits.data_ptr(), k, xs,
+                  n, d, *entries, lse, *target, temperature, alpha, loss.data_ptr(), grad.data_ptr(), os)
+        if out is not None:
+            self._written(out)
+        return loss, grad
+
+    # ---- beam search ----
+    def beam_select(self, logits, scores, keep: int | None = None, finished=None, eos_id: int = -1, token_dtype=None):
+        """(scores, parents, tokens, finished) [batch, keep]: the `keep` (as many as there are beams if not given) best of scores + log_softmax(logits) over the beams and the
+        vocabulary of each sequence, in descending order; equal ones: lower beam, larger logit, lower id.
+        logits [batch, beams, vocabulary], scores f32 [batch, beams] (-inf: a beam without candidates, such as all but one in the first step).  A beam with
+        `finished` (bool [batch, beams]) goes on as it is, with eos_id.  parents are int32, tokens int64 (or token_dtype); finished, tokens == eos_id, is None without an
+        eos_id.  Places for which no candidate is left: score -inf, parent 0, token eos_id (0 without one)."""
+        torch = self._torch
+        if logits.dim() != 3:
+            _refuse("logits: [batch, beams, vocabulary] is wanted")
+        k, n, d, xs = self._rows(logits, "logits")
+        batch, beams = logits.shape[:2]
+        if keep is None:
+            keep = beams
+        if k not in _FLOATS or not 1 <= beams <= _MOST_BEAMS or not 1 <= keep <= _MOST_BEAMS:
+            _refuse(f"logits {tuple(logits.shape)} {logits.dtype}, keep {keep}")
+        if not -1 <= eos_id < d:
+            _refuse(f"eos_id {eos_id}")
+        sp, fp = self._of_rows(scores, (batch, beams), "scores"), None
+        if finished is not None:
+            if finished.get_device() != self._index or finished.dtype != torch.bool or finished.shape != (batch, beams) or not finished.is_contiguous() or eos_id < 0:
+                _refuse(f"finished: bool {(batch, beams)} on {self.device}, contiguous, and an eos_id are wanted")
+            fp = finished.data_ptr()
+        tk = self._type.get(token_dtype, 6 if token_dtype is None else -1)
+        if tk != 5 and tk != 6:
+            _refuse(f"token_dtype {token_dtype}")
+        new = lambda dtype: torch.empty((batch, keep), dtype=dtype, device=self.device)  # noqa: E731
+        out, parents, tokens = new(torch.float32), new(torch.int32), new(token_dtype or torch.int64)
+        ended = new(torch.bool) if eos_id >= 0 else None
+        self._run("beam_select", self._L.beam_select, (logits, scores, finished, out, parents, tokens, ended), logits.data_ptr(), k, xs, batch, beams, d, sp, fp,
+                  eos_id, keep, out.data_ptr(), parents.data_ptr(), tokens.data_ptr(), tk, ended.data_ptr() if ended is not None else None)
+        return out, parents, tokens, ended
+
+    def _state(self, t, batch: int, what: str):
+        """(distance of rows, distance of pieces, bytes of a piece, pieces) of a tensor [batch, beams, ...], in bytes.  A row is one piece of neighbouring elements, or pieces at
+        one distance (the heads of a buffer with room for more positions)."""
+        size, shape = t.element_size(), t.shape
+        beams = shape[1]
+        if t.is_contiguous():
+            row = (t.numel() // (batch * beams) if batch else 0) * size
+            return row, row, row, 1
+        stride = t.stride()
+        row = stride[1] if beams > 1 else stride[0] if batch > 1 else 0
+        if batch > 1 and beams > 1 and stride[0] != beams * stride[1]:
+            _refuse(f"{what}: the beams' rows have to be one distance apart")
+        runs = [[1, 1]]                     # [elements or pieces, distance], innermost first
+        for length, st in zip(reversed(shape[2:]), reversed(stride[2:])):
+            if length == 1:
+                continue
+            if st == runs[-1][0] * runs[-1][1]:
+                runs[-1][0] *= length
+            else:
+                runs.append([length, st])
+        if len(runs) > 2:
+            _refuse(f"{what}: a row has to be pieces of neighbouring elements at one distance")
+        piece, (pieces, apart) = runs[0][0], runs[1] if len(runs) == 2 else (1, 0)
+        if pieces == 1:
+            apart = piece
+        span = (pieces - 1) * apart + piece
+        if batch * beams <= 1:
+            row = span
+        if apart < piece or row < span:
+            _refuse(f"{what}: rows overlap")
+        return row * size, apart * size, piece * size, pieces
+
+    def beam_reorder(self, states, parents, out=None):
+        """states[k][b, j] = states[k][b, parents[b, j]] for tensors [batch, beams, ...] of any type, in place; or into the tensors of `out` [batch, keep, ...].  Returns the tensors
+        written.  parents [batch, keep] (int32, int64).  A row (what follows the first two dimensions) is neighbouring elements, or pieces of them at one distance, such as the filled
+        part of a cache [batch, beams, heads, room, dim].  A parent outside [0, beams) raises the sticky error; its row becomes zeros, in place it stays as it was."""
+        states = list(states)
+        pk = self._ids(parents)
+        if parents.dim() != 2 or not states:
+            _refuse("parents: [batch, keep], and states are wanted")
+        batch, keep = parents.shape
+        given = out is not None
+        out = list(out) if given else states
+        if len(out) != len(states):
+            _refuse("out: as many tensors as states are wanted")
+        beams = states[0].shape[1] if states[0].dim() > 1 else 0
+        if not 1 <= beams <= _MOST_BEAMS or not 1 <= keep <= _MOST_BEAMS or (not given and keep != beams):
+            _refuse(f"{beams} beams, {keep} parents")
+        table = array("q")
+        for t, o in zip(states, out):
+            if t.get_device() != self._index or o.get_device() != self._index:
+                _refuse(f"states: tensors on {self.device} are wanted")
+            if t.dim() < 2 or t.shape[:2] != (batch, beams) or o.shape != (batch, keep, *t.shape[2:]) or o.dtype != t.dtype:
+                _refuse(f"states: [{batch}, {beams}, ...] -> [{batch}, {keep}, ...] is wanted")
+            row, apart, piece, pieces = self._state(t, batch, "states")
+            orow, oapart = row, apart
+            if o is not t:
+                orow, oapart, opiece, opieces = self._state(o, batch, "out")
+                if (opiece, opieces) != (piece, pieces):         # the smaller pieces are those of both, if the larger ones hold whole ones of them
+                    if opieces > 1 and pieces > 1 or (opiece * opieces) != (piece * pieces):
+                        _refuse("out: pieces of other sizes than the states'")
+                    if pieces == 1:
+                        piece, pieces, apart = opiece, opieces, opiece
+                    else:
+                        oapart = piece
+            table.extend((t.data_ptr(), o.data_ptr(), row, orow, apart, oapart, piece, pieces if piece else 0))
+        self._run("beam_reorder", self._L.beam_reorder, (states, out, (parents,)), table.buffer_info()[0], len(states), batch, beams, parents.data_ptr(), pk, keep)
+        self._written(out)
+        return out
