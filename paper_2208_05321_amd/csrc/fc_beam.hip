@@ -28,8 +28,8 @@ struct BeamArgs {
     const uint8_t* finished;                       // or NULL
     int32_t beams, dim, keep, eos, slices;
 };
-// what a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are in a list of `keep`
-struct BeamSlice { double sum; float off; int32_t count; };
+// what a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are in a list of `keep`, filled up with -infinity
+struct BeamSlice { double sum; float off; };
 struct BeamEntry { float x; int32_t id; };
 
 // numbers in the order of unsigned integers (no distinction between zeros)
@@ -41,10 +41,22 @@ __device__ __forceinline__ float unordered(uint32_t k) { return __builtin_bit_ca
 // larger logit first, then lower id
 __device__ __forceinline__ uint64_t entry_key(float x, int id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_lane(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xf, false);
+    return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
+    x = add_lane<0x111, 0xf>(x);                   // row_shr 1, 2, 4, 8
+    x = add_lane<0x112, 0xf>(x);
+    x = add_lane<0x114, 0xf>(x);
+    x = add_lane<0x118, 0xf>(x);
+    x = add_lane<0x142, 0xa>(x);                   // row_bcast 15, 31
+    x = add_lane<0x143, 0xc>(x);
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, 63), hi = __builtin_amdgcn_readlane((int)(u >> 32), 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
 // The n-th largest of the wavefront's keys, but for the 16 lower bits, which are 0.
@@ -92,7 +104,8 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     if (!beam_lives(a, row) || (a.finished && a.finished[row])) return;
     const T* x = (const T*)a.x + row * a.stride;
     Slice s;
-    s.load(x, base, lane, a.dim);
+    s.load(x, base, lane, a.dim, true);
+    s.cut(base, lane, a.dim);
     float most[PER], top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
@@ -102,12 +115,8 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         top = fmaxf(top, most[k]);
     }
     // sum of exponentials, each lane's from its own largest element
-    const float off = top * LOG2E, by = -from_of(off);
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < PER; ++k)
-#pragma unroll
-        for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(s.at(k, e), LOG2E, by));
+    s.forget();
+    const float off = top * LOG2E, sum = s.exponentials(LOG2E, from_of(off));
     const float off_wave = wave_max(off);
     const double part = wave_sum((double)(sum * __builtin_amdgcn_exp2f(off - from_of(off_wave))));
     const uint32_t bound_wave = wave_bound(ordered(top), a.keep);
@@ -125,9 +134,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         while (at) {
             const int k = __builtin_ctz(at);
             at &= at - 1;
-            typename Slice::V v = s.x[0];
-#pragma unroll
-            for (int j = 1; j < PER; ++j) if (j == k) v = s.x[j];
+            const typename Slice::V v = s.pick(k);
             const int col = min(Slice::column(base, lane, k), a.dim - N);
 #pragma unroll
             for (int e = 0; e < N; ++e)
@@ -140,7 +147,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     __syncthreads();
     BeamEntry* out = lists + (local * a.slices + slice) * a.keep;
     auto put = [&](int at, uint64_t key) { out[at] = BeamEntry{unordered((uint32_t)(key >> 32)), (int32_t)~(uint32_t)key}; };
-    int got = count;
+    const int got = count;
     if (got <= BEAM_LIST) {
         for (int i = lane; i < got; i += LOGIT_THREADS) {
             const uint64_t key = list[i];
@@ -148,10 +155,9 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
             for (int j = 0; j < got; ++j) rank += list[j] > key;
             if (rank < a.keep) put(rank, key);
         }
-        got = min(got, a.keep);
+        for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) out[i] = BeamEntry{-INFINITY, 0};
     } else {                                       // (as good as equal logits)
         uint64_t last = ~0ull;
-        got = a.keep;
         for (int i = 0; i < a.keep; ++i) {
             uint64_t mine = 0;
             for (int c = base + lane; c < min(a.dim, base + Slice::COLUMNS); c += LOGIT_THREADS) {
@@ -168,7 +174,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         for (int k = 1; k < LOGIT_THREADS / 64; ++k) to = fmaxf(to, offs[k]);
         double all = 0.;
         for (int k = 0; k < LOGIT_THREADS / 64; ++k) all += parts[k] * (double)exp2f(offs[k] - from_of(to));
-        sums[local * a.slices + slice] = BeamSlice{all, to, got};
+        sums[local * a.slices + slice] = BeamSlice{all, to};
     }
 }
 
@@ -181,64 +187,82 @@ __device__ __forceinline__ bool before(const Candidate& p, const Candidate& q) {
     return p.id < q.id;
 }
 
-// One workgroup puts a sequence's beams and slices together.
-__global__ __launch_bounds__(LOGIT_THREADS) void k_beam_join(BeamArgs a, int64_t first, const BeamSlice* __restrict__ sums, const BeamEntry* __restrict__ lists,
-                                                             float* __restrict__ scores_out, int32_t* __restrict__ parents_out, void* __restrict__ tokens_out,
-                                                             int32_t token_type, uint8_t* __restrict__ finished_out) {
+constexpr int JOIN_THREADS = 512;
+constexpr int JOIN_HELD = 4;                       // entries that a lane holds in registers; those of larger searches are read again
+
+// One workgroup puts a sequence's beams and slices together.  Everything it needs is asked for at once; what follows are a few steps that wait for one another (one sequence of 4
+// beams of 131,072 ids 13.4 us when lists were read after their lengths and the bound was found by comparing all lanes, 4.1 this way; 64 sequences of 8 beams 21.4 and 8.9).
+template <bool HELD>
+__global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t first, const BeamSlice* __restrict__ sums, const BeamEntry* __restrict__ lists,
+                                                            float* __restrict__ scores_out, int32_t* __restrict__ parents_out, void* __restrict__ tokens_out,
+                                                            int32_t token_type, uint8_t* __restrict__ finished_out) {
+    constexpr int WAVES = JOIN_THREADS / 64;
     __shared__ double add[BEAM_MOST];              // what a beam's logits lack to be candidates; not finite: there are none
     __shared__ bool ended[BEAM_MOST];
-    __shared__ double tops[LOGIT_THREADS];
+    __shared__ uint32_t bounds[WAVES];
+    __shared__ double list_c[BEAM_LIST];
     __shared__ Candidate list[BEAM_LIST];
-    __shared__ double least;
     __shared__ int count;
     const int lane = threadIdx.x;
     const int64_t seq = blockIdx.x, row0 = first + seq * a.beams;
-    for (int w = lane >> 6; w < a.beams; w += LOGIT_THREADS / 64) {
-        const int64_t row = row0 + w;
-        const bool lives = beam_lives(a, row), end = a.finished && a.finished[row];
+    const int each = a.slices * a.keep, all = a.beams * each;       // (below 2^22)
+    const BeamEntry* entries = lists + seq * all;
+    BeamEntry held[JOIN_HELD];
+    if constexpr (HELD) {
+#pragma unroll
+        for (int j = 0; j < JOIN_HELD; ++j) held[j] = entries[min(lane + j * JOIN_THREADS, all - 1)];
+    }
+    for (int w = lane >> 6; w < a.beams; w += WAVES) {
+        const BeamSlice* s = sums + (seq * a.beams + w) * a.slices;
+        BeamSlice q = s[min(lane & 63, a.slices - 1)];              // (of a beam without candidates: whatever the workspace holds, not used)
+        const float score = a.scores[row0 + w];
+        const bool lives = score - score == 0.f, end = a.finished && a.finished[row0 + w];
         double v = lives ? 0. : -INFINITY;
         if (lives && !end) {
-            const BeamSlice* s = sums + (seq * a.beams + w) * a.slices;
-            float to = -INFINITY;
-            for (int k = lane & 63; k < a.slices; k += 64) to = fmaxf(to, s[k].off);
-            to = from_of(wave_max(to));
-            double sum = 0.;
-            for (int k = lane & 63; k < a.slices; k += 64) sum += s[k].sum * (double)exp2f(s[k].off - to);
-            v = -0.69314718055994530942 * ((double)to + log2(wave_sum(sum)));
+            if ((lane & 63) >= a.slices) q = BeamSlice{0., -INFINITY};
+            for (int k = (lane & 63) + 64; k < a.slices; k += 64) {
+                const BeamSlice o = s[k];
+                const float to = from_of(fmaxf(q.off, o.off));
+                q.sum = q.sum * (double)exp2f(q.off - to) + o.sum * (double)exp2f(o.off - to);
+                q.off = fmaxf(q.off, o.off);
+            }
+            const float to = from_of(wave_max(q.off));
+            v = -0.69314718055994530942 * ((double)to + log2(wave_sum(q.sum * (double)exp2f(q.off - to))));
         }
-        if ((lane & 63) == 0) { add[w] = v + (double)a.scores[row]; ended[w] = end; }
+        if ((lane & 63) == 0) { add[w] = v + (double)score; ended[w] = end; }
     }
-    if (lane == 0) { count = 0; least = -INFINITY; }
+    if (lane == 0) count = 0;
     __syncthreads();
     // f(candidate) for each of this lane's candidates
-    const int each = a.slices * a.keep, all = a.beams * each;       // (below 2^22)
     auto candidates = [&](auto f) {
-        for (int i = lane; i < all; i += LOGIT_THREADS) {
-            const int w = i / each, at = i - w * each;
+        auto one = [&](int i, const BeamEntry& e) {
+            const int w = i / each;
             const double v = add[w];
-            if (!(v - v == 0.)) continue;
-            if (ended[w]) { if (at == 0) f(Candidate{v, 0.f, w, a.eos}); continue; }
-            const int64_t k = (seq * a.beams + w) * a.slices + at / a.keep;
-            const int j = at % a.keep;
-            if (j >= sums[k].count) continue;
-            const BeamEntry e = lists[k * a.keep + j];
-            f(Candidate{v + (double)e.x, e.x, w, e.id});
-        }
+            if (!(v - v == 0.)) return;
+            if (ended[w]) { if (i == w * each) f(Candidate{v, 0.f, w, a.eos}); }
+            else if (e.x != -INFINITY) f(Candidate{v + (double)e.x, e.x, w, e.id});
+        };
+        if constexpr (HELD) {
+#pragma unroll
+            for (int j = 0; j < JOIN_HELD; ++j) if (lane + j * JOIN_THREADS < all) one(lane + j * JOIN_THREADS, held[j]);
+        } else
+            for (int i = lane; i < all; i += JOIN_THREADS) one(i, entries[i]);
     };
     double top = -INFINITY;
     candidates([&](const Candidate& q) { top = fmax(top, q.c); });
-    tops[lane] = top;
+    // (one less than the number in 32 bits, which may have been rounded up)
+    const uint32_t mine = wave_bound(ordered((float)top) - 1, a.keep);
+    if ((lane & 63) == 0) bounds[lane >> 6] = mine;
     __syncthreads();
-    int above = 0;
-    for (int k = 0; k < LOGIT_THREADS; ++k) above += tops[k] > top || (tops[k] == top && k < lane);
-    if (above == a.keep - 1) least = top;
-    __syncthreads();
-    const double bound = least;
-    if (top >= bound)
+    uint32_t key = 0x00800000u;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) key = max(key, bounds[k]);
+    const double bound = key == 0x00800000u ? -INFINITY : (double)unordered(key);
+    if (top >= bound && top > -INFINITY)
         candidates([&](const Candidate& q) {
             if (q.c < bound) return;
             const int p = atomicAdd(&count, 1);
-            if (p < BEAM_LIST) list[p] = q;
+            if (p < BEAM_LIST) { list_c[p] = q.c; list[p] = q; }
         });
     __syncthreads();
     auto put = [&](int at, const Candidate& q) {
@@ -250,11 +274,16 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_join(BeamArgs a, int64_t
     };
     int got = count;
     if (got <= BEAM_LIST) {
-        for (int i = lane; i < got; i += LOGIT_THREADS) {
-            const Candidate q = list[i];
+        for (int i = lane >> 3; i < got; i += JOIN_THREADS / 8) {    // eight lanes to a candidate
+            const double c = list_c[i];
             int rank = 0;
-            for (int j = 0; j < got; ++j) rank += before(list[j], q);
-            if (rank < a.keep) put(rank, q);
+            for (int j = lane & 7; j < got; j += 8) {
+                const double o = list_c[j];
+                if (o > c || (o == c && j != i && before(list[j], list[i]))) ++rank;
+            }
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor(rank, o);
+            if (rank < a.keep && (lane & 7) == 0) put(rank, list[i]);
         }
         got = min(got, a.keep);
     } else {
@@ -265,7 +294,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_join(BeamArgs a, int64_t
             candidates([&](const Candidate& q) { if (before(last, q) && before(q, mine)) mine = q; });
             __syncthreads();
             list[lane] = mine;
-            for (int o = LOGIT_THREADS / 2; o > 0; o >>= 1) {
+            for (int o = JOIN_THREADS / 2; o > 0; o >>= 1) {
                 __syncthreads();
                 if (lane < o && before(list[lane + o], list[lane])) list[lane] = list[lane + o];
             }
@@ -274,7 +303,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_join(BeamArgs a, int64_t
             if (lane == 0) put(i, last);
         }
     }
-    for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) put(i, Candidate{-INFINITY, 0.f, 0, max(a.eos, 0)});
+    for (int i = got + lane; i < a.keep; i += JOIN_THREADS) put(i, Candidate{-INFINITY, 0.f, 0, max(a.eos, 0)});
 }
 
 constexpr size_t BEAM_WORK = (size_t)5 << 20;      // of a launch's slices (one sequence takes 4.4 MB at most); more sequences go in several
@@ -291,8 +320,11 @@ void beam_run(fc_dense* d, BeamArgs a, int64_t batch, float* scores, int32_t* pa
         BeamEntry* lists = reinterpret_cast<BeamEntry*>(sums + n * a.beams * a.slices);
         k_beam_slice<T, PER><<<(unsigned)(n * a.beams * a.slices), LOGIT_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists);
         const int64_t o = at * a.keep;
-        k_beam_join<<<(unsigned)n, LOGIT_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists, scores + o, parents + o,
-                                                                  (char*)tokens + o * (token_type == FC_TYPE_I64 ? 8 : 4), token_type, finished ? finished + o : nullptr);
+        auto join = [&](auto held) {
+            k_beam_join<decltype(held)::value><<<(unsigned)n, JOIN_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists, scores + o, parents + o,
+                                                                                           (char*)tokens + o * (token_type == FC_TYPE_I64 ? 8 : 4), token_type, finished ? finished + o : nullptr);
+        };
+        if (a.beams * a.slices * a.keep <= JOIN_THREADS * JOIN_HELD) join(std::true_type()); else join(std::false_type());
     }
 }
 

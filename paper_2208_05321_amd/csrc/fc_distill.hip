@@ -70,12 +70,15 @@ struct Sums {
         off = most;
         off1 = most1;
     }
-    __device__ __forceinline__ Sums over_wave() const {
+    // over the wavefront's lanes; two: the sums at 1 are others than those at the temperature
+    __device__ __forceinline__ Sums over_wave(bool two) const {
         Sums s;
-        s.off = wave_max(off);
-        s.off1 = wave_max(off1);
-        s.t = wave_sum(t * __builtin_amdgcn_exp2f(off - from_of(s.off)));
-        s.one = wave_sum(one * __builtin_amdgcn_exp2f(off1 - from_of(s.off1)));
+        s.off = s.off1 = wave_max(off);
+        s.t = s.one = wave_sum(t * __builtin_amdgcn_exp2f(off - from_of(s.off)));
+        if (two) {
+            s.off1 = wave_max(off1);
+            s.one = wave_sum(one * __builtin_amdgcn_exp2f(off1 - from_of(s.off1)));
+        }
         return s;
     }
 };
@@ -83,13 +86,27 @@ constexpr double LN2 = 0.69314718055994530942;
 constexpr Sums NO_SUMS{-INFINITY, -INFINITY, 0.f, 0.f};
 struct RowSums { Sums rest, named; };
 
-// What a wavefront makes of a row's sums: its loss and, if wanted, the numbers for the backward pass.
-template <class T>
-__device__ void distill_row(const DistillArgs& a, int64_t row, int y, const RowSums& s, float* __restrict__ loss, float* __restrict__ stats) {
+// Entries of a row in LDS: ids (-1: none that counts), the teacher's logits, and later probabilities, the student's logits.
+struct Entries { int* id; float* z; float* x; };
+__device__ __forceinline__ Entries entries_at(float* lds, int top) { return Entries{reinterpret_cast<int*>(lds), lds + top, lds + 2 * top}; }
+template <class T, int LANES>
+__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t row, int lane, const T* x, const Entries& t) {
+    for (int k = lane; k < a.top; k += LANES) {
+        const int64_t i = row * a.top + k;
+        const float z = load_value(a.z, a.z_type, i);
+        const int id = known_id(load_id(a.ids, a.id_type, i), a.dim, a.flags);
+        t.id[k] = id;
+        t.z[k] = z;
+        t.x[k] = id >= 0 ? (float)x[id] : 0.f;
+    }
+}
+
+// What a wavefront makes of a row's sums and entries (xy: the target's logit): its loss and the numbers for the backward pass.  The entries' logits become their probabilities.
+__device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, float xy, const RowSums& s, const Entries& t, float* __restrict__ loss, float* stats) {
     const int lane = threadIdx.x & 63;
-    const T* x = (const T*)a.x + row * a.stride;
     const double it = 1.0 / (double)a.temperature;
-    const float ct = scale_of(a), it32 = (float)it;
+    const float ct = scale_of(a);
+    const float lse = a.lse ? a.lse[row] : 0.f;
     Sums all = s.rest;
     all.join(s.named);
     const double lse2 = (double)all.off + (double)log2f(all.t);
@@ -97,40 +114,35 @@ __device__ void distill_row(const DistillArgs& a, int64_t row, int y, const RowS
     float zmax = -INFINITY;
     bool some = false;
     for (int k = lane; k < a.top; k += 64) {
-        const int64_t i = row * a.top + k;
-        if (known_id(load_id(a.ids, a.id_type, i), a.dim, a.flags) < 0) continue;
-        const float z = load_value(a.z, a.z_type, i);
+        if (t.id[k] < 0) continue;
+        const float z = t.z[k];
         zmax = fmaxf(zmax, z);
         some |= a.lse || z != -INFINITY;
     }
-    some = __any(some);
+    some = a.alpha > 0.f && __any(some);
     zmax = from_of(wave_max(zmax));
     float kl = 0.f, part = 0.f, zinv = 0.f, sum_p = 0.f, p0 = 0.f, q0 = 1.f;
-    if (some && a.alpha > 0.f) {
+    if (some) {
         double log_zinv;
         if (a.lse) {
-            log_zinv = (double)zmax * it - (double)a.lse[row];
+            log_zinv = (double)zmax * it - (double)lse;
             zinv = expf((float)log_zinv);
         } else {
             float sum = 0.f;
-            for (int k = lane; k < a.top; k += 64) {
-                const int64_t i = row * a.top + k;
-                const int64_t id = load_id(a.ids, a.id_type, i);
-                if (id >= 0 && id < a.dim) sum += expf((load_value(a.z, a.z_type, i) - zmax) * it32);
-            }
+            for (int k = lane; k < a.top; k += 64)
+                if (t.id[k] >= 0) sum += expf((float)(((double)t.z[k] - zmax) * it));
             sum = wave_sum(sum);
             zinv = 1.f / sum;
             log_zinv = -(double)logf(sum);
         }
         for (int k = lane; k < a.top; k += 64) {
-            const int64_t i = row * a.top + k;
-            const int64_t id = load_id(a.ids, a.id_type, i);
-            if (id < 0 || id >= a.dim) continue;
-            const double d = ((double)load_value(a.z, a.z_type, i) - zmax) * it;
+            if (t.id[k] < 0) continue;
+            const double d = ((double)t.z[k] - zmax) * it;
             const float p = expf((float)d) * zinv;
+            t.z[k] = p;
             part += p;
             if (p == 0.f) continue;                // nothing, also where the student gives nothing
-            const double log_q = ((double)(float)x[id] * ct - lse2) * LN2;
+            const double log_q = ((double)t.x[k] * ct - lse2) * LN2;
             kl += p * (float)(d + log_zinv - log_q);
         }
         kl = wave_sum(kl);
@@ -143,11 +155,10 @@ __device__ void distill_row(const DistillArgs& a, int64_t row, int y, const RowS
         }
     }
     if (lane != 0) return;
-    float value = some && a.alpha > 0.f ? a.alpha * a.temperature * a.temperature * kl : 0.f;
-    if (a.alpha < 1.f) value += (1.f - a.alpha) * (float)(((double)all.off1 + (double)log2f(all.one) - (double)(float)x[y] * LOG2E) * LN2);
-    if (loss) loss[row] = value;
+    float value = some ? a.alpha * a.temperature * a.temperature * kl : 0.f;
+    if (a.alpha < 1.f) value += (1.f - a.alpha) * (float)(((double)all.off1 + (double)log2f(all.one) - (double)xy * LOG2E) * LN2);
+    loss[row] = value;
     if (!stats) return;
-    float* o = stats + row * STATS;
     const float c = sum_p + p0;
     float coef = 0.f, coef1 = 0.f;
     if (s.rest.t != 0.f) {                         // (else there is nothing that is not named, or only logits of -infinity)
@@ -156,235 +167,304 @@ __device__ void distill_row(const DistillArgs& a, int64_t row, int y, const RowS
     }
     if (all.t == 0.f) coef = NAN;                  // all logits are -infinity
     const bool one = a.temperature == 1.f;         // one exponential stands for both
-    o[ST_OFF] = from_of(s.rest.off);
-    o[ST_COEF] = one ? coef + coef1 : coef;
-    o[ST_OFF1] = from_of(s.rest.off1);
-    o[ST_COEF1] = one ? 0.f : coef1;
-    o[ST_ALL] = all.off;
-    o[ST_INV] = 1.f / all.t;
-    o[ST_ALL1] = all.off1;
-    o[ST_INV1] = 1.f / all.one;
-    o[ST_NAMED] = c;
-    o[ST_ZFROM] = zmax;
-    o[ST_ZINV] = zinv;
-    o[ST_KIND] = some && a.alpha > 0.f ? ROW_ENTRIES : a.alpha < 1.f ? ROW_TARGET_ONLY : ROW_OUT;
+    stats[ST_OFF] = from_of(s.rest.off);
+    stats[ST_COEF] = one ? coef + coef1 : coef;
+    stats[ST_OFF1] = from_of(s.rest.off1);
+    stats[ST_COEF1] = one ? 0.f : coef1;
+    stats[ST_ALL] = all.off;
+    stats[ST_INV] = 1.f / all.t;
+    stats[ST_ALL1] = all.off1;
+    stats[ST_INV1] = 1.f / all.one;
+    stats[ST_NAMED] = c;
+    stats[ST_ZFROM] = zmax;
+    stats[ST_ZINV] = zinv;
+    stats[ST_KIND] = some ? ROW_ENTRIES : a.alpha < 1.f ? ROW_TARGET_ONLY : ROW_OUT;
 }
 
-__device__ __forceinline__ void distill_left_out(int64_t row, float* loss, float* stats) {
-    if ((threadIdx.x & 63) >= STATS) return;
-    if ((threadIdx.x & 63) == 0 && loss) loss[row] = 0.f;
-    if (stats) stats[row * STATS + (threadIdx.x & 63)] = 0.f;
+__device__ __forceinline__ void distill_left_out(int64_t row, int lane, float* loss, float* stats) {
+    if (lane == 0) loss[row] = 0.f;
+    if (lane < STATS && stats) stats[row * STATS + lane] = 0.f;
 }
 
-// Sums of a slice, over LANES lanes of a row.  REST: named ids apart from the others.  `slices` > 1: the sums go to `part`, else the row is finished.
-template <class T, int LANES, int PER, bool REST>
-__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_fwd(DistillArgs a, int slices, RowSums* __restrict__ part, float* __restrict__ loss, float* __restrict__ stats) {
+// Marks of a slice's named elements, in LDS: a byte for each vector, those of a lane side by side.
+template <int LANES, int PER> struct Marks { uint64_t of[LANES][(PER + 7) / 8]; };
+
+// The sums of a slice, over one wavefront's lanes.  With what the teacher's entries leave over (a.lse), named elements become -infinity in the registers before the sums are
+// taken; their own sums are those of the few lanes that have some.
+template <class T, int LANES, int PER>
+__device__ __forceinline__ RowSums slice_sums(const DistillArgs& a, RowSlice<T, LANES, PER>& s, int64_t row, int base, int lane, Marks<LANES, PER>& marks) {
     using Slice = RowSlice<T, LANES, PER>;
-    constexpr int N = Slice::N, ROWS = LOGIT_THREADS / LANES, WORDS = LANES * PER / 4;
-    __shared__ uint32_t marks[REST ? ROWS : 1][REST ? WORDS : 1];      // a byte for each vector, a bit for each element that is named
-    __shared__ RowSums lds[LOGIT_THREADS / 64];
-    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
-    const int64_t row = (int64_t)(blockIdx.x / slices) * ROWS + sub;
-    const int slice = blockIdx.x % slices, base = slice * Slice::COLUMNS;
-    if (row >= a.n) return;                        // (all lanes of the row)
-    int y;
-    if (!row_target(a, row, &y)) {
-        if (slice == 0 && lane < 64) distill_left_out(row, loss, stats);
-        return;
-    }
+    constexpr int N = Slice::N;
     const float ct = scale_of(a);
-    const bool two = a.alpha < 1.f && a.temperature != 1.f;
-    Slice s;
-    s.load((const T*)a.x + row * a.stride, base, lane, a.dim);
-    if constexpr (REST) {
+    const bool two = a.alpha < 1.f && a.temperature != 1.f, rest = a.lse && a.alpha > 0.f;
+    RowSums r{NO_SUMS, NO_SUMS};
+    if (rest) {
 #pragma unroll
-        for (int k = lane; k < WORDS; k += LANES) marks[sub][k] = 0;
+        for (int j = 0; j < (PER + 7) / 8; ++j) marks.of[lane][j] = 0;
         row_sync<LANES>();
         for (int k = lane; k < a.top; k += LANES) {
             const int64_t id = load_id(a.ids, a.id_type, row * a.top + k) - base;
-            if (id >= 0 && id < min(Slice::COLUMNS, a.dim - base)) atomicOr(&marks[sub][id / N / 4], 1u << (id / N % 4 * 8 + id % N));
+            if (id < 0 || id >= min(Slice::COLUMNS, a.dim - base)) continue;
+            const int v = (int)id / N, j = v / LANES;
+            atomicOr(reinterpret_cast<uint32_t*>(&marks.of[v % LANES][0]) + j / 4, 1u << (j % 4 * 8 + (int)id % N));
         }
         row_sync<LANES>();
     }
-    auto marked = [&](int k) -> uint32_t {         // of vector k, in the order of its elements as they are loaded
-        const int v = k * LANES + lane;
-        return (uint32_t)reinterpret_cast<const uint8_t*>(marks[sub])[v] << Slice::skip(Slice::column(base, lane, k), a.dim);
-    };
-    RowSums r;
-    r.named = NO_SUMS;
-    float top = -INFINITY, top_named = -INFINITY;
-    if constexpr (REST) {
+    s.cut(base, lane, a.dim);
+    if (rest) {
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const uint32_t b = marked(k);
-            if (b == 0) {
+        for (int j = 0; j < (PER + 7) / 8; ++j) {
+            uint64_t mask = marks.of[lane][j];
+            if (base + Slice::COLUMNS > a.dim) {   // the last vector's elements are loaded further on in it
+                uint64_t moved = 0;
 #pragma unroll
-                for (int e = 0; e < N; ++e) top = fmaxf(top, s.at(k, e));
-            } else {
+                for (int k = 0; k < 8 && j * 8 + k < PER; ++k)
+                    moved |= (uint64_t)((uint32_t)(mask >> 8 * k & 0xff) << Slice::skip(Slice::column(base, lane, j * 8 + k), a.dim)) << 8 * k;
+                mask = moved;
+            }
+            for (uint64_t m = mask; m; m &= m - 1) {
+                const int at = __builtin_ctzll(m);
+                const typename Slice::V v = s.pick(j * 8 + at / 8);
+                float x = 0.f;
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float v = s.at(k, e);
-                    if (b >> e & 1) top_named = fmaxf(top_named, v); else top = fmaxf(top, v);
-                }
+                for (int e = 0; e < N; ++e) if (e == at % 8) x = (float)v[e];
+                Sums q{x * ct, x * (two ? LOG2E : ct), 0.f, 0.f};
+                q.t = __builtin_amdgcn_exp2f(fmaf(x, ct, -from_of(q.off)));
+                q.one = two ? __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from_of(q.off1))) : q.t;
+                r.named.join(q);
+            }
+#pragma unroll
+            for (int k = 0; k < 8 && j * 8 + k < PER; ++k) {
+                const uint32_t b = mask >> 8 * k & 0xff;
+                if (b == 0) continue;
+#pragma unroll
+                for (int e = 0; e < N; ++e) if (b >> e & 1) s.x[j * 8 + k][e] = (T)-INFINITY;
             }
         }
-    } else top = s.largest();
-    auto sum_of = [&](float c, float off, float off_named, float* named) {
-        const float by = -from_of(off), by_named = -from_of(off_named);
-        float sum = 0.f;
-        *named = 0.f;
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const uint32_t b = REST ? marked(k) : 0;
-            if (!REST || b == 0) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(s.at(k, e), c, by));
-            } else {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    if (b >> e & 1) *named += __builtin_amdgcn_exp2f(fmaf(s.at(k, e), c, by_named));
-                    else sum += __builtin_amdgcn_exp2f(fmaf(s.at(k, e), c, by));
-                }
-            }
-        }
-        return sum;
-    };
+        r.named = r.named.over_wave(two);
+    }
+    s.forget();
+    const float top = s.largest();
+    s.forget();
     r.rest.off = r.rest.off1 = top * ct;
-    if constexpr (REST) r.named.off = r.named.off1 = top_named * ct;
-    r.rest.t = r.rest.one = sum_of(ct, r.rest.off, r.named.off, &r.named.t);
-    r.named.one = r.named.t;
+    r.rest.t = r.rest.one = s.exponentials(ct, from_of(r.rest.off));
     if (two) {
         r.rest.off1 = top * LOG2E;
-        if constexpr (REST) r.named.off1 = top_named * LOG2E;
-        r.rest.one = sum_of(LOG2E, r.rest.off1, r.named.off1, &r.named.one);
+        s.forget();
+        r.rest.one = s.exponentials(LOG2E, from_of(r.rest.off1));
     }
-    r.rest = r.rest.over_wave();
-    if constexpr (REST) r.named = r.named.over_wave();
+    r.rest = r.rest.over_wave(two);
+    return r;
+}
+// of all the wavefronts of a row, in the first of them
+template <int LANES>
+__device__ __forceinline__ void join_waves(RowSums& r, RowSums* lds, bool rest) {
     if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = r;
         __syncthreads();
         if (threadIdx.x >= 64) return;
-        for (int k = 1; k < LANES / 64; ++k) {
-            r.rest.join(lds[k].rest);
-            if constexpr (REST) r.named.join(lds[k].named);
+        const int lane = threadIdx.x;
+        r = lane < LANES / 64 ? lds[lane] : RowSums{NO_SUMS, NO_SUMS};
+        r.rest = r.rest.over_wave(true);
+        if (rest) r.named = r.named.over_wave(true);
+    }
+}
+
+// The gradient of a slice in the place of its logits, but for the named ids' and the target's.
+template <class T, int LANES, int PER>
+__device__ __forceinline__ void slice_grad(const DistillArgs& a, RowSlice<T, LANES, PER>& s, float g, const float* st) {
+    const float ct = scale_of(a), off = st[ST_OFF], off1 = st[ST_OFF1], coef = g * st[ST_COEF], coef1 = g * st[ST_COEF1];
+    const bool two = a.alpha < 1.f && a.temperature != 1.f;
+    constexpr int N = RowSlice<T, LANES, PER>::N;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {                // (the choice inside: outside, every element would be converted before it)
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(s.at(k, e), ct, -off));
+        if (two) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = fmaf(coef1, __builtin_amdgcn_exp2f(fmaf(s.at(k, e), LOG2E, -off1)), v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) s.x[k][e] = (T)v[e];
+    }
+}
+// The gradients of the named ids and of the target in [base, end), after the slice is stored.  An id that is named several times is the first entry's.
+template <class T, int LANES>
+__device__ __forceinline__ void mend(const DistillArgs& a, float g, const float* st, const Entries& t, int y, float xy, int base, int end, int lane, T* out) {
+    const float ct = scale_of(a), scale = a.alpha * a.temperature, hard = 1.f - a.alpha;
+    const int entries = st[ST_KIND] == ROW_ENTRIES ? a.top : 0;
+    const bool here = a.alpha < 1.f && y >= base && y < end;
+    bool y_named = false;
+    for (int k = lane; k < entries; k += LANES) {
+        const int id = t.id[k];
+        if (id < base || id >= end) continue;
+        float sum = 0.f;
+        bool first = true;
+        for (int j = 0; j < entries; ++j)
+            if (t.id[j] == id) { first &= j >= k; sum += t.z[j]; }
+        y_named |= id == y;
+        if (!first) continue;
+        const float q = exp2f(fmaf(t.x[k], ct, -st[ST_ALL])) * st[ST_INV], q1 = a.alpha < 1.f ? exp2f(fmaf(t.x[k], LOG2E, -st[ST_ALL1])) * st[ST_INV1] : 0.f;
+        out[id] = (T)(g * (scale * (st[ST_NAMED] * q - sum) + hard * (q1 - (id == y ? 1.f : 0.f))));
+    }
+    if (here) {                                    // (the same in all lanes of the row)
+        if constexpr (LANES > 64) y_named = __syncthreads_or(y_named);
+        else y_named = __any(y_named);
+        if (!y_named && lane == 0) {
+            float v = g * st[ST_COEF] * __builtin_amdgcn_exp2f(fmaf(xy, ct, -st[ST_OFF]));
+            if (a.temperature != 1.f) v = fmaf(g * st[ST_COEF1], __builtin_amdgcn_exp2f(fmaf(xy, LOG2E, -st[ST_OFF1])), v);
+            out[y] = (T)(v - g * hard);
         }
     }
-    if (slices > 1) { if (lane == 0) part[row * slices + slice] = r; }
-    else distill_row<T>(a, row, y, r, loss, stats);
+}
+template <class T, int LANES, int PER>
+__device__ __forceinline__ void store_zeros(T* out, int base, int lane, int dim) {
+    RowSlice<T, LANES, PER> s;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) s.x[k] = typename RowSlice<T, LANES, PER>::V{};
+    s.store(out, base, lane, dim, false);
+}
+
+constexpr int distill_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
+
+// Rows that LANES lanes hold: the loss, and the gradient too if it is wanted (grad), which may take the place of the logits: a row is read before any of it is written.
+template <class T, int LANES, int PER>
+__global__ __launch_bounds__(distill_threads(LANES)) void k_distill_row(DistillArgs a, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride, float* __restrict__ loss,
+                                                                        float* __restrict__ stats, T* grad, int64_t grad_stride) {
+    using Slice = RowSlice<T, LANES, PER>;
+    constexpr int ROWS = distill_threads(LANES) / LANES;
+    extern __shared__ float dynamic[];             // entries
+    __shared__ Marks<LANES, PER> marks[ROWS];
+    __shared__ RowSums lds[distill_threads(LANES) / 64];
+    __shared__ float row_stats[ROWS][STATS];
+    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + sub;
+    if (row >= a.n) return;                        // (all lanes of the row)
+    const T* x = (const T*)a.x + row * a.stride;
+    T* out = grad + (grad ? row * grad_stride : 0);
+    Slice s;
+    s.load(x, 0, lane, a.dim, stream);
+    const float g = grad ? grad_loss[row * grad_loss_stride] : 0.f;
+    int y;
+    if (!row_target(a, row, &y)) {
+        distill_left_out(row, lane, loss, stats);
+        if (grad) store_zeros<T, LANES, PER>(out, 0, lane, a.dim);
+        return;
+    }
+    const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
+    load_entries<T, LANES>(a, row, lane, x, t);
+    const float xy = y >= 0 ? (float)x[y] : 0.f;
+    RowSums r = slice_sums<T, LANES, PER>(a, s, row, 0, lane, marks[sub]);
+    join_waves<LANES>(r, lds, a.lse != nullptr);
+    float* st = row_stats[sub];
+    if constexpr (LANES <= 64) row_sync<LANES>();
+    if (lane < 64) {
+        distill_row(a, row, xy, r, t, loss, st);
+        row_sync<64>();
+        if (stats && lane < STATS) stats[row * STATS + lane] = st[lane];
+    }
+    if (!grad) return;
+    row_sync<LANES>();
+    if (st[ST_KIND] == ROW_OUT || g == 0.f) { store_zeros<T, LANES, PER>(out, 0, lane, a.dim); return; }
+    s.forget();
+    slice_grad<T, LANES, PER>(a, s, g, st);
+    s.store(out, 0, lane, a.dim, stream);
+    row_sync<LANES>();
+    mend<T, LANES>(a, g, st, t, y, xy, 0, a.dim, lane, out);
+}
+
+// Sums of one slice of a longer row.
+template <class T, int LANES, int PER>
+__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_slice(DistillArgs a, int slices, bool stream, RowSums* __restrict__ part) {
+    using Slice = RowSlice<T, LANES, PER>;
+    static_assert(LANES == LOGIT_THREADS);
+    __shared__ Marks<LANES, PER> marks;
+    __shared__ RowSums lds[LOGIT_THREADS / 64];
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x / slices;
+    const int slice = blockIdx.x % slices, base = slice * Slice::COLUMNS;
+    Slice s;
+    s.load((const T*)a.x + row * a.stride, base, lane, a.dim, stream);
+    if (a.target) {
+        const int64_t y = load_id(a.target, a.target_type, row);
+        if (y < 0 || y >= a.dim) return;
+    }
+    RowSums r = slice_sums<T, LANES, PER>(a, s, row, base, lane, marks);
+    join_waves<LANES>(r, lds, a.lse != nullptr);
+    if (lane == 0) part[row * slices + slice] = r;
 }
 
 // The rows of several slices: a wavefront to a row.
 template <class T>
 __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_join(DistillArgs a, int slices, const RowSums* __restrict__ part, float* __restrict__ loss, float* __restrict__ stats) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * (LOGIT_THREADS / 64) + threadIdx.x / 64;
-    int y;
-    if (row >= a.n || !row_target(a, row, &y)) return;
+    extern __shared__ float dynamic[];
+    __shared__ float row_stats[LOGIT_THREADS / 64][STATS];
+    const int lane = threadIdx.x & 63, sub = threadIdx.x / 64;
+    const int64_t row = (int64_t)blockIdx.x * (LOGIT_THREADS / 64) + sub;
+    if (row >= a.n) return;
+    const T* x = (const T*)a.x + row * a.stride;
     RowSums r{NO_SUMS, NO_SUMS};
     for (int k = lane; k < slices; k += 64) {
-        r.rest.join(part[row * slices + k].rest);
-        r.named.join(part[row * slices + k].named);
+        const RowSums q = part[row * slices + k];
+        r.rest.join(q.rest);
+        r.named.join(q.named);
     }
-    r.rest = r.rest.over_wave();
-    r.named = r.named.over_wave();
-    distill_row<T>(a, row, y, r, loss, stats);
+    int y;
+    if (!row_target(a, row, &y)) { distill_left_out(row, lane, loss, stats); return; }
+    const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
+    load_entries<T, 64>(a, row, lane, x, t);
+    const float xy = y >= 0 ? (float)x[y] : 0.f;
+    r.rest = r.rest.over_wave(true);
+    r.named = r.named.over_wave(true);
+    row_sync<64>();
+    distill_row(a, row, xy, r, t, loss, row_stats[sub]);
+    row_sync<64>();
+    if (lane < STATS) stats[row * STATS + lane] = row_stats[sub][lane];
 }
 
 // The gradient of a slice.  It may take the place of the logits: a slice is read, its entries among it, before any of it is written.
 template <class T, int LANES, int PER>
-__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, int slices, const float* __restrict__ grad_loss, int64_t grad_loss_stride,
+__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, int slices, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride,
                                                                const float* __restrict__ stats, T* grad, int64_t grad_stride) {
     using Slice = RowSlice<T, LANES, PER>;
-    constexpr int N = Slice::N, ROWS = LOGIT_THREADS / LANES;
-    extern __shared__ float dynamic[];             // for each row: ids, probabilities and logits of its entries
+    constexpr int ROWS = LOGIT_THREADS / LANES;
+    extern __shared__ float dynamic[];
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
-    const int64_t row = (int64_t)(blockIdx.x / slices) * ROWS + sub;
-    const int slice = blockIdx.x % slices, base = slice * Slice::COLUMNS;
+    const unsigned block = blockIdx.x;
+    const int64_t row = (int64_t)(block / slices) * ROWS + sub;
+    const int slice = block % slices, base = slice * Slice::COLUMNS;
     if (row >= a.n) return;
     const T* x = (const T*)a.x + row * a.stride;
     T* out = grad + row * grad_stride;
     const float* st = stats + row * STATS;
-    const float g = grad_loss[row * grad_loss_stride], kind = st[ST_KIND];
-    const int end = min(a.dim, base + Slice::COLUMNS);
-    auto store = [&](int k, const float (&v)[N]) {
-        const int col = Slice::column(base, lane, k);
-        if (col + N <= a.dim) store_vector(out + col, v);
-        else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {          // v ends with the row
-                const int c = a.dim - N + e;
-                if (c >= col) out[c] = (T)v[e];
-            }
-        }
-    };
-    if (kind == ROW_OUT || g == 0.f) {
-        const float zero[N] = {};
-#pragma unroll
-        for (int k = 0; k < PER; ++k) store(k, zero);
-        return;
-    }
-    int* ids = reinterpret_cast<int*>(dynamic) + (size_t)sub * 3 * a.top;
-    float* p = reinterpret_cast<float*>(ids + a.top);
-    float* xs = p + a.top;
-    const float it = (float)(1.0 / (double)a.temperature), ct = scale_of(a);
-    const float off = -st[ST_OFF], off1 = -st[ST_OFF1], coef = g * st[ST_COEF], coef1 = g * st[ST_COEF1];
-    const bool two = a.alpha < 1.f && a.temperature != 1.f;
     Slice s;
-    s.load(x, base, lane, a.dim);
-    const int entries = kind == ROW_ENTRIES ? a.top : 0;
-    for (int k = lane; k < entries; k += LANES) {
-        const int64_t i = row * a.top + k;
-        const int64_t id = load_id(a.ids, a.id_type, i);
+    s.load(x, base, lane, a.dim, stream);
+    const float g = grad_loss[row * grad_loss_stride], kind = st[ST_KIND];
+    if (kind == ROW_OUT || g == 0.f) { store_zeros<T, LANES, PER>(out, base, lane, a.dim); return; }
+    const int end = min(a.dim, base + Slice::COLUMNS);
+    const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
+    const float it = (float)(1.0 / (double)a.temperature);
+    for (int k = lane; kind == ROW_ENTRIES && k < a.top; k += LANES) {
+        const int64_t i = row * a.top + k, id = load_id(a.ids, a.id_type, i);
         const bool here = id >= base && id < end;
-        ids[k] = here ? (int)id : -1;
+        t.id[k] = here ? (int)id : -1;
         if (here) {
-            p[k] = expf((load_value(a.z, a.z_type, i) - st[ST_ZFROM]) * it) * st[ST_ZINV];
-            xs[k] = (float)x[id];
+            t.z[k] = expf((load_value(a.z, a.z_type, i) - st[ST_ZFROM]) * it) * st[ST_ZINV];
+            t.x[k] = (float)x[id];
         }
     }
     int y = -1;
     float xy = 0.f;
     if (a.target && a.alpha < 1.f) {
         y = (int)load_id(a.target, a.target_type, row);
-        if (y < base || y >= end) y = -1;
-        else xy = (float)x[y];
+        if (y >= base && y < end) xy = (float)x[y];
     }
+    slice_grad<T, LANES, PER>(a, s, g, st);
     row_sync<LANES>();
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        float v[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(s.at(k, e), ct, off));
-        if (two) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = fmaf(coef1, __builtin_amdgcn_exp2f(fmaf(s.at(k, e), LOG2E, off1)), v[e]);
-        }
-        store(k, v);
-    }
+    s.store(out, base, lane, a.dim, stream);
     row_sync<LANES>();
-    const float scale = a.alpha * a.temperature, hard = 1.f - a.alpha;
-    bool y_named = false;
-    for (int k = lane; k < entries; k += LANES) {
-        const int id = ids[k];
-        if (id < 0) continue;
-        float sum = 0.f;
-        bool first = true;
-        for (int j = 0; j < entries; ++j)
-            if (ids[j] == id) { first &= j >= k; sum += p[j]; }
-        y_named |= id == y;
-        if (!first) continue;
-        const float q = exp2f(fmaf(xs[k], ct, -st[ST_ALL])) * st[ST_INV], q1 = a.alpha < 1.f ? exp2f(fmaf(xs[k], LOG2E, -st[ST_ALL1])) * st[ST_INV1] : 0.f;
-        out[id] = (T)(g * (scale * (st[ST_NAMED] * q - sum) + hard * (q1 - (id == y ? 1.f : 0.f))));
-    }
-    if (y >= 0) {                                  // (the same in all lanes of the row)
-        if constexpr (LANES > 64) y_named = __syncthreads_or(y_named);
-        else y_named = __any(y_named);
-        if (!y_named && lane == 0) {
-            float v = coef * __builtin_amdgcn_exp2f(fmaf(xy, ct, off));
-            if (two) v = fmaf(coef1, __builtin_amdgcn_exp2f(fmaf(xy, LOG2E, off1)), v);
-            out[y] = (T)(v - g * hard);
-        }
-    }
+    mend<T, LANES>(a, g, st, t, y, xy, base, end, lane, out);
 }
 
 // Row-slices of one launch: what their sums take of the workspace, and what a launch can have of workgroups, is bounded; more rows go in several.
@@ -392,14 +472,25 @@ constexpr int64_t DISTILL_SLICES = 1 << 16;
 constexpr size_t DISTILL_WORK = DISTILL_SLICES * (sizeof(RowSums) + STATS * sizeof(float));
 size_t distill_work_bytes() { return DISTILL_WORK; }
 
-// f(lanes of a slice, vectors of a lane), as constants, for n rows of `vectors`
+// f(lanes of a slice, vectors of a lane), as constants, for rows of `vectors`
 template <class F>
-void by_slice(int64_t n, int64_t vectors, F f) {
+void by_slice(int64_t vectors, F f) {
     using std::integral_constant;
     if (vectors <= 64 * 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
     else if (vectors <= 64 * 8) f(integral_constant<int, 64>(), integral_constant<int, 8>());
-    else if (n * cdiv(vectors, LOGIT_THREADS * 8) < 512) f(integral_constant<int, 256>(), integral_constant<int, 2>());
     else f(integral_constant<int, 256>(), integral_constant<int, 8>());
+}
+// the same for rows that one workgroup holds
+constexpr int64_t ROW_MOST = 1024 * 16;
+template <class F>
+void by_row(int64_t vectors, F f) {
+    using std::integral_constant;
+    if (vectors <= 64 * 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
+    else if (vectors <= 64 * 8) f(integral_constant<int, 64>(), integral_constant<int, 8>());
+    else if (vectors <= 256 * 8) f(integral_constant<int, 256>(), integral_constant<int, 8>());
+    else if (vectors <= 512 * 8) f(integral_constant<int, 512>(), integral_constant<int, 8>());
+    else if (vectors <= 1024 * 8) f(integral_constant<int, 1024>(), integral_constant<int, 8>());
+    else f(integral_constant<int, 1024>(), integral_constant<int, 16>());
 }
 
 // the rows [at, at + n) of a call
@@ -427,34 +518,59 @@ struct DistillCall {
     bool fwd, bwd;
 };
 
+static bool in_one_workgroup(const DistillCall& c, int64_t vectors) {
+    return vectors <= 512 * 8 || (c.bwd && vectors <= ROW_MOST && c.a.n >= 64);
+}
+
 template <class T>
 int distill_run(const DistillCall& c) {
     constexpr int N = VECTOR<T>;
     const DistillArgs& a = c.a;
     const hipStream_t st = c.d->stream;
+    const int64_t vectors = cdiv(a.dim, N);
+    const size_t entry_bytes = (size_t)a.top * 12;
+    // Logits that the memory-side cache does not hold until the next pass (256 MB, the gradient among them) stay out of its way.  us: 8192 rows of 131,072 bf16 (2.1 GB), loss
+    // 373 / 363; 4096 such rows, loss and then gradient 580 / 574; 777 of 50,021 f16 (78 MB) 74 / 81.
+    const bool stream = a.n * a.dim * (int64_t)sizeof(T) > (int64_t)128 << 20;
+    if (c.fwd && in_one_workgroup(c, vectors)) {
+        by_row(vectors, [&](auto l, auto p) {
+            constexpr int LANES = decltype(l)::value, PER = decltype(p)::value, THREADS = distill_threads(LANES), ROWS = THREADS / LANES;
+            const int64_t most = LAUNCH_THREADS / LANES;
+            for (int64_t at = 0; at < a.n; at += most) {
+                const DistillArgs b = rows_of(a, at, std::min(most, a.n - at), sizeof(T));
+                k_distill_row<T, LANES, PER><<<(unsigned)cdiv(b.n, ROWS), THREADS, ROWS * entry_bytes, st>>>(
+                    b, stream, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, c.loss + at, c.stats ? c.stats + at * STATS : nullptr,
+                    c.grad ? (T*)c.grad + at * c.grad_stride : nullptr, c.grad_stride);
+            }
+        });
+        FC_HIP(hipGetLastError());
+        return FC_OK;
+    }
     if (c.fwd) FC_TRY(dense_work(c.d, DISTILL_WORK));
     RowSums* part = reinterpret_cast<RowSums*>(c.d->work);
     float* work_stats = reinterpret_cast<float*>(c.d->work + DISTILL_SLICES * sizeof(RowSums));
-    by_slice(a.n, cdiv(a.dim, N), [&](auto l, auto p) {
+    auto run = [&](auto l, auto p) {
         constexpr int LANES = decltype(l)::value, PER = decltype(p)::value, ROWS = LOGIT_THREADS / LANES;
         const int slices = (int)cdiv(a.dim, RowSlice<T, LANES, PER>::COLUMNS);
         const int64_t most = DISTILL_SLICES / slices;
         for (int64_t at = 0; at < a.n; at += most) {
             const int64_t n = std::min(most, a.n - at);
             const DistillArgs b = rows_of(a, at, n, sizeof(T));
-            float* loss = c.loss ? c.loss + at : nullptr;
-            float* stats = c.stats ? c.stats + at * STATS : c.bwd ? work_stats : nullptr;
+            float* stats = c.stats ? c.stats + at * STATS : work_stats;
             const unsigned blocks = (unsigned)(cdiv(n, ROWS) * slices);
-            if (c.fwd) {
-                if (a.lse && a.alpha > 0.f) k_distill_fwd<T, LANES, PER, true><<<blocks, LOGIT_THREADS, 0, st>>>(b, slices, part, loss, stats);
-                else k_distill_fwd<T, LANES, PER, false><<<blocks, LOGIT_THREADS, 0, st>>>(b, slices, part, loss, stats);
-                if (slices > 1) k_distill_join<T><<<(unsigned)cdiv(n, LOGIT_THREADS / 64), LOGIT_THREADS, 0, st>>>(b, slices, part, loss, stats);
-            }
+            if constexpr (LANES == LOGIT_THREADS)
+                if (c.fwd) {
+                    k_distill_slice<T, LANES, PER><<<blocks, LOGIT_THREADS, 0, st>>>(b, slices, stream, part);
+                    k_distill_join<T><<<(unsigned)cdiv(n, LOGIT_THREADS / 64), LOGIT_THREADS, LOGIT_THREADS / 64 * entry_bytes, st>>>(b, slices, part, c.loss + at, stats);
+                }
             if (c.bwd)
-                k_distill_bwd<T, LANES, PER><<<blocks, LOGIT_THREADS, (size_t)ROWS * a.top * 12, st>>>(
-                    b, slices, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats, (T*)c.grad + at * c.grad_stride, c.grad_stride);
+                k_distill_bwd<T, LANES, PER><<<blocks, LOGIT_THREADS, ROWS * entry_bytes, st>>>(
+                    b, slices, stream, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats, (T*)c.grad + at * c.grad_stride, c.grad_stride);
         }
-    });
+    };
+    // Slices of 8 vectors a lane, or of 2 where those of 8 are fewer than two workgroups a compute unit.
+    if (vectors > 64 * 8 && a.n * cdiv(vectors, LOGIT_THREADS * 8) < 512) run(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    else by_slice(vectors, run);
     FC_HIP(hipGetLastError());
     return FC_OK;
 }
