@@ -79,6 +79,14 @@ __device__ __forceinline__ void store_from_float(T* __restrict__ p, const float 
 // lane at a time, from changing that order, and is no instruction itself.
 __device__ __forceinline__ void read_before_stores() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+// f(), which the compiler does not merge with a like sequence of another branch: accesses that go past the caches and those that do not are one to it, and become ordinary ones.
+template <int WHICH, class F>
+__device__ __forceinline__ void apart(F f) {
+    asm volatile("; %0" ::"i"(WHICH));
+    f();
+    asm volatile("; %0" ::"i"(WHICH));
+}
+
 // Sum over the wavefront's lanes, all of them active, in every lane.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float add_lane(float x) {

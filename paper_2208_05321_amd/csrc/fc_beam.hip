@@ -89,81 +89,105 @@ __device__ __forceinline__ bool beam_lives(const BeamArgs& a, int64_t row) {
     return s - s == 0.f;
 }
 
+// `run` neighbouring slices of a row, one after the other.  Of each wavefront's lanes the largest elements so far give a bound that a quarter of `keep` of them reach; the least of
+// the four is reached by `keep` elements.  (The `keep`-th of one wavefront's is a bound as well, and four times as many elements are above it.)  After the first slice a
+// wavefront looks at the bounds when it meets elements above its own; what the others have come to meanwhile does not matter, as bounds only rise.
 template <class T, int PER>
-__global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_t first, BeamSlice* __restrict__ sums, BeamEntry* __restrict__ lists) {
+__global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_t first, int run, BeamSlice* __restrict__ sums, BeamEntry* __restrict__ lists) {
     using Slice = RowSlice<T, LOGIT_THREADS, PER>;
-    constexpr int N = Slice::N;
-    __shared__ uint64_t list[BEAM_LIST];
-    __shared__ uint64_t best[LOGIT_THREADS / 64];
-    __shared__ uint32_t bounds[LOGIT_THREADS / 64];
-    __shared__ float offs[LOGIT_THREADS / 64];
-    __shared__ double parts[LOGIT_THREADS / 64];
-    __shared__ int count;
-    const int lane = threadIdx.x, slice = blockIdx.x % a.slices, base = slice * Slice::COLUMNS;
+    constexpr int N = Slice::N, WAVES = LOGIT_THREADS / 64;
+    __shared__ uint64_t list[BEAM_LIST], few[BEAM_LIST];
+    __shared__ uint64_t best[WAVES];
+    __shared__ float offs[WAVES];
+    __shared__ double parts[WAVES];
+    __shared__ uint32_t bounds[WAVES];
+    __shared__ int count, kept;
+    const int lane = threadIdx.x, part = blockIdx.x % a.slices, begin = part * run * Slice::COLUMNS;
     const int64_t local = blockIdx.x / a.slices, row = first + local;
     if (!beam_lives(a, row) || (a.finished && a.finished[row])) return;
     const T* x = (const T*)a.x + row * a.stride;
+    const int end = (int)min((int64_t)a.dim, begin + (int64_t)run * Slice::COLUMNS);
     Slice s;
-    s.load(x, base, lane, a.dim, true);
-    s.cut(base, lane, a.dim);
-    float most[PER], top = -INFINITY;
+    s.load(x, begin, lane, a.dim, true);
+    if (lane == 0) count = kept = 0;
+    auto bound = [&]() {
+        uint32_t b = *(volatile uint32_t*)&bounds[0];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        most[k] = s.at(k, 0);
-#pragma unroll
-        for (int e = 1; e < N; ++e) most[k] = fmaxf(most[k], s.at(k, e));
-        top = fmaxf(top, most[k]);
-    }
-    // sum of exponentials, each lane's from its own largest element
-    s.forget();
-    const float off = top * LOG2E, sum = s.exponentials(LOG2E, from_of(off));
-    const float off_wave = wave_max(off);
-    const double part = wave_sum((double)(sum * __builtin_amdgcn_exp2f(off - from_of(off_wave))));
-    const uint32_t bound_wave = wave_bound(ordered(top), a.keep);
-    if (lane == 0) count = 0;
-    if ((lane & 63) == 0) { offs[lane >> 6] = off_wave; parts[lane >> 6] = part; bounds[lane >> 6] = bound_wave; }
-    __syncthreads();
-    uint32_t bound = 0x00800000u;                  // the lowest finite number: -infinity is no candidate
-#pragma unroll
-    for (int k = 0; k < LOGIT_THREADS / 64; ++k) bound = max(bound, bounds[k]);
-    const float least = unordered(bound);
-    if (top >= least) {
+        for (int k = 1; k < WAVES; ++k) b = min(b, *(volatile uint32_t*)&bounds[k]);
+        return max(b, 0x00800000u);                // the lowest finite number: -infinity is no candidate
+    };
+    float lane_top = -INFINITY, off = -INFINITY, sum = 0.f, least = -INFINITY;
+    for (int base = begin; base < end; base += Slice::COLUMNS) {
+        const int lane = here(threadIdx.x);
+        if (base > begin) s.load_long(x, base, lane, a.dim, true);
+        s.cut(base, lane, a.dim);
+        const float top = s.largest();
+        s.forget();
+        // sum of exponentials, each lane's from its own largest element so far
+        const float to = fmaxf(off, top * LOG2E);
+        sum = sum * __builtin_amdgcn_exp2f(off - from_of(to)) + s.exponentials(LOG2E, from_of(to));
+        off = to;
+        lane_top = fmaxf(lane_top, top);
+        if (base > begin && !__any(top >= least)) continue;
+        const uint32_t mine = wave_bound(ordered(lane_top), (a.keep + WAVES - 1) / WAVES);
+        if ((lane & 63) == 0) *(volatile uint32_t*)&bounds[lane >> 6] = mine;
+        if (base == begin) __syncthreads();
+        least = unordered(bound());
+        if (!(top >= least)) continue;
         uint32_t at = 0;
+        s.forget();
 #pragma unroll
-        for (int k = 0; k < PER; ++k) if (most[k] >= least) at |= 1u << k;
+        for (int k = 0; k < PER; ++k) if (s.largest(k) >= least) at |= 1u << k;
         while (at) {
             const int k = __builtin_ctz(at);
             at &= at - 1;
             const typename Slice::V v = s.pick(k);
             const int col = min(Slice::column(base, lane, k), a.dim - N);
+            uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if ((float)v[e] >= least) {
-                    const int p = atomicAdd(&count, 1);
-                    if (p < BEAM_LIST) list[p] = entry_key((float)v[e], col + e);
-                }
+            for (int e = 0; e < N; ++e) hits |= (float)v[e] >= least ? 1u << e : 0;
+            while (hits) {
+                const int e = __builtin_ctz(hits);
+                hits &= hits - 1;
+                float f = (float)v[0];
+#pragma unroll
+                for (int j = 1; j < N; ++j) { const float y = (float)v[j]; f = j == e ? y : f; }
+                const int p = atomicAdd(&count, 1);
+                if (p < BEAM_LIST) list[p] = entry_key(f, col + e);
+            }
         }
     }
+    const float off_wave = wave_max(off);
+    const double sum_wave = wave_sum((double)(sum * __builtin_amdgcn_exp2f(off - from_of(off_wave))));
+    if ((lane & 63) == 0) { offs[lane >> 6] = off_wave; parts[lane >> 6] = sum_wave; }
     __syncthreads();
-    BeamEntry* out = lists + (local * a.slices + slice) * a.keep;
+    BeamEntry* out = lists + (local * a.slices + part) * a.keep;
     auto put = [&](int at, uint64_t key) { out[at] = BeamEntry{unordered((uint32_t)(key >> 32)), (int32_t)~(uint32_t)key}; };
-    const int got = count;
-    if (got <= BEAM_LIST) {
-        for (int i = lane; i < got; i += LOGIT_THREADS) {
+    const uint64_t lowest = (uint64_t)bound() << 32;
+    if (count <= BEAM_LIST) {
+        for (int i = lane; i < count; i += LOGIT_THREADS) {
             const uint64_t key = list[i];
+            if (key >= lowest) few[atomicAdd(&kept, 1)] = key;
+        }
+        __syncthreads();
+        const int got = kept;
+        for (int i = lane >> 3; i < got; i += LOGIT_THREADS / 8) {   // eight lanes to an element
+            const uint64_t key = few[i];
             int rank = 0;
-            for (int j = 0; j < got; ++j) rank += list[j] > key;
-            if (rank < a.keep) put(rank, key);
+            for (int j = lane & 7; j < got; j += 8) rank += few[j] > key;
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor(rank, o);
+            if (rank < a.keep && (lane & 7) == 0) put(rank, key);
         }
         for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) out[i] = BeamEntry{-INFINITY, 0};
     } else {                                       // (as good as equal logits)
         uint64_t last = ~0ull;
         for (int i = 0; i < a.keep; ++i) {
             uint64_t mine = 0;
-            for (int c = base + lane; c < min(a.dim, base + Slice::COLUMNS); c += LOGIT_THREADS) {
+            for (int c = begin + lane; c < end; c += LOGIT_THREADS) {
                 const float v = (float)x[c];
                 const uint64_t key = entry_key(v, c);
-                if (v >= least && key < last && key > mine) mine = key;
+                if (v == v && key >= lowest && key < last && key > mine) mine = key;
             }
             last = block_max(mine, best);
             if (lane == 0) put(i, last);
@@ -171,10 +195,10 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     }
     if (lane == 0) {
         float to = offs[0];
-        for (int k = 1; k < LOGIT_THREADS / 64; ++k) to = fmaxf(to, offs[k]);
+        for (int k = 1; k < WAVES; ++k) to = fmaxf(to, offs[k]);
         double all = 0.;
-        for (int k = 0; k < LOGIT_THREADS / 64; ++k) all += parts[k] * (double)exp2f(offs[k] - from_of(to));
-        sums[local * a.slices + slice] = BeamSlice{all, to};
+        for (int k = 0; k < WAVES; ++k) all += parts[k] * (double)exp2f(offs[k] - from_of(to));
+        sums[local * a.slices + part] = BeamSlice{all, to};
     }
 }
 
@@ -306,19 +330,21 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
     for (int i = got + lane; i < a.keep; i += JOIN_THREADS) put(i, Candidate{-INFINITY, 0.f, 0, max(a.eos, 0)});
 }
 
+constexpr int64_t BEAM_GROUPS = 1024;             // workgroups of the first step, beyond which they take several slices each
 constexpr size_t BEAM_WORK = (size_t)5 << 20;      // of a launch's slices (one sequence takes 4.4 MB at most); more sequences go in several
 size_t beam_work_bytes() { return BEAM_WORK; }
 
 template <class T, int PER>
 void beam_run(fc_dense* d, BeamArgs a, int64_t batch, float* scores, int32_t* parents, void* tokens, int32_t token_type, uint8_t* finished) {
-    a.slices = (int32_t)cdiv(a.dim, RowSlice<T, LOGIT_THREADS, PER>::COLUMNS);
+    const int64_t slices = cdiv(a.dim, RowSlice<T, LOGIT_THREADS, PER>::COLUMNS), run = std::clamp<int64_t>(batch * a.beams * slices / BEAM_GROUPS, 1, 8);
+    a.slices = (int32_t)cdiv(slices, run);
     const size_t of_seq = (size_t)a.beams * a.slices * (sizeof(BeamSlice) + a.keep * sizeof(BeamEntry));
     const int64_t most = std::max<int64_t>(1, (int64_t)(BEAM_WORK / of_seq));
     for (int64_t at = 0; at < batch; at += most) {
         const int64_t n = std::min(most, batch - at);
         BeamSlice* sums = reinterpret_cast<BeamSlice*>(d->work);
         BeamEntry* lists = reinterpret_cast<BeamEntry*>(sums + n * a.beams * a.slices);
-        k_beam_slice<T, PER><<<(unsigned)(n * a.beams * a.slices), LOGIT_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists);
+        k_beam_slice<T, PER><<<(unsigned)(n * a.beams * a.slices), LOGIT_THREADS, 0, d->stream>>>(a, at * a.beams, (int)run, sums, lists);
         const int64_t o = at * a.keep;
         auto join = [&](auto held) {
             k_beam_join<decltype(held)::value><<<(unsigned)n, JOIN_THREADS, 0, d->stream>>>(a, at * a.beams, sums, lists, scores + o, parents + o,

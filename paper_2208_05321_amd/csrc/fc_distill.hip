@@ -84,7 +84,11 @@ struct Sums {
 };
 constexpr double LN2 = 0.69314718055994530942;
 constexpr Sums NO_SUMS{-INFINITY, -INFINITY, 0.f, 0.f};
-struct RowSums { Sums rest, named; };
+// What is left of a row, or of a slice, without the named ids where P_0 needs that; twice: an id was seen to be named more than once.
+struct RowSums { Sums rest; float twice; };
+
+// of an entry's probability, from that of the largest
+__device__ __forceinline__ double exponent(float z, float zmax, double it) { return ((double)z - zmax) * it; }
 
 // Entries of a row in LDS: ids (-1: none that counts), the teacher's logits, and later probabilities, the student's logits.
 struct Entries { int* id; float* z; float* x; };
@@ -107,8 +111,24 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, f
     const double it = 1.0 / (double)a.temperature;
     const float ct = scale_of(a);
     const float lse = a.lse ? a.lse[row] : 0.f;
+    const bool two = a.alpha < 1.f && a.temperature != 1.f;
     Sums all = s.rest;
-    all.join(s.named);
+    if (a.lse && a.alpha > 0.f) {                  // and the named ones, each once
+        Sums named = NO_SUMS;
+        for (int k = lane; k < a.top; k += 64) {
+            const int id = t.id[k];
+            bool counts = id >= 0;
+            if (s.twice != 0.f)
+                for (int j = 0; j < k; ++j) counts &= t.id[j] != id;
+            if (!counts) continue;
+            const float x = t.x[k];
+            Sums q{x * ct, x * (two ? LOG2E : ct), 0.f, 0.f};
+            q.t = __builtin_amdgcn_exp2f(fmaf(x, ct, -from_of(q.off)));
+            q.one = two ? __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from_of(q.off1))) : q.t;
+            named.join(q);
+        }
+        all.join(named.over_wave(two));
+    }
     const double lse2 = (double)all.off + (double)log2f(all.t);
 
     float zmax = -INFINITY;
@@ -130,14 +150,14 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, f
         } else {
             float sum = 0.f;
             for (int k = lane; k < a.top; k += 64)
-                if (t.id[k] >= 0) sum += expf((float)(((double)t.z[k] - zmax) * it));
+                if (t.id[k] >= 0) sum += expf((float)exponent(t.z[k], zmax, it));
             sum = wave_sum(sum);
             zinv = 1.f / sum;
             log_zinv = -(double)logf(sum);
         }
         for (int k = lane; k < a.top; k += 64) {
             if (t.id[k] < 0) continue;
-            const double d = ((double)t.z[k] - zmax) * it;
+            const double d = exponent(t.z[k], zmax, it);
             const float p = expf((float)d) * zinv;
             t.z[k] = p;
             part += p;
@@ -157,8 +177,7 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, f
     if (lane != 0) return;
     float value = some ? a.alpha * a.temperature * a.temperature * kl : 0.f;
     if (a.alpha < 1.f) value += (1.f - a.alpha) * (float)(((double)all.off1 + (double)log2f(all.one) - (double)xy * LOG2E) * LN2);
-    loss[row] = value;
-    if (!stats) return;
+    if (loss) loss[row] = value;
     const float c = sum_p + p0;
     float coef = 0.f, coef1 = 0.f;
     if (s.rest.t != 0.f) {                         // (else there is nothing that is not named, or only logits of -infinity)
@@ -187,86 +206,70 @@ __device__ __forceinline__ void distill_left_out(int64_t row, int lane, float* l
 }
 
 // Marks of a slice's named elements, in LDS: a byte for each vector, those of a lane side by side.
-template <int LANES, int PER> struct Marks { uint64_t of[LANES][(PER + 7) / 8]; };
+template <int LANES, int PER> struct Marks { uint64_t of[LANES][(PER + 7) / 8]; int32_t twice; };
 
-// The sums of a slice, over one wavefront's lanes.  With what the teacher's entries leave over (a.lse), named elements become -infinity in the registers before the sums are
-// taken; their own sums are those of the few lanes that have some.
+// Marks the elements of a slice that the row's entries name.
 template <class T, int LANES, int PER>
-__device__ __forceinline__ RowSums slice_sums(const DistillArgs& a, RowSlice<T, LANES, PER>& s, int64_t row, int base, int lane, Marks<LANES, PER>& marks) {
+__device__ __forceinline__ void mark_named(const DistillArgs& a, int64_t row, int base, int lane, Marks<LANES, PER>& marks) {
+    constexpr int N = VECTOR<T>, COLUMNS = RowSlice<T, LANES, PER>::COLUMNS;
+#pragma unroll
+    for (int j = 0; j < (PER + 7) / 8; ++j) marks.of[lane][j] = 0;
+    if (lane == 0) marks.twice = 0;
+    row_sync<LANES>();
+    for (int k = lane; k < a.top; k += LANES) {
+        const int64_t id = load_id(a.ids, a.id_type, row * a.top + k) - base;
+        if (id < 0 || id >= min(COLUMNS, a.dim - base)) continue;
+        const int v = (int)id / N, j = v / LANES;
+        const uint32_t bit = 1u << (j % 4 * 8 + (int)id % N);
+        if (atomicOr(reinterpret_cast<uint32_t*>(&marks.of[v % LANES][0]) + j / 4, bit) & bit) marks.twice = 1;
+    }
+    row_sync<LANES>();
+}
+
+// Adds a slice to a lane's sums; marked elements become -infinity in the registers before.
+template <class T, int LANES, int PER>
+__device__ __forceinline__ void add_slice(const DistillArgs& a, RowSlice<T, LANES, PER>& s, int base, int lane, const Marks<LANES, PER>* marks, Sums& r) {
     using Slice = RowSlice<T, LANES, PER>;
     constexpr int N = Slice::N;
     const float ct = scale_of(a);
-    const bool two = a.alpha < 1.f && a.temperature != 1.f, rest = a.lse && a.alpha > 0.f;
-    RowSums r{NO_SUMS, NO_SUMS};
-    if (rest) {
-#pragma unroll
-        for (int j = 0; j < (PER + 7) / 8; ++j) marks.of[lane][j] = 0;
-        row_sync<LANES>();
-        for (int k = lane; k < a.top; k += LANES) {
-            const int64_t id = load_id(a.ids, a.id_type, row * a.top + k) - base;
-            if (id < 0 || id >= min(Slice::COLUMNS, a.dim - base)) continue;
-            const int v = (int)id / N, j = v / LANES;
-            atomicOr(reinterpret_cast<uint32_t*>(&marks.of[v % LANES][0]) + j / 4, 1u << (j % 4 * 8 + (int)id % N));
-        }
-        row_sync<LANES>();
-    }
     s.cut(base, lane, a.dim);
-    if (rest) {
+    if (marks) {
 #pragma unroll
         for (int j = 0; j < (PER + 7) / 8; ++j) {
-            uint64_t mask = marks.of[lane][j];
-            if (base + Slice::COLUMNS > a.dim) {   // the last vector's elements are loaded further on in it
-                uint64_t moved = 0;
-#pragma unroll
-                for (int k = 0; k < 8 && j * 8 + k < PER; ++k)
-                    moved |= (uint64_t)((uint32_t)(mask >> 8 * k & 0xff) << Slice::skip(Slice::column(base, lane, j * 8 + k), a.dim)) << 8 * k;
-                mask = moved;
-            }
-            for (uint64_t m = mask; m; m &= m - 1) {
-                const int at = __builtin_ctzll(m);
-                const typename Slice::V v = s.pick(j * 8 + at / 8);
-                float x = 0.f;
-#pragma unroll
-                for (int e = 0; e < N; ++e) if (e == at % 8) x = (float)v[e];
-                Sums q{x * ct, x * (two ? LOG2E : ct), 0.f, 0.f};
-                q.t = __builtin_amdgcn_exp2f(fmaf(x, ct, -from_of(q.off)));
-                q.one = two ? __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from_of(q.off1))) : q.t;
-                r.named.join(q);
-            }
+            const uint64_t mask = marks->of[lane][j];
+            if (mask == 0) continue;
 #pragma unroll
             for (int k = 0; k < 8 && j * 8 + k < PER; ++k) {
-                const uint32_t b = mask >> 8 * k & 0xff;
+                uint32_t b = mask >> 8 * k & 0xff;
                 if (b == 0) continue;
+                if (base + Slice::COLUMNS > a.dim) b <<= Slice::skip(Slice::column(base, lane, j * 8 + k), a.dim);     // the last vector's elements are loaded further on in it
 #pragma unroll
                 for (int e = 0; e < N; ++e) if (b >> e & 1) s.x[j * 8 + k][e] = (T)-INFINITY;
             }
         }
-        r.named = r.named.over_wave(two);
     }
     s.forget();
     const float top = s.largest();
     s.forget();
-    r.rest.off = r.rest.off1 = top * ct;
-    r.rest.t = r.rest.one = s.exponentials(ct, from_of(r.rest.off));
-    if (two) {
-        r.rest.off1 = top * LOG2E;
+    r.off = r.off1 = top * ct;
+    r.t = r.one = s.exponentials(ct, from_of(r.off));
+    if (a.alpha < 1.f && a.temperature != 1.f) {
+        r.off1 = top * LOG2E;
         s.forget();
-        r.rest.one = s.exponentials(LOG2E, from_of(r.rest.off1));
+        r.one = s.exponentials(LOG2E, from_of(r.off1));
     }
-    r.rest = r.rest.over_wave(two);
-    return r;
 }
 // of all the wavefronts of a row, in the first of them
 template <int LANES>
-__device__ __forceinline__ void join_waves(RowSums& r, RowSums* lds, bool rest) {
+__device__ __forceinline__ void join_waves(const DistillArgs& a, Sums& r, Sums* lds) {
+    const bool two = a.alpha < 1.f && a.temperature != 1.f;
+    r = r.over_wave(two);
     if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = r;
         __syncthreads();
         if (threadIdx.x >= 64) return;
-        const int lane = threadIdx.x;
-        r = lane < LANES / 64 ? lds[lane] : RowSums{NO_SUMS, NO_SUMS};
-        r.rest = r.rest.over_wave(true);
-        if (rest) r.named = r.named.over_wave(true);
+        r = threadIdx.x < LANES / 64 ? lds[threadIdx.x] : NO_SUMS;
+        r = r.over_wave(two);
     }
 }
 
@@ -328,17 +331,19 @@ __device__ __forceinline__ void store_zeros(T* out, int base, int lane, int dim)
 
 constexpr int distill_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
-// Rows that LANES lanes hold: the loss, and the gradient too if it is wanted (grad), which may take the place of the logits: a row is read before any of it is written.
+// Rows that LANES lanes hold: the loss, and the gradient too if it is wanted (grad), which may take the place of the logits: a row is read before any of it is written.  The row waits in
+// registers while one wavefront works on its entries, so what counts is how many rows a compute unit holds: 80 registers and three rows of 64 KB, though some
+// 40 bytes of a lane then go through memory (16,384 rows of 32,768 bf16: 4 to 8 wavefronts a SIMD 532 / - / 446 / 490 / 586 us).
 template <class T, int LANES, int PER>
-__global__ __launch_bounds__(distill_threads(LANES)) void k_distill_row(DistillArgs a, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride, float* __restrict__ loss,
+__global__ __launch_bounds__(distill_threads(LANES)) __attribute__((amdgpu_waves_per_eu(LANES <= 512 ? 6 : 4))) void k_distill_row(DistillArgs a, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride, float* __restrict__ loss,
                                                                         float* __restrict__ stats, T* grad, int64_t grad_stride) {
     using Slice = RowSlice<T, LANES, PER>;
     constexpr int ROWS = distill_threads(LANES) / LANES;
     extern __shared__ float dynamic[];             // entries
     __shared__ Marks<LANES, PER> marks[ROWS];
-    __shared__ RowSums lds[distill_threads(LANES) / 64];
+    __shared__ Sums lds[distill_threads(LANES) / 64];
     __shared__ float row_stats[ROWS][STATS];
-    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES, sub = LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : threadIdx.x / LANES;
     const int64_t row = (int64_t)blockIdx.x * ROWS + sub;
     if (row >= a.n) return;                        // (all lanes of the row)
     const T* x = (const T*)a.x + row * a.stride;
@@ -355,8 +360,12 @@ __global__ __launch_bounds__(distill_threads(LANES)) void k_distill_row(DistillA
     const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
     load_entries<T, LANES>(a, row, lane, x, t);
     const float xy = y >= 0 ? (float)x[y] : 0.f;
-    RowSums r = slice_sums<T, LANES, PER>(a, s, row, 0, lane, marks[sub]);
-    join_waves<LANES>(r, lds, a.lse != nullptr);
+    const bool rest = a.lse && a.alpha > 0.f;
+    if (rest) mark_named<T, LANES, PER>(a, row, 0, lane, marks[sub]);
+    RowSums r{NO_SUMS, 0.f};
+    add_slice<T, LANES, PER>(a, s, 0, lane, rest ? &marks[sub] : nullptr, r.rest);
+    join_waves<LANES>(a, r.rest, lds);
+    if (rest) r.twice = (float)marks[sub].twice;
     float* st = row_stats[sub];
     if constexpr (LANES <= 64) row_sync<LANES>();
     if (lane < 64) {
@@ -380,7 +389,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_slice(DistillArgs a, 
     using Slice = RowSlice<T, LANES, PER>;
     static_assert(LANES == LOGIT_THREADS);
     __shared__ Marks<LANES, PER> marks;
-    __shared__ RowSums lds[LOGIT_THREADS / 64];
+    __shared__ Sums lds[LOGIT_THREADS / 64];
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x / slices;
     const int slice = blockIdx.x % slices, base = slice * Slice::COLUMNS;
@@ -390,9 +399,25 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_slice(DistillArgs a, 
         const int64_t y = load_id(a.target, a.target_type, row);
         if (y < 0 || y >= a.dim) return;
     }
-    RowSums r = slice_sums<T, LANES, PER>(a, s, row, base, lane, marks);
-    join_waves<LANES>(r, lds, a.lse != nullptr);
-    if (lane == 0) part[row * slices + slice] = r;
+    const bool rest = a.lse && a.alpha > 0.f;
+    if (rest) mark_named<T, LANES, PER>(a, row, base, lane, marks);
+    Sums r = NO_SUMS;
+    add_slice<T, LANES, PER>(a, s, base, lane, rest ? &marks : nullptr, r);
+    join_waves<LANES>(a, r, lds);
+    if (lane == 0) part[row * slices + slice] = RowSums{r, rest ? (float)marks.twice : 0.f};
+}
+
+// The sums of a row's slices, by a wavefront.
+__device__ __forceinline__ RowSums row_sums(const DistillArgs& a, const RowSums* __restrict__ part, int64_t row, int slices) {
+    RowSums r{NO_SUMS, 0.f};
+    for (int k = threadIdx.x & 63; k < slices; k += 64) {
+        const RowSums q = part[row * slices + k];
+        r.rest.join(q.rest);
+        r.twice = fmaxf(r.twice, q.twice);
+    }
+    r.rest = r.rest.over_wave(a.alpha < 1.f && a.temperature != 1.f);
+    r.twice = __any(r.twice != 0.f) ? 1.f : 0.f;
+    return r;
 }
 
 // The rows of several slices: a wavefront to a row.
@@ -404,19 +429,12 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_join(DistillArgs a, i
     const int64_t row = (int64_t)blockIdx.x * (LOGIT_THREADS / 64) + sub;
     if (row >= a.n) return;
     const T* x = (const T*)a.x + row * a.stride;
-    RowSums r{NO_SUMS, NO_SUMS};
-    for (int k = lane; k < slices; k += 64) {
-        const RowSums q = part[row * slices + k];
-        r.rest.join(q.rest);
-        r.named.join(q.named);
-    }
+    const RowSums r = row_sums(a, part, row, slices);
     int y;
     if (!row_target(a, row, &y)) { distill_left_out(row, lane, loss, stats); return; }
     const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
     load_entries<T, 64>(a, row, lane, x, t);
     const float xy = y >= 0 ? (float)x[y] : 0.f;
-    r.rest = r.rest.over_wave(true);
-    r.named = r.named.over_wave(true);
     row_sync<64>();
     distill_row(a, row, xy, r, t, loss, row_stats[sub]);
     row_sync<64>();
@@ -424,41 +442,60 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_join(DistillArgs a, i
 }
 
 // The gradient of a slice.  It may take the place of the logits: a slice is read, its entries among it, before any of it is written.
-template <class T, int LANES, int PER>
-__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, int slices, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride,
-                                                               const float* __restrict__ stats, T* grad, int64_t grad_stride) {
+// PARTS: the row's slices have not been joined; every workgroup does that for itself, which saves few rows a launch, and the first slice's stores the loss.  Not in place: a
+// workgroup reads all of the row's entries, when others may have stored their slices.
+template <class T, int LANES, int PER, bool PARTS>
+__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, int slices, bool stream, const RowSums* __restrict__ part, float* __restrict__ loss,
+                                                               const float* __restrict__ grad_loss, int64_t grad_loss_stride, const float* __restrict__ stats, T* grad,
+                                                               int64_t grad_stride) {
     using Slice = RowSlice<T, LANES, PER>;
     constexpr int ROWS = LOGIT_THREADS / LANES;
+    static_assert(!PARTS || ROWS == 1);
     extern __shared__ float dynamic[];
-    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
-    const unsigned block = blockIdx.x;
-    const int64_t row = (int64_t)(block / slices) * ROWS + sub;
-    const int slice = block % slices, base = slice * Slice::COLUMNS;
+    __shared__ float row_stats[PARTS ? STATS : 1];
+    const int lane = threadIdx.x % LANES, sub = LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : threadIdx.x / LANES;
+    const int64_t row = (int64_t)(blockIdx.x / slices) * ROWS + sub;
+    const int slice = blockIdx.x % slices, base = slice * Slice::COLUMNS;
     if (row >= a.n) return;
     const T* x = (const T*)a.x + row * a.stride;
     T* out = grad + row * grad_stride;
-    const float* st = stats + row * STATS;
     Slice s;
     s.load(x, base, lane, a.dim, stream);
-    const float g = grad_loss[row * grad_loss_stride], kind = st[ST_KIND];
-    if (kind == ROW_OUT || g == 0.f) { store_zeros<T, LANES, PER>(out, base, lane, a.dim); return; }
+    const float g = grad_loss[row * grad_loss_stride];
     const int end = min(a.dim, base + Slice::COLUMNS);
     const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
-    const float it = (float)(1.0 / (double)a.temperature);
-    for (int k = lane; kind == ROW_ENTRIES && k < a.top; k += LANES) {
-        const int64_t i = row * a.top + k, id = load_id(a.ids, a.id_type, i);
-        const bool here = id >= base && id < end;
-        t.id[k] = here ? (int)id : -1;
-        if (here) {
-            t.z[k] = expf((load_value(a.z, a.z_type, i) - st[ST_ZFROM]) * it) * st[ST_ZINV];
-            t.x[k] = (float)x[id];
-        }
-    }
+    const float* st = PARTS ? row_stats : stats + row * STATS;
     int y = -1;
     float xy = 0.f;
-    if (a.target && a.alpha < 1.f) {
-        y = (int)load_id(a.target, a.target_type, row);
-        if (y >= base && y < end) xy = (float)x[y];
+    if constexpr (PARTS) {
+        if (!row_target(a, row, &y)) {
+            if (slice == 0) distill_left_out(row, lane, loss, nullptr);
+            store_zeros<T, LANES, PER>(out, base, lane, a.dim);
+            return;
+        }
+        load_entries<T, LANES>(a, row, lane, x, t);
+        if (y >= 0) xy = (float)x[y];
+        __syncthreads();
+        if (lane < 64) distill_row(a, row, xy, row_sums(a, part, row, slices), t, slice == 0 ? loss : nullptr, row_stats);
+        __syncthreads();
+        if (st[ST_KIND] == ROW_OUT || g == 0.f) { store_zeros<T, LANES, PER>(out, base, lane, a.dim); return; }
+    } else {
+        const float kind = st[ST_KIND];
+        if (kind == ROW_OUT || g == 0.f) { store_zeros<T, LANES, PER>(out, base, lane, a.dim); return; }
+        const double it = 1.0 / (double)a.temperature;
+        for (int k = lane; kind == ROW_ENTRIES && k < a.top; k += LANES) {
+            const int64_t i = row * a.top + k, id = load_id(a.ids, a.id_type, i);
+            const bool here = id >= base && id < end;
+            t.id[k] = here ? (int)id : -1;
+            if (here) {
+                t.z[k] = expf((float)exponent(load_value(a.z, a.z_type, i), st[ST_ZFROM], it)) * st[ST_ZINV];
+                t.x[k] = (float)x[id];
+            }
+        }
+        if (a.target && a.alpha < 1.f) {
+            y = (int)load_id(a.target, a.target_type, row);
+            if (y >= base && y < end) xy = (float)x[y];
+        }
     }
     slice_grad<T, LANES, PER>(a, s, g, st);
     row_sync<LANES>();
@@ -518,8 +555,13 @@ struct DistillCall {
     bool fwd, bwd;
 };
 
+constexpr int64_t DISTILL_FEW = 64;
+// Whether a workgroup takes a whole row, in one launch, or rows are cut into slices.  us, whole rows / slices: gradient, 4096 rows of 131,072 bf16 485 / 540, 200 of 50,021 f16
+// 19.4 / 29.4, 70 18.0 / 18.4, 16,000 of 16,384 bf16 215 / 287, of 5000 f32 157 / 225; loss, 16,000 of 16,000 bf16 130 / 116, of 30,000 230 / 178, of 5000 f32 78 / 75, but
+// 100 of 30,000 bf16 11.7 / 14.7.
 static bool in_one_workgroup(const DistillCall& c, int64_t vectors) {
-    return vectors <= 512 * 8 || (c.bwd && vectors <= ROW_MOST && c.a.n >= 64);
+    if (c.bwd) return vectors <= 512 * 8 || (vectors <= ROW_MOST && c.a.n >= DISTILL_FEW);
+    return vectors <= 64 * 8 || (vectors <= 512 * 8 && c.a.n <= 1024);
 }
 
 template <class T>
@@ -558,14 +600,18 @@ int distill_run(const DistillCall& c) {
             const DistillArgs b = rows_of(a, at, n, sizeof(T));
             float* stats = c.stats ? c.stats + at * STATS : work_stats;
             const unsigned blocks = (unsigned)(cdiv(n, ROWS) * slices);
+            auto backward = [&](auto parts) {
+                k_distill_bwd<T, LANES, PER, decltype(parts)::value><<<blocks, LOGIT_THREADS, ROWS * entry_bytes, st>>>(
+                    b, slices, stream, part, c.loss ? c.loss + at : nullptr, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats, (T*)c.grad + at * c.grad_stride,
+                    c.grad_stride);
+            };
             if constexpr (LANES == LOGIT_THREADS)
                 if (c.fwd) {
                     k_distill_slice<T, LANES, PER><<<blocks, LOGIT_THREADS, 0, st>>>(b, slices, stream, part);
+                    if (c.bwd && !c.stats && a.n < DISTILL_FEW && c.grad != a.x) { backward(std::true_type()); continue; }
                     k_distill_join<T><<<(unsigned)cdiv(n, LOGIT_THREADS / 64), LOGIT_THREADS, LOGIT_THREADS / 64 * entry_bytes, st>>>(b, slices, part, c.loss + at, stats);
                 }
-            if (c.bwd)
-                k_distill_bwd<T, LANES, PER><<<blocks, LOGIT_THREADS, ROWS * entry_bytes, st>>>(
-                    b, slices, stream, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats, (T*)c.grad + at * c.grad_stride, c.grad_stride);
+            if (c.bwd) backward(std::false_type());
         }
     };
     // Slices of 8 vectors a lane, or of 2 where those of 8 are fewer than two workgroups a compute unit.

@@ -38,12 +38,14 @@ __device__ __forceinline__ void move_chunk(const char* src, char* dst, int64_t s
 #pragma unroll
     for (int i = 0; i < MOST; ++i)
         v[i] = *reinterpret_cast<const typename Chunk<BYTES>::V*>(src + __builtin_amdgcn_readfirstlane(m.from[min(i, n - 1)]) * src_row);
+    using V = typename Chunk<BYTES>::V;
+    auto each = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < MOST; ++i)
-        if (i < n) {
-            auto* o = reinterpret_cast<typename Chunk<BYTES>::V*>(dst + __builtin_amdgcn_readfirstlane(m.to[i]) * dst_row);
-            if (stream) __builtin_nontemporal_store(v[i], o); else *o = v[i];
-        }
+        for (int i = 0; i < MOST; ++i)
+            if (i < n) f(i, dst + __builtin_amdgcn_readfirstlane(m.to[i]) * dst_row);
+    };
+    if (stream) apart<1>([&] { each([&](int i, char* o) { __builtin_nontemporal_store(v[i], reinterpret_cast<V*>(o)); }); });
+    else apart<0>([&] { each([&](int i, char* o) { *reinterpret_cast<V*>(o) = v[i]; }); });
 }
 template <int BYTES, int MOST>
 __device__ __forceinline__ void move_rows(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, bool stream) {

@@ -10,19 +10,30 @@ namespace fc {
 constexpr int LOGIT_THREADS = 256;                 // of a workgroup
 constexpr float LOG2E = 1.44269504088896340736f;
 
-__device__ __forceinline__ float wave_max(float x) {       // of numbers; in every lane
-    auto step = [](float v, auto ctrl, auto rows) {
-        const int o = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, -INFINITY), __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
-        return fmaxf(v, __builtin_bit_cast(float, o));
-    };
-    using std::integral_constant;
-    x = step(x, integral_constant<int, 0x111>(), integral_constant<int, 0xf>());       // row_shr 1, 2, 4, 8
-    x = step(x, integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
-    x = step(x, integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
-    x = step(x, integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
-    x = step(x, integral_constant<int, 0x142>(), integral_constant<int, 0xa>());       // row_bcast 15, 31
-    x = step(x, integral_constant<int, 0x143>(), integral_constant<int, 0xc>());
+// of numbers; in every lane.  (Lanes without a neighbour keep what they have.  Two wait states lie between a register's result and another lane's use of it.)
+__device__ __forceinline__ float wave_max(float x) {
+    asm("s_nop 1\n v_max_f32_dpp %0, %0, %0 row_shr:1 row_mask:0xf bank_mask:0xf\n"
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_shr:2 row_mask:0xf bank_mask:0xf\n"
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_shr:4 row_mask:0xf bank_mask:0xf\n"
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_shr:8 row_mask:0xf bank_mask:0xf\n"
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_bcast:15 row_mask:0xa bank_mask:0xf\n"
+        "s_nop 1\n v_max_f32_dpp %0, %0, %0 row_bcast:31 row_mask:0xc bank_mask:0xf\n"
+        "s_nop 1" : "+v"(x));
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// The lane's number, as a value of this place of the program: what follows from it is worked out here, and not kept in registers from before a loop, or for after it.
+__device__ __forceinline__ int here(int lane) {
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
+// The largest of three; NaN only if all are.  (Written as one instruction: of maxima of elements of 16 bits the compiler makes maxima in 16 bits, and of those, in bf16,
+// maxima in 32 bits that are converted back each, three instructions more an element.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
 // Waits of the LANES threads that share a row for one another: a wavefront's accesses leave in the order of its instructions, so that one
@@ -47,16 +58,26 @@ struct RowSlice {
     static __device__ __forceinline__ int column(int base, int lane, int k) { return base + (k * LANES + lane) * N; }
     static __device__ __forceinline__ int skip(int col, int dim) { return min(max(col - (dim - N), 0), N); }
 
-    // stream: nobody reads the row again soon; it is kept out of the caches' way
+    // f(k, vector k's address) of a whole slice: the wavefront's lanes share an address but for 16 bytes times their number, which leaves 64-bit addresses out of the vector registers
+    template <class P, class F>
+    static __device__ __forceinline__ void each(P* row, int base, int lane, F f) {
+        P* p = row + base;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) f(k, p + k * LANES * N + (uint32_t)lane * N);
+    }
+    // of a row of a vector at least; stream: nobody reads the row again soon; it is kept out of the caches' way
+    __device__ __forceinline__ void load_long(const T* row, int base, int lane, int dim, bool stream) {
+        auto plain = [&](int k, const T* p) { x[k] = *reinterpret_cast<const V*>(p); };
+        auto past = [&](int k, const T* p) { x[k] = __builtin_nontemporal_load(reinterpret_cast<const V*>(p)); };
+        if (base + COLUMNS > dim) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) plain(k, row + min(column(base, lane, k), dim - N));
+        } else if (stream) apart<1>([&] { each(row, base, lane, past); });
+        else apart<0>([&] { each(row, base, lane, plain); });
+    }
     __device__ __forceinline__ void load(const T* row, int base, int lane, int dim, bool stream) {
-        auto from = [&](int k) { return reinterpret_cast<const V*>(row + min(column(base, lane, k), dim - N)); };
-        if (dim >= N && stream) {
-#pragma unroll
-            for (int k = 0; k < PER; ++k) x[k] = __builtin_nontemporal_load(from(k));
-        } else if (dim >= N) {
-#pragma unroll
-            for (int k = 0; k < PER; ++k) x[k] = *from(k);
-        } else {
+        if (dim >= N) load_long(row, base, lane, dim, stream);
+        else {
 #pragma unroll
             for (int k = 0; k < PER; ++k)
 #pragma unroll
@@ -94,13 +115,42 @@ struct RowSlice {
         }
         return v;
     }
-    __device__ __forceinline__ float largest() const {
+    __device__ __forceinline__ float largest(int k) const {
         float m = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < PER; ++k)
-#pragma unroll
-            for (int e = 0; e < N; ++e) m = fmaxf(m, at(k, e));
+        for (int e = 0; e < N; e += 2) m = max3(m, at(k, e), at(k, e + 1));
         return m;
+    }
+    // (Elements of 16 bits are compared as integers, two at a time, without being converted.  In that order the numbers of sign 0 come as they are, above those of sign 1,
+    // which come the other way round: where all are of sign 1 the largest is the smallest of their bits.)
+    __device__ __forceinline__ float largest() const {
+        if constexpr (sizeof(T) == 2) {
+            typedef int16_t I2 __attribute__((ext_vector_type(2)));
+            typedef uint16_t U2 __attribute__((ext_vector_type(2)));
+            typedef uint32_t W __attribute__((ext_vector_type(4)));
+            auto pairs = [&](int k, auto f) {
+                const W w = __builtin_bit_cast(W, x[k]);
+                const uint32_t p[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f(p[j]);
+            };
+            I2 i = I2{INT16_MIN, INT16_MIN};
+#pragma unroll
+            for (int k = 0; k < PER; ++k) pairs(k, [&](uint32_t p) { i = __builtin_elementwise_max(i, __builtin_bit_cast(I2, p)); });
+            int16_t best = i[0] > i[1] ? i[0] : i[1];
+            if (best < 0) {
+                U2 u = U2{UINT16_MAX, UINT16_MAX};
+#pragma unroll
+                for (int k = 0; k < PER; ++k) pairs(k, [&](uint32_t p) { u = __builtin_elementwise_min(u, __builtin_bit_cast(U2, p)); });
+                best = (int16_t)(u[0] < u[1] ? u[0] : u[1]);
+            }
+            return (float)__builtin_bit_cast(T, best);
+        } else {
+            float m = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < PER; k += 2) m = max3(m, largest(k), largest(k + 1));
+            return m;
+        }
     }
     // sum of 2^(x c - off)
     __device__ __forceinline__ float exponentials(float c, float off) const {
@@ -114,13 +164,18 @@ struct RowSlice {
     // Stores the slice, whose elements are results by now, but for the row's last vector where that is not a whole one; that is the business of one lane of the row, at the
     // end (code for it at every vector is most of a kernel).
     __device__ __forceinline__ void store(T* row, int base, int lane, int dim, bool stream) const {
+auto plain = [&](int k, T* p) { *reinterpret_cast<V*>(p) = x[k]; };
+        auto past = [&](int k, T* p) { __builtin_nontemporal_store(x[k], reinterpret_cast<V*>(p)); };
+        if (base + COLUMNS <= dim) {
+            if (stream) apart<1>([&] { each(row, base, lane, past); });
+            else apart<0>([&] { each(row, base, lane, plain); });
+            return;
+        }
+        lane = here(lane);
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int col = column(base, lane, k);
-            if (col + N <= dim) {
-                V* p = reinterpret_cast<V*>(row + col);
-                if (stream) __builtin_nontemporal_store(x[k], p); else *p = x[k];
-            }
+            if (col + N <= dim) plain(k, row + col);
         }
         const int whole = dim - dim % N, last = (whole - base) / N;
         if (whole < dim && whole >= base && whole < base + COLUMNS && last % LANES == lane) {
