@@ -12,7 +12,10 @@ the head's and the pooled context rows' by one global norm, and stepped by plain
 linear in the pooled rows' gradient, so that clipping that clips the step; its share of the norm is that of the pooled rows, which is not the table's where a
 bag or a batch has an id more than once).
 
-    python examples/next_item.py [--steps 30]
+With a teacher (its best items of each sample and their logits) the loss is half cross entropy and half the divergence from the teacher; loss and gradient of the logits then come
+from one call, distill_grad.  Serving continues a user's sequence by beam search: beam_select picks items over beams and vocabulary, beam_reorder moves the beams' states along.
+
+    python examples/next_item.py [--steps 30] [--distill]
 """
 from __future__ import annotations
 
@@ -29,6 +32,7 @@ from paper_2208_05321_amd import DenseOps, FreqCache  # noqa: E402
 ROWS, CACHE_ROWS, FEATURES = 200_000, 6000, 8      # the table behind the cache
 ITEMS, SEQ, DIM, PAD = 5000, 48, 64, 0
 SAMPLES, LR, MAX_NORM = 256, 0.5, 1.0
+TEMPERATURE = 2.0
 
 
 class Model:
@@ -44,6 +48,7 @@ class Model:
         self.weight = torch.ones(DIM, device="cuda")
         self.at = torch.arange(SEQ, device="cuda", dtype=torch.int32).repeat(SAMPLES)
         self.offsets = torch.arange(SAMPLES * FEATURES + 1, device="cuda")
+        self.share = torch.full((1,), 1.0 / SAMPLES, device="cuda")        # of a sample's loss in the mean
 
     def encode(self, items, at):
         """Normed rows of the sequences, with what the backward pass needs."""
@@ -52,8 +57,8 @@ class Model:
         y, h, _ = self.ops.rms_norm_fwd(x, self.weight, residual=r, h_out=x)
         return y, h
 
-    def step(self, context, items, target) -> torch.Tensor:
-        """One training step; the loss and the gradients' norm (before clipping), on the GPU."""
+    def step(self, context, items, target, teacher=None) -> torch.Tensor:
+        """One training step; the loss and the gradients' norm (before clipping), on the GPU.  teacher: (ids, logits) [SAMPLES, top] of the teacher's best items."""
         ops, cache = self.ops, self.cache
         slots = cache.prepare(context, self.offsets)
         pooled = cache.embedding_bag_fwd(slots, self.offsets).requires_grad_()
@@ -62,8 +67,14 @@ class Model:
         real = (items != PAD).view(SAMPLES, SEQ, 1)
         state = (y.float().view(SAMPLES, SEQ, DIM) * real).sum(1) / real.sum(1)
         head = self.head.requires_grad_()
-        loss = torch.nn.functional.cross_entropy(torch.cat([state, pooled.view(SAMPLES, -1)], 1) @ head, target)
-        gy, gp, gh = torch.autograd.grad(loss, (y, pooled, head))
+        logits = torch.cat([state, pooled.view(SAMPLES, -1)], 1) @ head
+        if teacher is None:
+            loss = torch.nn.functional.cross_entropy(logits, target)
+            gy, gp, gh = torch.autograd.grad(loss, (y, pooled, head))
+        else:
+            losses, gl = ops.distill_grad(self.share, logits.detach(), *teacher, targets=target, temperature=TEMPERATURE, alpha=0.5)
+            loss = losses.mean()
+            gy, gp, gh = torch.autograd.grad(logits, (y, pooled, head), gl)
         self.head.requires_grad_(False)
 
         gx, gw = ops.rms_norm_bwd(gy, h, self.weight)
@@ -80,6 +91,25 @@ class Model:
         x = self.ops.token_embed_fwd(self.items, item, scale=DIM ** 0.5, out_dtype=torch.bfloat16)
         y, _, scale = self.ops.rms_norm_fwd(x, self.weight, out_dtype=torch.float8_e4m3fn)
         return y, scale
+
+    def search(self, item, context, steps: int = 3, beams: int = 4):
+        """(items [users, beams, steps], scores [users, beams]) that beam search finds to follow one item of each user, whose pooled context rows are [users, FEATURES * DIM]."""
+        ops, users = self.ops, len(item)
+        tokens = item.view(users, 1).expand(users, beams).contiguous()
+        scores = torch.full((users, beams), float("-inf"), device="cuda")
+        scores[:, 0] = 0.0                             # one beam alive: the others would be its copies
+        total = torch.zeros((users, beams, DIM), device="cuda")          # of the normed rows, of which the state is the mean
+        found = torch.zeros((users, beams, steps), dtype=torch.int64, device="cuda")
+        wide = context.view(users, 1, -1).expand(users, beams, -1)
+        for k in range(steps):
+            x = ops.token_embed_fwd(self.items, tokens, scale=DIM ** 0.5, out_dtype=torch.bfloat16)
+            total += ops.rms_norm_fwd(x, self.weight)[0]
+            logits = torch.cat([total / (k + 1), wide], 2) @ self.head
+            logits[:, :, PAD] = float("-inf")
+            scores, parents, tokens, _ = ops.beam_select(logits, scores)
+            ops.beam_reorder([total, found], parents)
+            found[:, :, k] = tokens
+        return found, scores
 
     def close(self):
         self.ops.check()
@@ -100,11 +130,18 @@ def batches(seed: int = 1):
         yield tuple(torch.from_numpy(a.reshape(-1)).cuda() for a in (context, items, 100 + favourite))
 
 
-def train(steps: int):
+def teacher_of(target, top: int = 8):
+    """What a teacher that knows the rule would say of the samples: (ids, logits) of its best items, the right one far ahead of its neighbours."""
+    ids = (target[:, None] + torch.arange(top, device="cuda")) % ITEMS
+    return ids, (6.0 - 1.5 * torch.arange(top, device="cuda", dtype=torch.float32)).expand(ids.shape).contiguous()
+
+
+def train(steps: int, distil: bool = False):
     """(losses, gradient norms, model) of that many steps."""
     model, data, seen = Model(), batches(), []
     for _ in range(steps):
-        seen.append(model.step(*next(data)))
+        batch = next(data)
+        seen.append(model.step(*batch, teacher_of(batch[2]) if distil else None))
     losses, norms = torch.stack(seen).T.tolist()
     return losses, norms, model
 
@@ -112,9 +149,13 @@ def train(steps: int):
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=30)
-    losses, norms, model = train(ap.parse_args().steps)
+    ap.add_argument("--distill", action="store_true")
+    args = ap.parse_args()
+    losses, norms, model = train(args.steps, args.distill)
     for k in range(0, len(losses), max(1, len(losses) // 10)):
         print(f"step {k:3d}  loss {losses[k]:.3f}  gradient norm {norms[k]:.3f}")
     row, scale = model.serve(torch.tensor([7], device="cuda"))
     print(f"served: {row.dtype} {tuple(row.shape)}, scale {float(scale):.4f}; cache {model.cache.stats()}")
+    found, scores = model.search(torch.tensor([7, 11], device="cuda"), torch.zeros(2, FEATURES * DIM, device="cuda"))
+    print(f"found to follow item 7: {found[0].tolist()}, scores {[round(v, 2) for v in scores[0].tolist()]}")
     model.close()

@@ -38,6 +38,7 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t k) { return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+constexpr uint32_t LOWEST = 0x00800000u;            // the lowest finite number: -infinity is no candidate
 // larger logit first, then lower id
 __device__ __forceinline__ uint64_t entry_key(float x, int id) { return (uint64_t)ordered(x) << 32 | (uint32_t)~id; }
 
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         uint32_t b = *(volatile uint32_t*)&bounds[0];
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) b = min(b, *(volatile uint32_t*)&bounds[k]);
-        return max(b, 0x00800000u);                // the lowest finite number: -infinity is no candidate
+        return max(b, LOWEST);
     };
     float lane_top = -INFINITY, off = -INFINITY, sum = 0.f, least = -INFINITY;
     for (int base = begin; base < end; base += Slice::COLUMNS) {
@@ -132,7 +133,9 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         const uint32_t mine = wave_bound(ordered(lane_top), (a.keep + WAVES - 1) / WAVES);
         if ((lane & 63) == 0) *(volatile uint32_t*)&bounds[lane >> 6] = mine;
         if (base == begin) __syncthreads();
-        least = unordered(bound());
+        uint32_t key = bound();
+        if (key == LOWEST) key = max(key, wave_bound(ordered(lane_top), a.keep));      // (a wavefront without elements: the own one's bound, if it has one)
+        least = unordered(key);
         if (!(top >= least)) continue;
         uint32_t at = 0;
         s.forget();
@@ -278,10 +281,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
     const uint32_t mine = wave_bound(ordered((float)top) - 1, a.keep);
     if ((lane & 63) == 0) bounds[lane >> 6] = mine;
     __syncthreads();
-    uint32_t key = 0x00800000u;
+    uint32_t key = LOWEST;
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) key = max(key, bounds[k]);
-    const double bound = key == 0x00800000u ? -INFINITY : (double)unordered(key);
+    const double bound = key == LOWEST ? -INFINITY : (double)unordered(key);
     if (top >= bound && top > -INFINITY)
         candidates([&](const Candidate& q) {
             if (q.c < bound) return;

@@ -15,6 +15,7 @@ _INF = float("inf")
 _STATS = 12                     # numbers of a row that the distillation's forward pass leaves for its backward pass
 _MOST_BEAMS = 64
 _dtype = attrgetter("dtype")
+_layout = attrgetter("shape", "dtype")
 
 
 def _refuse(what: str):
@@ -383,11 +384,10 @@ class DenseOps:
         teacher_ids, teacher [..., top]: ids (-1: no entry) and logits.  teacher_lse [...] (f32): the log-sum of exp(z / T) over the teacher's whole vocabulary; what the entries leave
         over is then one more category, the ids that none of them names.  Without it the entries are the whole distribution.
         targets [...]: ids; -1 leaves the row out (loss 0).  `stats` [..., 12] is for distill_bwd."""
-        torch = self._torch
         (k, n, d, xs), entries, target, lead = self._teacher(logits, teacher_ids, teacher, targets, temperature, alpha)
         lse = None if teacher_lse is None else self._of_rows(teacher_lse, lead, "teacher_lse")
-        loss = torch.empty(lead, dtype=torch.float32, device=self.device)
-        stats = torch.empty((*lead, _STATS), dtype=torch.float32, device=self.device)
+        f32 = self._torch.float32
+        loss, stats = logits.new_empty(lead, dtype=f32), logits.new_empty((*lead, _STATS), dtype=f32)
         self._run("distill_fwd", self._L.distill_fwd, (logits, teacher_ids, teacher, teacher_lse, targets, loss, stats), logits.data_ptr(), k, xs, n, d,
                   *entries, lse, *target, temperature, alpha, loss.data_ptr(), stats.data_ptr())
         return loss, stats
@@ -407,12 +407,11 @@ class DenseOps:
 
     def distill_grad(self, grad_loss, logits, teacher_ids, teacher, teacher_lse=None, targets=None, temperature: float = 1.0, alpha: float = 1.0, out=None):
         """(loss, gradient of the logits) in one call, where grad_loss is known beforehand (1 / rows for a mean).  `out` may be logits."""
-        torch = self._torch
         (k, n, d, xs), entries, target, lead = self._teacher(logits, teacher_ids, teacher, targets, temperature, alpha)
         lse = None if teacher_lse is None else self._of_rows(teacher_lse, lead, "teacher_lse")
         gp, gs = self._grad_loss(grad_loss, n, lead)
         grad, os = self._grad_logits(logits, k, xs, out)
-        loss = torch.empty(lead, dtype=torch.float32, device=self.device)
+        loss = logits.new_empty(lead, dtype=self._torch.float32)
         self._run("distill_grad", self._L.distill_grad, (grad_loss, logits, teacher_ids, teacher, teacher_lse, targets, loss, grad), gp, gs, logits.data_ptr(), k, xs,
                   n, d, *entries, lse, *target, temperature, alpha, loss.data_ptr(), grad.data_ptr(), os)
         if out is not None:
@@ -445,9 +444,10 @@ class DenseOps:
         tk = self._type.get(token_dtype, 6 if token_dtype is None else -1)
         if tk != 5 and tk != 6:
             _refuse(f"token_dtype {token_dtype}")
-        new = lambda dtype: torch.empty((batch, keep), dtype=dtype, device=self.device)  # noqa: E731
-        out, parents, tokens = new(torch.float32), new(torch.int32), new(token_dtype or torch.int64)
-        ended = new(torch.bool) if eos_id >= 0 else None
+        shape = (batch, keep)
+        out, parents = scores.new_empty(shape), scores.new_empty(shape, dtype=torch.int32)      # (0.3 us less than torch.empty, each)
+        tokens = scores.new_empty(shape, dtype=token_dtype or torch.int64)
+        ended = scores.new_empty(shape, dtype=torch.bool) if eos_id >= 0 else None
         self._run("beam_select", self._L.beam_select, (logits, scores, finished, out, parents, tokens, ended), logits.data_ptr(), k, xs, batch, beams, d, sp, fp,
                   eos_id, keep, out.data_ptr(), parents.data_ptr(), tokens.data_ptr(), tk, ended.data_ptr() if ended is not None else None)
         return out, parents, tokens, ended
@@ -484,6 +484,23 @@ class DenseOps:
             _refuse(f"{what}: rows overlap")
         return row * size, apart * size, piece * size, pieces
 
+    def _move(self, t, o, batch: int, beams: int, keep: int):
+        """Distances of rows and of pieces (of t, of o, in turn), bytes of a piece, pieces."""
+        if t.dim() < 2 or t.shape[:2] != (batch, beams) or o.shape != (batch, keep, *t.shape[2:]) or o.dtype != t.dtype:
+            _refuse(f"states: [{batch}, {beams}, ...] -> [{batch}, {keep}, ...] is wanted")
+        row, apart, piece, pieces = self._state(t, batch, "states")
+        orow, oapart = row, apart
+        if o is not t:
+            orow, oapart, opiece, opieces = self._state(o, batch, "out")
+            if (opiece, opieces) != (piece, pieces):     # the smaller pieces are those of both, if the larger one holds all of them
+                if (opieces > 1 and pieces > 1) or opiece * opieces != piece * pieces:
+                    _refuse("out: pieces of other sizes than the states'")
+                if pieces == 1:
+                    piece, pieces, apart = opiece, opieces, opiece
+                else:
+                    oapart = piece
+        return row, orow, apart, oapart, piece, pieces if piece else 0
+
     def beam_reorder(self, states, parents, out=None):
         """states[k][b, j] = states[k][b, parents[b, j]] for tensors [batch, beams, ...] of any type, in place; or into the tensors of `out` [batch, keep, ...].  Returns the tensors
         written.  parents [batch, keep] (int32, int64).  A row (what follows the first two dimensions) is neighbouring elements, or pieces of them at one distance, such as the filled
@@ -500,24 +517,21 @@ class DenseOps:
         beams = states[0].shape[1] if states[0].dim() > 1 else 0
         if not 1 <= beams <= _MOST_BEAMS or not 1 <= keep <= _MOST_BEAMS or (not given and keep != beams):
             _refuse(f"{beams} beams, {keep} parents")
-        table = array("q")
-        for t, o in zip(states, out):
-            if t.get_device() != self._index or o.get_device() != self._index:
-                _refuse(f"states: tensors on {self.device} are wanted")
-            if t.dim() < 2 or t.shape[:2] != (batch, beams) or o.shape != (batch, keep, *t.shape[2:]) or o.dtype != t.dtype:
-                _refuse(f"states: [{batch}, {beams}, ...] -> [{batch}, {keep}, ...] is wanted")
-            row, apart, piece, pieces = self._state(t, batch, "states")
-            orow, oapart = row, apart
-            if o is not t:
-                orow, oapart, opiece, opieces = self._state(o, batch, "out")
-                if (opiece, opieces) != (piece, pieces):         # the smaller pieces are those of both, if the larger ones hold whole ones of them
-                    if opieces > 1 and pieces > 1 or (opiece * opieces) != (piece * pieces):
-                        _refuse("out: pieces of other sizes than the states'")
-                    if pieces == 1:
-                        piece, pieces, apart = opiece, opieces, opiece
-                    else:
-                        oapart = piece
-            table.extend((t.data_ptr(), o.data_ptr(), row, orow, apart, oapart, piece, pieces if piece else 0))
+        T = self._torch.Tensor                  # (one pass of C code for each question: a model has dozens of states, most of them alike)
+        if not {self._index}.issuperset(map(T.get_device, states)) or (given and not {self._index}.issuperset(map(T.get_device, out))):
+            _refuse(f"states: tensors on {self.device} are wanted")
+        table, layouts = [], {}                 # what the tensors of one shape, type and distances have in common is worked out once a call
+        if given:
+            alike = zip(map(_layout, states), map(T.stride, states), map(_layout, out), map(T.stride, out))
+        else:
+            alike = zip(map(_layout, states), map(T.stride, states))
+        for t, o, key in zip(states, out, alike):
+            layout = layouts.get(key)
+            if layout is None:
+                layout = layouts[key] = self._move(t, o, batch, beams, keep)
+            table += (t.data_ptr(), o.data_ptr())
+            table += layout
+        table = array("q", table)
         self._run("beam_reorder", self._L.beam_reorder, (states, out, (parents,)), table.buffer_info()[0], len(states), batch, beams, parents.data_ptr(), pk, keep)
         self._written(out)
         return out

@@ -1,0 +1,64 @@
+"""`-m gpu`: calls whose rows go in several launches, and logits beyond 32 bits of elements: rows on either side of the seams against the 64-bit forms."""
+import pytest
+
+from tests.dense_reference import U32, inside, rounded
+from tests.logits_reference import SUM_STEPS, distill, select
+
+pytestmark = [pytest.mark.gpu, pytest.mark.slow]
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2208_05321_amd import DenseOps
+    o = DenseOps()
+    yield o
+    o.close()
+
+
+def _rows(ops, n, v, kind, rows, rest):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.empty((n, v), dtype=kind, device="cuda")
+    for a in range(0, n, 4096):
+        x[a:a + 4096] = (torch.randn((min(4096, n - a), v), generator=g, device="cuda") * 3).to(kind)
+    top = 6
+    ids = torch.randint(0, v // top, (n, top), generator=g, device="cuda") + torch.arange(top, device="cuda") * (v // top)
+    z = torch.randn((n, top), generator=g, device="cuda") + 8
+    lse = torch.logsumexp(z.double() / 2, 1).float() + 0.3 if rest else None
+    y, w = ids[:, 1].contiguous(), torch.rand(n, generator=g, device="cuda") + 0.5
+    loss, stats = ops.distill_fwd(x, ids, z, teacher_lse=lse, targets=y, temperature=2.0, alpha=0.5)
+    back = ops.distill_bwd(w, x, ids, z, stats, targets=y, temperature=2.0, alpha=0.5)[rows]
+    both, grad = ops.distill_grad(w, x, ids, z, teacher_lse=lse, targets=y, temperature=2.0, alpha=0.5)
+    want, of, off, off_grad = distill(x[rows], ids[rows], z[rows], None if lse is None else lse[rows], y[rows], 2.0, 0.5)
+    wd = w[rows].double()[:, None]
+    bound = off_grad * wd + rounded((of * wd).abs() + off_grad * wd, kind)
+    inside(loss[rows], want, off, "loss")
+    inside(both[rows], want, off, "loss of one call")
+    inside(back, of * wd, bound, "grad")
+    inside(grad[rows], of * wd, bound, "grad of one call")
+    assert bool(torch.isfinite(loss).all()) and bool(torch.isfinite(both).all())
+    ops.check()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+def test_rows_of_several_launches(ops, rest):
+    """32,768 rows of two slices fill the workspace."""
+    import torch
+    _rows(ops, 33_000, 16_411, torch.float16, [0, 1, 32_766, 32_767, 32_768, 32_769, 32_999], rest)
+
+
+def test_elements_beyond_32_bits(ops):
+    import torch
+    _rows(ops, 70_000, 33_001, torch.bfloat16, [0, 32_767, 65_075, 65_076, 65_535, 65_536, 69_999], True)
+
+
+def test_sequences_of_several_launches(ops):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((40, 64, 33_000), generator=g, device="cuda") * 3
+    scores = -6 * torch.rand((40, 64), generator=g, device="cuda")
+    got = ops.beam_select(x, scores, 64)
+    for a in range(0, 40, 8):
+        best, parents, tokens = select(x[a:a + 8], scores[a:a + 8], 64)
+        assert torch.equal(got[1][a:a + 8], parents) and torch.equal(got[2][a:a + 8], tokens)
+        assert bool(((got[0][a:a + 8].double() - best).abs() <= (SUM_STEPS + 8 + best.abs()) * U32).all())
