@@ -92,7 +92,14 @@ __device__ __forceinline__ double exponent(float z, float zmax, double it) { ret
 
 // Entries of a row in LDS: ids (-1: none that counts), the teacher's logits, and later probabilities, the student's logits.
 struct Entries { int* id; float* z; float* x; };
-__device__ __forceinline__ Entries entries_at(float* lds, int top) { return Entries{reinterpret_cast<int*>(lds), lds + top, lds + 2 * top}; }
+constexpr __host__ __device__ int entries_room(int top) { return (top + 3) & ~3; }        // (ids are looked through four at a time)
+__device__ __forceinline__ Entries entries_at(float* lds, int sub, int top) {
+    const int room = entries_room(top);
+    lds += (size_t)sub * 3 * room;
+    return Entries{reinterpret_cast<int*>(lds), lds + room, lds + 2 * room};
+}
+// the places behind the last entry
+__device__ __forceinline__ void end_entries(const Entries& t, int lane, int top) { if (top + lane < entries_room(top)) t.id[top + lane] = -1; }
 template <class T, int LANES>
 __device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t row, int lane, const T* x, const Entries& t) {
     for (int k = lane; k < a.top; k += LANES) {
@@ -103,6 +110,7 @@ __device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t row, 
         t.z[k] = z;
         t.x[k] = id >= 0 ? (float)x[id] : 0.f;
     }
+    end_entries(t, lane, a.top);
 }
 
 // What a wavefront makes of a row's sums and entries (xy: the target's logit): its loss and the numbers for the backward pass.  The entries' logits become their probabilities.
@@ -302,10 +310,18 @@ __device__ __forceinline__ void mend(const DistillArgs& a, float g, const float*
     for (int k = lane; k < entries; k += LANES) {
         const int id = t.id[k];
         if (id < base || id >= end) continue;
-        float sum = 0.f;
+        int times = 0;
+        for (int j = 0; j < entries; j += 4) {
+            const int4 q = *reinterpret_cast<const int4*>(t.id + j);
+            times += (q.x == id) + (q.y == id) + (q.z == id) + (q.w == id);
+        }
+        float sum = t.z[k];
         bool first = true;
-        for (int j = 0; j < entries; ++j)
-            if (t.id[j] == id) { first &= j >= k; sum += t.z[j]; }
+        if (times > 1) {
+            sum = 0.f;
+            for (int j = 0; j < entries; ++j)
+                if (t.id[j] == id) { first &= j >= k; sum += t.z[j]; }
+        }
         y_named |= id == y;
         if (!first) continue;
         const float q = exp2f(fmaf(t.x[k], ct, -st[ST_ALL])) * st[ST_INV], q1 = a.alpha < 1.f ? exp2f(fmaf(t.x[k], LOG2E, -st[ST_ALL1])) * st[ST_INV1] : 0.f;
@@ -339,7 +355,7 @@ __global__ __launch_bounds__(distill_threads(LANES)) __attribute__((amdgpu_waves
                                                                         float* __restrict__ stats, T* grad, int64_t grad_stride) {
     using Slice = RowSlice<T, LANES, PER>;
     constexpr int ROWS = distill_threads(LANES) / LANES;
-    extern __shared__ float dynamic[];             // entries
+    extern __shared__ __align__(16) float dynamic[];             // entries
     __shared__ Marks<LANES, PER> marks[ROWS];
     __shared__ Sums lds[distill_threads(LANES) / 64];
     __shared__ float row_stats[ROWS][STATS];
@@ -357,7 +373,7 @@ __global__ __launch_bounds__(distill_threads(LANES)) __attribute__((amdgpu_waves
         if (grad) store_zeros<T, LANES, PER>(out, 0, lane, a.dim);
         return;
     }
-    const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
+    const Entries t = entries_at(dynamic, sub, a.top);
     load_entries<T, LANES>(a, row, lane, x, t);
     const float xy = y >= 0 ? (float)x[y] : 0.f;
     const bool rest = a.lse && a.alpha > 0.f;
@@ -423,7 +439,7 @@ __device__ __forceinline__ RowSums row_sums(const DistillArgs& a, const RowSums*
 // The rows of several slices: a wavefront to a row.
 template <class T>
 __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_join(DistillArgs a, int slices, const RowSums* __restrict__ part, float* __restrict__ loss, float* __restrict__ stats) {
-    extern __shared__ float dynamic[];
+    extern __shared__ __align__(16) float dynamic[];
     __shared__ float row_stats[LOGIT_THREADS / 64][STATS];
     const int lane = threadIdx.x & 63, sub = threadIdx.x / 64;
     const int64_t row = (int64_t)blockIdx.x * (LOGIT_THREADS / 64) + sub;
@@ -432,7 +448,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_join(DistillArgs a, i
     const RowSums r = row_sums(a, part, row, slices);
     int y;
     if (!row_target(a, row, &y)) { distill_left_out(row, lane, loss, stats); return; }
-    const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
+    const Entries t = entries_at(dynamic, sub, a.top);
     load_entries<T, 64>(a, row, lane, x, t);
     const float xy = y >= 0 ? (float)x[y] : 0.f;
     row_sync<64>();
@@ -451,7 +467,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, in
     using Slice = RowSlice<T, LANES, PER>;
     constexpr int ROWS = LOGIT_THREADS / LANES;
     static_assert(!PARTS || ROWS == 1);
-    extern __shared__ float dynamic[];
+    extern __shared__ __align__(16) float dynamic[];
     __shared__ float row_stats[PARTS ? STATS : 1];
     const int lane = threadIdx.x % LANES, sub = LANES == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : threadIdx.x / LANES;
     const int64_t row = (int64_t)(blockIdx.x / slices) * ROWS + sub;
@@ -463,7 +479,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, in
     s.load(x, base, lane, a.dim, stream);
     const float g = grad_loss[row * grad_loss_stride];
     const int end = min(a.dim, base + Slice::COLUMNS);
-    const Entries t = entries_at(dynamic + (size_t)sub * 3 * a.top, a.top);
+    const Entries t = entries_at(dynamic, sub, a.top);
     const float* st = PARTS ? row_stats : stats + row * STATS;
     int y = -1;
     float xy = 0.f;
@@ -492,6 +508,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, in
                 t.x[k] = (float)x[id];
             }
         }
+        end_entries(t, lane, a.top);
         if (a.target && a.alpha < 1.f) {
             y = (int)load_id(a.target, a.target_type, row);
             if (y >= base && y < end) xy = (float)x[y];
@@ -515,6 +532,7 @@ void by_slice(int64_t vectors, F f) {
     using std::integral_constant;
     if (vectors <= 64 * 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
     else if (vectors <= 64 * 8) f(integral_constant<int, 64>(), integral_constant<int, 8>());
+    else if (vectors <= 256 * 4) f(integral_constant<int, 256>(), integral_constant<int, 4>());
     else f(integral_constant<int, 256>(), integral_constant<int, 8>());
 }
 // the same for rows that one workgroup holds
@@ -524,6 +542,7 @@ void by_row(int64_t vectors, F f) {
     using std::integral_constant;
     if (vectors <= 64 * 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
     else if (vectors <= 64 * 8) f(integral_constant<int, 64>(), integral_constant<int, 8>());
+    else if (vectors <= 256 * 4) f(integral_constant<int, 256>(), integral_constant<int, 4>());
     else if (vectors <= 256 * 8) f(integral_constant<int, 256>(), integral_constant<int, 8>());
     else if (vectors <= 512 * 8) f(integral_constant<int, 512>(), integral_constant<int, 8>());
     else if (vectors <= 1024 * 8) f(integral_constant<int, 1024>(), integral_constant<int, 8>());
@@ -561,7 +580,7 @@ constexpr int64_t DISTILL_FEW = 64;
 // 100 of 30,000 bf16 11.7 / 14.7.
 static bool in_one_workgroup(const DistillCall& c, int64_t vectors) {
     if (c.bwd) return vectors <= 512 * 8 || (vectors <= ROW_MOST && c.a.n >= DISTILL_FEW);
-    return vectors <= 64 * 8 || (vectors <= 512 * 8 && c.a.n <= 1024);
+    return vectors <= 256 * 4 || (vectors <= 512 * 8 && c.a.n <= 1024);
 }
 
 template <class T>
@@ -570,7 +589,7 @@ int distill_run(const DistillCall& c) {
     const DistillArgs& a = c.a;
     const hipStream_t st = c.d->stream;
     const int64_t vectors = cdiv(a.dim, N);
-    const size_t entry_bytes = (size_t)a.top * 12;
+    const size_t entry_bytes = (size_t)entries_room(a.top) * 12;
     // Logits that the memory-side cache does not hold until the next pass (256 MB, the gradient among them) stay out of its way.  us: 8192 rows of 131,072 bf16 (2.1 GB), loss
     // 373 / 363; 4096 such rows, loss and then gradient 580 / 574; 777 of 50,021 f16 (78 MB) 74 / 81.
     const bool stream = a.n * a.dim * (int64_t)sizeof(T) > (int64_t)128 << 20;
@@ -605,7 +624,7 @@ int distill_run(const DistillCall& c) {
                     b, slices, stream, part, c.loss ? c.loss + at : nullptr, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats, (T*)c.grad + at * c.grad_stride,
                     c.grad_stride);
             };
-            if constexpr (LANES == LOGIT_THREADS)
+            if constexpr (LANES == LOGIT_THREADS && PER != 4)      // (shorter rows have gone the other way)
                 if (c.fwd) {
                     k_distill_slice<T, LANES, PER><<<blocks, LOGIT_THREADS, 0, st>>>(b, slices, stream, part);
                     if (c.bwd && !c.stats && a.n < DISTILL_FEW && c.grad != a.x) { backward(std::true_type()); continue; }

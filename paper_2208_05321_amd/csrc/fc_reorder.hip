@@ -31,25 +31,26 @@ template <> struct Chunk<1> { typedef uint8_t V; };
 
 struct Moves { int from[STATE_MOST_BEAMS], to[STATE_MOST_BEAMS]; int count, none; };       // none: rows that become zeros, listed from the end of `to`
 
-// Every move of one chunk of the rows: all rows are read before one is written, as in place a row may be another's source.
+// Moves [begin, begin + n) of one chunk of the rows: all rows are read before one is written, as in place a row may be another's source.
 template <int BYTES, int MOST>
-__device__ __forceinline__ void move_chunk(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, int n, bool stream) {
+__device__ __forceinline__ void move_chunk(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, int begin, int n, bool stream) {
     typename Chunk<BYTES>::V v[MOST];
 #pragma unroll
     for (int i = 0; i < MOST; ++i)
-        v[i] = *reinterpret_cast<const typename Chunk<BYTES>::V*>(src + __builtin_amdgcn_readfirstlane(m.from[min(i, n - 1)]) * src_row);
+        v[i] = *reinterpret_cast<const typename Chunk<BYTES>::V*>(src + __builtin_amdgcn_readfirstlane(m.from[begin + min(i, n - 1)]) * src_row);
     using V = typename Chunk<BYTES>::V;
     auto each = [&](auto f) {
 #pragma unroll
         for (int i = 0; i < MOST; ++i)
-            if (i < n) f(i, dst + __builtin_amdgcn_readfirstlane(m.to[i]) * dst_row);
+            if (i < n) f(i, dst + __builtin_amdgcn_readfirstlane(m.to[begin + i]) * dst_row);
     };
     if (stream) apart<1>([&] { each([&](int i, char* o) { __builtin_nontemporal_store(v[i], reinterpret_cast<V*>(o)); }); });
     else apart<0>([&] { each([&](int i, char* o) { *reinterpret_cast<V*>(o) = v[i]; }); });
 }
 template <int BYTES, int MOST>
 __device__ __forceinline__ void move_rows(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, bool stream) {
-    if (m.count) move_chunk<BYTES, MOST>(src, dst, src_row, dst_row, m, m.count, stream);
+    const int count = __builtin_amdgcn_readfirstlane(m.count);
+    for (int k = 0; k < count; k += MOST) move_chunk<BYTES, MOST>(src, dst, src_row, dst_row, m, k, min(MOST, count - k), stream);
     for (int i = 0; i < m.none; ++i) *reinterpret_cast<typename Chunk<BYTES>::V*>(dst + m.to[STATE_MOST_BEAMS - 1 - i] * dst_row) = typename Chunk<BYTES>::V{};
 }
 template <int MOST>
@@ -101,7 +102,8 @@ __global__ __launch_bounds__(STATE_THREADS) void k_beam_reorder(StateGroup g, in
     const char* src = t.src + seq * beams * t.src_row;
     char* dst = t.dst + seq * keep * t.dst_row;
     const int n = __builtin_amdgcn_readfirstlane(m.count);
-    if (n <= 8) move_tile<8>(t, src, dst, tile, m, stream);
+    // In place all of a sequence's moves go at once, else eight at a time.
+    if (n <= 8 || !in_place) move_tile<8>(t, src, dst, tile, m, stream);
     else if (n <= 16) move_tile<16>(t, src, dst, tile, m, stream);
     else if (n <= 32) move_tile<32>(t, src, dst, tile, m, stream);
     else move_tile<64>(t, src, dst, tile, m, stream);
