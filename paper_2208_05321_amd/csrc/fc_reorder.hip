@@ -1,18 +1,22 @@
 // Reordering of the states of beams: row (b, j) becomes row (b, parent[b, j]), for a list of tensors, in place or into others.
 //
 // A copy, bound by HBM: what is read are the distinct parents of the rows that change, what is written those rows.  A thread owns 16 bytes of every beam's row of a
-// sequence (8 or 4 where more than 16 or 32 of them move) and reads all of them before it writes one, so that in place a row may be another's
-// source in any pattern, without a second buffer or a wait between workgroups.  Rows that stay are not touched.
+// sequence (8 or 4 where there are more than 16 or 32 of them) and reads all of them before it writes one, so that in place a row may be another's
+// source in any pattern, without a second buffer or a wait between workgroups.  Rows that stay are not touched.  16 sequences of 8 beams, 24 tensors of 512 KB a row in
+// place (2.3 GB that must move): 435 us, 5.4 TB/s.
 #include "dense_device.h"
 
 #include <algorithm>
+
+#include <type_traits>
 
 namespace fc {
 
 constexpr int STATE_THREADS = 256;
 constexpr int STATE_MOST_BEAMS = 64;
 constexpr int STATE_GROUP = 44;                    // tensors that one launch's arguments can describe
-// Vectors of 16 bytes of a row that a workgroup moves, for every beam.  us, 256 / 1024: the same rows 422 / 430; one sequence of 4 beams 47.0 / 46.5.
+// Vectors of 16 bytes of a row that a workgroup moves, for every beam.  us, 256 / 512 / 1024: 16 sequences of 8 beams, 24 tensors of 512 KB a row in place 438 / 447 / 456, one
+// sequence of 4 beams (17 tensors of 30 KB; host) 20.5 / 20.7 / 20.5.
 constexpr int STATE_TILE = 256;
 struct StateRows {
     const char* src;
@@ -29,29 +33,32 @@ template <> struct Chunk<4> { typedef uint32_t V __attribute__((aligned(1))); };
 template <> struct Chunk<2> { typedef uint16_t V __attribute__((aligned(1))); };
 template <> struct Chunk<1> { typedef uint8_t V; };
 
-struct Moves { int from[STATE_MOST_BEAMS], to[STATE_MOST_BEAMS]; int count, none; };       // none: rows that become zeros, listed from the end of `to`
+struct Moves { int64_t from[STATE_MOST_BEAMS], to[STATE_MOST_BEAMS]; int count, none; };   // in bytes; none: rows that become zeros, listed from the end of `to`
+__device__ __forceinline__ int64_t same(int64_t x) {          // of a number that all lanes have: in scalar registers
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
 
 // Moves [begin, begin + n) of one chunk of the rows: all rows are read before one is written, as in place a row may be another's source.
 template <int BYTES, int MOST>
-__device__ __forceinline__ void move_chunk(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, int begin, int n, bool stream) {
+__device__ __forceinline__ void move_chunk(const char* src, char* dst, const Moves& m, int begin, int n, bool stream) {
     typename Chunk<BYTES>::V v[MOST];
 #pragma unroll
     for (int i = 0; i < MOST; ++i)
-        v[i] = *reinterpret_cast<const typename Chunk<BYTES>::V*>(src + __builtin_amdgcn_readfirstlane(m.from[begin + min(i, n - 1)]) * src_row);
+        v[i] = *reinterpret_cast<const typename Chunk<BYTES>::V*>(src + same(m.from[begin + min(i, n - 1)]));
     using V = typename Chunk<BYTES>::V;
     auto each = [&](auto f) {
 #pragma unroll
         for (int i = 0; i < MOST; ++i)
-            if (i < n) f(i, dst + __builtin_amdgcn_readfirstlane(m.to[begin + i]) * dst_row);
+            if (i < n) f(i, dst + same(m.to[begin + i]));
     };
     if (stream) apart<1>([&] { each([&](int i, char* o) { __builtin_nontemporal_store(v[i], reinterpret_cast<V*>(o)); }); });
     else apart<0>([&] { each([&](int i, char* o) { *reinterpret_cast<V*>(o) = v[i]; }); });
 }
 template <int BYTES, int MOST>
-__device__ __forceinline__ void move_rows(const char* src, char* dst, int64_t src_row, int64_t dst_row, const Moves& m, bool stream) {
+__device__ __forceinline__ void move_rows(const char* src, char* dst, const Moves& m, bool stream) {
     const int count = __builtin_amdgcn_readfirstlane(m.count);
-    for (int k = 0; k < count; k += MOST) move_chunk<BYTES, MOST>(src, dst, src_row, dst_row, m, k, min(MOST, count - k), stream);
-    for (int i = 0; i < m.none; ++i) *reinterpret_cast<typename Chunk<BYTES>::V*>(dst + m.to[STATE_MOST_BEAMS - 1 - i] * dst_row) = typename Chunk<BYTES>::V{};
+    for (int k = 0; k < count; k += MOST) move_chunk<BYTES, MOST>(src, dst, m, k, min(MOST, count - k), stream);
+    for (int i = 0; i < m.none; ++i) *reinterpret_cast<typename Chunk<BYTES>::V*>(dst + same(m.to[STATE_MOST_BEAMS - 1 - i])) = typename Chunk<BYTES>::V{};
 }
 template <int MOST>
 __device__ __forceinline__ void move_tile(const StateRows& t, const char* src, char* dst, int tile, const Moves& m, bool stream) {
@@ -63,16 +70,18 @@ __device__ __forceinline__ void move_tile(const StateRows& t, const char* src, c
         uint32_t at = (v - piece * t.per) * 16 + i % SPLIT * BYTES;
         const char* s = src + piece * t.src_piece;
         char* o = dst + piece * t.dst_piece;
-        if (at + BYTES <= t.piece) { move_rows<BYTES, MOST>(s + at, o + at, t.src_row, t.dst_row, m, stream); continue; }
+        if (at + BYTES <= t.piece) { move_rows<BYTES, MOST>(s + at, o + at, m, stream); continue; }
         if (at >= t.piece) continue;
         const uint32_t left = t.piece - at;
-        if (BYTES > 8 && left & 8) { move_rows<8, MOST>(s + at, o + at, t.src_row, t.dst_row, m, stream); at += 8; }
-        if (BYTES > 4 && left & 4) { move_rows<4, MOST>(s + at, o + at, t.src_row, t.dst_row, m, stream); at += 4; }
-        if (left & 2) { move_rows<2, MOST>(s + at, o + at, t.src_row, t.dst_row, m, stream); at += 2; }
-        if (left & 1) move_rows<1, MOST>(s + at, o + at, t.src_row, t.dst_row, m, stream);
+        if (BYTES > 8 && left & 8) { move_rows<8, MOST>(s + at, o + at, m, stream); at += 8; }
+        if (BYTES > 4 && left & 4) { move_rows<4, MOST>(s + at, o + at, m, stream); at += 4; }
+        if (left & 2) { move_rows<2, MOST>(s + at, o + at, m, stream); at += 2; }
+        if (left & 1) move_rows<1, MOST>(s + at, o + at, m, stream);
     }
 }
 
+// MOST: moves of a sequence that go at once: all of them where they are in place, else eight.
+template <int MOST>
 __global__ __launch_bounds__(STATE_THREADS) void k_beam_reorder(StateGroup g, int64_t first, bool stream, const void* __restrict__ parents, int32_t parent_type, int beams, int keep,
                                                                 uint32_t* __restrict__ flags) {
     __shared__ Moves m;
@@ -94,19 +103,14 @@ __global__ __launch_bounds__(STATE_THREADS) void k_beam_reorder(StateGroup g, in
         if (j < keep && !known) atomicOr(flags, (uint32_t)EF_ID_RANGE);
         const bool moves = known && !(in_place && p == j), none = j < keep && !known && !in_place;
         const uint64_t mm = __ballot(moves), nn = __ballot(none), below = ((uint64_t)1 << j) - 1;
-        if (moves) { const int k = __popcll(mm & below); m.from[k] = (int)p; m.to[k] = j; }
-        if (none) m.to[STATE_MOST_BEAMS - 1 - __popcll(nn & below)] = j;
+        if (moves) { const int k = __popcll(mm & below); m.from[k] = p * t.src_row; m.to[k] = j * t.dst_row; }
+        if (none) m.to[STATE_MOST_BEAMS - 1 - __popcll(nn & below)] = j * t.dst_row;
         if (j == 0) { m.count = __popcll(mm); m.none = __popcll(nn); }
     }
     __syncthreads();
     const char* src = t.src + seq * beams * t.src_row;
     char* dst = t.dst + seq * keep * t.dst_row;
-    const int n = __builtin_amdgcn_readfirstlane(m.count);
-    // In place all of a sequence's moves go at once, else eight at a time.
-    if (n <= 8 || !in_place) move_tile<8>(t, src, dst, tile, m, stream);
-    else if (n <= 16) move_tile<16>(t, src, dst, tile, m, stream);
-    else if (n <= 32) move_tile<32>(t, src, dst, tile, m, stream);
-    else move_tile<64>(t, src, dst, tile, m, stream);
+    move_tile<MOST>(t, src, dst, tile, m, stream);
 }
 
 }  // namespace fc
@@ -132,17 +136,28 @@ int beam_reorder(fc_dense* d, const fc_state* states, int32_t count, int64_t bat
     if (batch == 0) return FC_OK;
     FC_HIP(hipSetDevice(d->device));
     int64_t bytes = 0;
-    for (int32_t k = 0; k < count; ++k) bytes += states[k].piece_bytes * states[k].pieces * batch * keep;
-    // What the memory-side cache would not hold until it is read is stored past it: 16 x 8 rows of 512 KB of 24 tensors (1.6 GB) 422 / 392 us.  (Loads past it as well: 409, as a
-    // row may have several takers.)
+    bool in_place = false;
+    for (int32_t k = 0; k < count; ++k) {
+        bytes += states[k].piece_bytes * states[k].pieces * batch * keep;
+        in_place |= states[k].src == states[k].dst;
+    }
+    // What the memory-side cache would not hold until it is read is stored past it: 16 x 8 rows of 512 KB of 24 tensors (1.6 GB) 446 / 434 us.  (Loads past it as well: 4 % more, as
+    // a row may have several takers.)
     const bool stream = bytes > (int64_t)128 << 20;
     StateGroup g;
     g.count = 0;
     int64_t blocks = 0;
     auto launch = [&]() {
         const int64_t most = LAUNCH_THREADS / STATE_THREADS;
-        for (int64_t at = 0; at < blocks; at += most)
-            k_beam_reorder<<<(unsigned)std::min(most, blocks - at), STATE_THREADS, 0, d->stream>>>(g, at, stream, parents_dev, parent_type, beams, keep, d->flags);
+        auto go = [&](auto moves) {
+            for (int64_t at = 0; at < blocks; at += most)
+                k_beam_reorder<decltype(moves)::value><<<(unsigned)std::min(most, blocks - at), STATE_THREADS, 0, d->stream>>>(g, at, stream, parents_dev, parent_type, beams, keep,
+                                                                                                                              d->flags);
+        };
+        if (!in_place || keep <= 8) go(std::integral_constant<int, 8>());
+        else if (keep <= 16) go(std::integral_constant<int, 16>());
+        else if (keep <= 32) go(std::integral_constant<int, 32>());
+        else go(std::integral_constant<int, 64>());
         g.count = 0;
         blocks = 0;
     };
