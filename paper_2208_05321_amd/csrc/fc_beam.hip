@@ -112,9 +112,9 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     s.load(x, begin, lane, a.dim, true);
     if (lane == 0) count = kept = 0;
     auto bound = [&]() {
-        uint32_t b = *(volatile uint32_t*)&bounds[0];
+        uint32_t b = __hip_atomic_load(&bounds[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k) b = min(b, *(volatile uint32_t*)&bounds[k]);
+        for (int k = 1; k < WAVES; ++k) b = min(b, __hip_atomic_load(&bounds[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         return max(b, LOWEST);
     };
     float lane_top = -INFINITY, off = -INFINITY, sum = 0.f, least = -INFINITY;
@@ -131,16 +131,14 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         lane_top = fmaxf(lane_top, top);
         if (base > begin && !__any(top >= least)) continue;
         const uint32_t mine = wave_bound(ordered(lane_top), (a.keep + WAVES - 1) / WAVES);
-        if ((lane & 63) == 0) *(volatile uint32_t*)&bounds[lane >> 6] = mine;
+        if ((lane & 63) == 0) __hip_atomic_store(&bounds[lane >> 6], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         if (base == begin) __syncthreads();
         uint32_t key = bound();
         if (key == LOWEST) key = max(key, wave_bound(ordered(lane_top), a.keep));      // (a wavefront without elements: the own one's bound, if it has one)
         least = unordered(key);
         if (!(top >= least)) continue;
-        uint32_t at = 0;
         s.forget();
-#pragma unroll
-        for (int k = 0; k < PER; ++k) if (s.largest(k) >= least) at |= 1u << k;
+        uint32_t at = s.vectors_from(least);
         while (at) {
             const int k = __builtin_ctz(at);
             at &= at - 1;

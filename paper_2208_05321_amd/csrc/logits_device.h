@@ -121,22 +121,28 @@ struct RowSlice {
         for (int e = 0; e < N; e += 2) m = max3(m, at(k, e), at(k, e + 1));
         return m;
     }
-    // (Elements of 16 bits are compared as integers, two at a time, without being converted.  In that order the numbers of sign 0 come as they are, above those of sign 1,
-    // which come the other way round: where all are of sign 1 the largest is the smallest of their bits.)
+    // The largest element.  (Elements of 16 bits are compared as integers, two at a time, without being converted.  In that order the numbers of sign 0 come as they are, above
+    // those of sign 1, which come the other way round: where all are of sign 1 the largest is the smallest of their bits.)
+    typedef int16_t I2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t U2 __attribute__((ext_vector_type(2)));
+    template <class F>
+    __device__ __forceinline__ void pairs(int k, F f) const {
+        typedef uint32_t W __attribute__((ext_vector_type(4)));
+        const W w = __builtin_bit_cast(W, x[k]);
+        const uint32_t p[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f(p[j]);
+    }
+    __device__ __forceinline__ I2 largest_pair(int k) const {
+        I2 i = I2{INT16_MIN, INT16_MIN};
+        pairs(k, [&](uint32_t p) { i = __builtin_elementwise_max(i, __builtin_bit_cast(I2, p)); });
+        return i;
+    }
     __device__ __forceinline__ float largest() const {
         if constexpr (sizeof(T) == 2) {
-            typedef int16_t I2 __attribute__((ext_vector_type(2)));
-            typedef uint16_t U2 __attribute__((ext_vector_type(2)));
-            typedef uint32_t W __attribute__((ext_vector_type(4)));
-            auto pairs = [&](int k, auto f) {
-                const W w = __builtin_bit_cast(W, x[k]);
-                const uint32_t p[4] = {w.x, w.y, w.z, w.w};
+            I2 i = largest_pair(0);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) f(p[j]);
-            };
-            I2 i = I2{INT16_MIN, INT16_MIN};
-#pragma unroll
-            for (int k = 0; k < PER; ++k) pairs(k, [&](uint32_t p) { i = __builtin_elementwise_max(i, __builtin_bit_cast(I2, p)); });
+            for (int k = 1; k < PER; ++k) i = __builtin_elementwise_max(i, largest_pair(k));
             int16_t best = i[0] > i[1] ? i[0] : i[1];
             if (best < 0) {
                 U2 u = U2{UINT16_MAX, UINT16_MAX};
@@ -151,6 +157,23 @@ struct RowSlice {
             for (int k = 0; k < PER; k += 2) m = max3(m, largest(k), largest(k + 1));
             return m;
         }
+    }
+    // A bit for each vector that has an element of `least` or more.
+    __device__ __forceinline__ uint32_t vectors_from(float least) const {
+        uint32_t at = 0;
+        if constexpr (sizeof(T) == 2)
+            if (least > 0.f) {                     // (all of sign 0, then: integers again)
+                const T t = (T)least;
+                const int16_t below = (int16_t)(__builtin_bit_cast(int16_t, t) - ((float)t >= least ? 1 : 0));
+                const I2 b = I2{below, below};
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (__builtin_bit_cast(uint32_t, __builtin_elementwise_max(largest_pair(k), b)) != __builtin_bit_cast(uint32_t, b)) at |= 1u << k;
+                return at;
+            }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) if (largest(k) >= least) at |= 1u << k;
+        return at;
     }
     // sum of 2^(x c - off)
     __device__ __forceinline__ float exponentials(float c, float off) const {
