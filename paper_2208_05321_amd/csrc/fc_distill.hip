@@ -458,10 +458,10 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_join(DistillArgs a, i
 }
 
 // The gradient of a slice.  It may take the place of the logits: a slice is read, its entries among it, before any of it is written.
-// PARTS: the row's slices have not been joined; every workgroup does that for itself, which saves few rows a launch, and the first slice's stores the loss.  Not in place: a
+// PARTS: the row's sums of slices (`parts` of them) have not been joined; every workgroup does that for itself, which saves few rows a launch, and the first slice's stores the loss.  Not in place: a
 // workgroup reads all of the row's entries, when others may have stored their slices.
 template <class T, int LANES, int PER, bool PARTS>
-__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, int slices, bool stream, const RowSums* __restrict__ part, float* __restrict__ loss,
+__global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, int slices, bool stream, const RowSums* __restrict__ part, int parts, float* __restrict__ loss,
                                                                const float* __restrict__ grad_loss, int64_t grad_loss_stride, const float* __restrict__ stats, T* grad,
                                                                int64_t grad_stride) {
     using Slice = RowSlice<T, LANES, PER>;
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_bwd(DistillArgs a, in
         load_entries<T, LANES>(a, row, lane, x, t);
         if (y >= 0) xy = (float)x[y];
         __syncthreads();
-        if (lane < 64) distill_row(a, row, xy, row_sums(a, part, row, slices), t, slice == 0 ? loss : nullptr, row_stats);
+        if (lane < 64) distill_row(a, row, xy, row_sums(a, part, row, parts), t, slice == 0 ? loss : nullptr, row_stats);
         __syncthreads();
         if (st[ST_KIND] == ROW_OUT || g == 0.f) { store_zeros<T, LANES, PER>(out, base, lane, a.dim); return; }
     } else {
@@ -526,14 +526,25 @@ constexpr int64_t DISTILL_SLICES = 1 << 16;
 constexpr size_t DISTILL_WORK = DISTILL_SLICES * (sizeof(RowSums) + STATS * sizeof(float));
 size_t distill_work_bytes() { return DISTILL_WORK; }
 
-// f(lanes of a slice, vectors of a lane), as constants, for rows of `vectors`
+// f(lanes of a slice, vectors of a lane), as constants, for the gradient of n rows of `vectors`.  Slices of 4 vectors a lane, or of 2 where those are fewer than four workgroups a
+// compute unit.  us, 8 / 4: 4096 rows of 131,072 bf16 363 / 353, 2000 182 / 170, 3000 of 50,021 155 / 115, 777 f16 38 / 31, 8000 of 30,000 bf16 165 / 161.
 template <class F>
-void by_slice(int64_t vectors, F f) {
+void by_slice(int64_t n, int64_t vectors, F f) {
     using std::integral_constant;
     if (vectors <= 64 * 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
     else if (vectors <= 64 * 8) f(integral_constant<int, 64>(), integral_constant<int, 8>());
-    else if (vectors <= 256 * 4) f(integral_constant<int, 256>(), integral_constant<int, 4>());
-    else f(integral_constant<int, 256>(), integral_constant<int, 8>());
+    else if (n * cdiv(vectors, 256 * 4) < 1024) f(integral_constant<int, 256>(), integral_constant<int, 2>());
+    else f(integral_constant<int, 256>(), integral_constant<int, 4>());
+}
+// f(vectors of a lane) for the sums of rows of more than 1024 vectors.  Slices of 8, or of 4 where the last one of 8 would be half empty, or more, among five at most, or of 2
+// where there are few.  us, 8 / 4: 4096 rows of 131,072 bf16 193 / 215, 8000 of 30,000 77 / 94, 4000 of 100,000 f32 228 / 240, but 3000 of 50,021 bf16 75 / 60.
+template <class F>
+void by_part(int64_t n, int64_t vectors, F f) {
+    using std::integral_constant;
+    const int64_t eights = cdiv(vectors, LOGIT_THREADS * 8);
+    if (n * eights < 512) f(integral_constant<int, 2>());
+    else if (eights <= 5 && cdiv(vectors, LOGIT_THREADS * 4) % 2 == 1) f(integral_constant<int, 4>());
+    else f(integral_constant<int, 8>());
 }
 // the same for rows that one workgroup holds
 constexpr int64_t ROW_MOST = 1024 * 16;
@@ -610,32 +621,37 @@ int distill_run(const DistillCall& c) {
     if (c.fwd) FC_TRY(dense_work(c.d, DISTILL_WORK));
     RowSums* part = reinterpret_cast<RowSums*>(c.d->work);
     float* work_stats = reinterpret_cast<float*>(c.d->work + DISTILL_SLICES * sizeof(RowSums));
-    auto run = [&](auto l, auto p) {
-        constexpr int LANES = decltype(l)::value, PER = decltype(p)::value, ROWS = LOGIT_THREADS / LANES;
-        const int slices = (int)cdiv(a.dim, RowSlice<T, LANES, PER>::COLUMNS);
-        const int64_t most = DISTILL_SLICES / slices;
-        for (int64_t at = 0; at < a.n; at += most) {
-            const int64_t n = std::min(most, a.n - at);
-            const DistillArgs b = rows_of(a, at, n, sizeof(T));
-            float* stats = c.stats ? c.stats + at * STATS : work_stats;
-            const unsigned blocks = (unsigned)(cdiv(n, ROWS) * slices);
-            auto backward = [&](auto parts) {
-                k_distill_bwd<T, LANES, PER, decltype(parts)::value><<<blocks, LOGIT_THREADS, ROWS * entry_bytes, st>>>(
-                    b, slices, stream, part, c.loss ? c.loss + at : nullptr, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats, (T*)c.grad + at * c.grad_stride,
-                    c.grad_stride);
-            };
-            if constexpr (LANES == LOGIT_THREADS && PER != 4)      // (shorter rows have gone the other way)
-                if (c.fwd) {
-                    k_distill_slice<T, LANES, PER><<<blocks, LOGIT_THREADS, 0, st>>>(b, slices, stream, part);
-                    if (c.bwd && !c.stats && a.n < DISTILL_FEW && c.grad != a.x) { backward(std::true_type()); continue; }
-                    k_distill_join<T><<<(unsigned)cdiv(n, LOGIT_THREADS / 64), LOGIT_THREADS, LOGIT_THREADS / 64 * entry_bytes, st>>>(b, slices, part, c.loss + at, stats);
-                }
-            if (c.bwd) backward(std::false_type());
+    const bool joins = c.fwd && c.bwd && !c.stats && a.n < DISTILL_FEW && c.grad != a.x;      // the gradient's kernel joins the slices
+    int parts = 1;                                 // slices of a row's sums
+    if (c.fwd) by_part(a.n, vectors, [&](auto p) { parts = (int)cdiv(vectors, LOGIT_THREADS * decltype(p)::value); });
+    // rows of a launch: as many as the workspace has slices for, or as a launch has workgroups for (the smallest slices have 128 vectors)
+    const int64_t most = c.fwd ? DISTILL_SLICES / parts : LAUNCH_THREADS / LOGIT_THREADS / cdiv(vectors, 128);
+    for (int64_t at = 0; at < a.n; at += most) {
+        const int64_t n = std::min(most, a.n - at);
+        const DistillArgs b = rows_of(a, at, n, sizeof(T));
+        float* stats = c.stats ? c.stats + at * STATS : work_stats;
+        if (c.fwd) {
+            by_part(a.n, vectors, [&](auto p) {
+                constexpr int PER = decltype(p)::value;
+                k_distill_slice<T, LOGIT_THREADS, PER><<<(unsigned)(n * parts), LOGIT_THREADS, 0, st>>>(b, parts, stream, part);
+            });
+            if (!joins)
+                k_distill_join<T><<<(unsigned)cdiv(n, LOGIT_THREADS / 64), LOGIT_THREADS, LOGIT_THREADS / 64 * entry_bytes, st>>>(b, parts, part, c.loss + at, stats);
         }
-    };
-    // Slices of 8 vectors a lane, or of 2 where those of 8 are fewer than two workgroups a compute unit.
-    if (vectors > 64 * 8 && a.n * cdiv(vectors, LOGIT_THREADS * 8) < 512) run(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    else by_slice(vectors, run);
+        if (!c.bwd) continue;
+        by_slice(a.n, vectors, [&](auto l, auto p) {
+            constexpr int LANES = decltype(l)::value, PER = decltype(p)::value, ROWS = LOGIT_THREADS / LANES;
+            auto backward = [&](auto joining) {
+                const int64_t slices = cdiv(vectors, LANES * PER);
+                k_distill_bwd<T, LANES, PER, decltype(joining)::value><<<(unsigned)(cdiv(n, ROWS) * slices), LOGIT_THREADS, ROWS * entry_bytes, st>>>(
+                    b, (int)slices, stream, part, parts, c.loss ? c.loss + at : nullptr, c.grad_loss + at * c.grad_loss_stride, c.grad_loss_stride, stats,
+                    (T*)c.grad + at * c.grad_stride, c.grad_stride);
+            };
+            if constexpr (LANES == LOGIT_THREADS)
+                if (joins) { backward(std::true_type()); return; }
+            backward(std::false_type());
+        });
+    }
     FC_HIP(hipGetLastError());
     return FC_OK;
 }

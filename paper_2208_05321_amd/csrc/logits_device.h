@@ -69,9 +69,19 @@ struct RowSlice {
     __device__ __forceinline__ void load_long(const T* row, int base, int lane, int dim, bool stream) {
         auto plain = [&](int k, const T* p) { x[k] = *reinterpret_cast<const V*>(p); };
         auto past = [&](int k, const T* p) { x[k] = __builtin_nontemporal_load(reinterpret_cast<const V*>(p)); };
-        if (base + COLUMNS > dim) {
+        auto some = [&](auto get) {                // of a slice that the row ends in; what is beyond the row is not asked for
 #pragma unroll
-            for (int k = 0; k < PER; ++k) plain(k, row + min(column(base, lane, k), dim - N));
+            for (int k = 0; k < PER; ++k) {
+                const int from = base + k * LANES * N;
+                if (from < dim) get(k, row + min(column(base, lane, k), dim - N));
+                else
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[k][e] = (T)-INFINITY;
+            }
+        };
+        if (base + COLUMNS > dim) {
+            if (stream) apart<2>([&] { some(past); });
+            else apart<3>([&] { some(plain); });
         } else if (stream) apart<1>([&] { each(row, base, lane, past); });
         else apart<0>([&] { each(row, base, lane, plain); });
     }
@@ -88,6 +98,7 @@ struct RowSlice {
         if (base + COLUMNS <= dim) return;
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
+            if (dim >= N && (base + (k + 1) * LANES * N <= dim || base + k * LANES * N >= dim)) continue;       // (all of the lanes' vectors are whole, or none is there)
             const int s = skip(column(base, lane, k), dim);
 #pragma unroll
             for (int e = 0; e < N; ++e) if (e < s) x[k][e] = (T)-INFINITY;

@@ -42,9 +42,11 @@ def _rows(ops, n, v, kind, rows, rest):
 
 @pytest.mark.parametrize("rest", [False, True])
 def test_rows_of_several_launches(ops, rest):
-    """32,768 rows of two slices fill the workspace."""
+    """21,845 rows of three slices, or 32,768 of two, fill the workspace."""
     import torch
-    _rows(ops, 33_000, 16_411, torch.float16, [0, 1, 32_766, 32_767, 32_768, 32_769, 32_999], rest)
+    _rows(ops, 33_000, 16_411, torch.float16, [0, 1, 21_844, 21_845, 21_846, 32_766, 32_767, 32_768, 32_769, 32_999], rest)
+    if rest:
+        _rows(ops, 33_000, 16_385 * 2 - 6, torch.float16, [0, 32_766, 32_767, 32_768, 32_999], rest)
 
 
 def test_elements_beyond_32_bits(ops):
