@@ -7,13 +7,13 @@
 //   d/dx_v = a T [c Q_v - sum of P_k with t_k = v] + (1 - a) [softmax(x)_v - (v = y)] for a named v, c = sum P_k + P_0
 //            a T [c Q_v - P_0 Q_v / Q_0]           + (1 - a) [softmax(x)_v - (v = y)] for the others
 //
-// A slice of a row is in registers, so each pass reads the logits once: HBM bounds it.  With P_0 the sums over the ids that are not named are kept apart from those
+// A slice of a row is in registers, so each pass reads the logits once: HBM bounds it.  8192 rows of 131,072 bf16, loss: 319 us, 6.7 TB/s; loss and gradient together of 16,384 rows of
+// 32,768, each read once and written once: 427 us, 5.0 TB/s (rows wait in registers for their sums); of 4096 rows of 131,072 in two passes 555 us, the second 353, 6.1 TB/s.  With P_0 the sums over the ids that are not named are kept apart from those
 // over the named ones, each relative to its own largest element, so that neither is a difference of nearly equal numbers nor lost below the other.
 // The gradient of the others is then one product with an exponential; the entries and the target are mended afterwards, from their own formula.
 #include "logits_device.h"
 
 #include <algorithm>
-
 #include <type_traits>
 
 namespace fc {
@@ -586,12 +586,15 @@ struct DistillCall {
 };
 
 constexpr int64_t DISTILL_FEW = 64;
-// Whether a workgroup takes a whole row, in one launch, or rows are cut into slices.  us, whole rows / slices: gradient, 4096 rows of 131,072 bf16 485 / 540, 200 of 50,021 f16
-// 19.4 / 29.4, 70 18.0 / 18.4, 16,000 of 16,384 bf16 215 / 287, of 5000 f32 157 / 225; loss, 16,000 of 16,000 bf16 130 / 116, of 30,000 230 / 178, of 5000 f32 78 / 75, but
-// 100 of 30,000 bf16 11.7 / 14.7.
+// Whether a workgroup takes a whole row, in one launch, or rows are cut into slices.  Loss and gradient: rows of up to 4096 vectors; larger ones, of which a compute unit holds two or
+// one, only where they leave few lanes idle and have one exponential an element (nothing else runs while a workgroup works).  us, whole rows / slices, bf16: 16,384 rows of 32,768 430 / 564,
+// 4000 of 20,000 111 / 116; one exponential: 4000 of 131,072 476 / 504, 300 of 65,536 30 / 33, 4000 of 60,000 271 / 253 (f32, 2000 of 30,000, 114 / 129), of 50,021 335 / 268;
+// two exponentials: 4000 of 131,072 582 / 533, of 65,536 314 / 276.  The loss alone: 16,000 rows of 16,000 bf16 130 / 116, of 30,000 230 / 178, but 100 of 30,000 11.7 / 14.7.
 static bool in_one_workgroup(const DistillCall& c, int64_t vectors) {
-    if (c.bwd) return vectors <= 512 * 8 || (vectors <= ROW_MOST && c.a.n >= DISTILL_FEW);
-    return vectors <= 256 * 4 || (vectors <= 512 * 8 && c.a.n <= 1024);
+    if (!c.bwd) return vectors <= 256 * 4 || (vectors <= 512 * 8 && c.a.n <= 1024);
+    if (vectors <= 512 * 8) return true;
+    const bool two = c.a.alpha < 1.f && c.a.temperature != 1.f;
+    return !two && c.a.n >= DISTILL_FEW && vectors <= ROW_MOST && vectors * 8 >= (vectors <= ROW_MOST / 2 ? ROW_MOST / 2 : ROW_MOST) * 7;
 }
 
 template <class T>
@@ -602,7 +605,7 @@ int distill_run(const DistillCall& c) {
     const int64_t vectors = cdiv(a.dim, N);
     const size_t entry_bytes = (size_t)entries_room(a.top) * 12;
     // Logits that the memory-side cache does not hold until the next pass (256 MB, the gradient among them) stay out of its way.  us: 8192 rows of 131,072 bf16 (2.1 GB), loss
-    // 373 / 363; 4096 such rows, loss and then gradient 580 / 574; 777 of 50,021 f16 (78 MB) 74 / 81.
+    // 357 / 319; 4096 such rows, the loss before its gradient 218 / 183; but 777 of 50,021 f16 (78 MB), loss and then gradient 74 / 81.
     const bool stream = a.n * a.dim * (int64_t)sizeof(T) > (int64_t)128 << 20;
     if (c.fwd && in_one_workgroup(c, vectors)) {
         by_row(vectors, [&](auto l, auto p) {

@@ -7,7 +7,6 @@
 #include "dense_device.h"
 
 #include <algorithm>
-
 #include <type_traits>
 
 namespace fc {

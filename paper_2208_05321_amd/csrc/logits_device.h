@@ -198,7 +198,7 @@ struct RowSlice {
     // Stores the slice, whose elements are results by now, but for the row's last vector where that is not a whole one; that is the business of one lane of the row, at the
     // end (code for it at every vector is most of a kernel).
     __device__ __forceinline__ void store(T* row, int base, int lane, int dim, bool stream) const {
-auto plain = [&](int k, T* p) { *reinterpret_cast<V*>(p) = x[k]; };
+        auto plain = [&](int k, T* p) { *reinterpret_cast<V*>(p) = x[k]; };
         auto past = [&](int k, T* p) { __builtin_nontemporal_store(x[k], reinterpret_cast<V*>(p)); };
         if (base + COLUMNS <= dim) {
             if (stream) apart<1>([&] { each(row, base, lane, past); });

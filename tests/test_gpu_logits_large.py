@@ -15,7 +15,7 @@ def ops():
     o.close()
 
 
-def _rows(ops, n, v, kind, rows, rest):
+def _rows(ops, n, v, kind, rows, rest, t=2.0):
     import torch
     g = torch.Generator(device="cuda").manual_seed(n)
     x = torch.empty((n, v), dtype=kind, device="cuda")
@@ -24,12 +24,12 @@ def _rows(ops, n, v, kind, rows, rest):
     top = 6
     ids = torch.randint(0, v // top, (n, top), generator=g, device="cuda") + torch.arange(top, device="cuda") * (v // top)
     z = torch.randn((n, top), generator=g, device="cuda") + 8
-    lse = torch.logsumexp(z.double() / 2, 1).float() + 0.3 if rest else None
+    lse = torch.logsumexp(z.double() / t, 1).float() + 0.3 if rest else None
     y, w = ids[:, 1].contiguous(), torch.rand(n, generator=g, device="cuda") + 0.5
-    loss, stats = ops.distill_fwd(x, ids, z, teacher_lse=lse, targets=y, temperature=2.0, alpha=0.5)
-    back = ops.distill_bwd(w, x, ids, z, stats, targets=y, temperature=2.0, alpha=0.5)[rows]
-    both, grad = ops.distill_grad(w, x, ids, z, teacher_lse=lse, targets=y, temperature=2.0, alpha=0.5)
-    want, of, off, off_grad = distill(x[rows], ids[rows], z[rows], None if lse is None else lse[rows], y[rows], 2.0, 0.5)
+    loss, stats = ops.distill_fwd(x, ids, z, teacher_lse=lse, targets=y, temperature=t, alpha=0.5)
+    back = ops.distill_bwd(w, x, ids, z, stats, targets=y, temperature=t, alpha=0.5)[rows]
+    both, grad = ops.distill_grad(w, x, ids, z, teacher_lse=lse, targets=y, temperature=t, alpha=0.5)
+    want, of, off, off_grad = distill(x[rows], ids[rows], z[rows], None if lse is None else lse[rows], y[rows], t, 0.5)
     wd = w[rows].double()[:, None]
     bound = off_grad * wd + rounded((of * wd).abs() + off_grad * wd, kind)
     inside(loss[rows], want, off, "loss")
@@ -47,6 +47,15 @@ def test_rows_of_several_launches(ops, rest):
     _rows(ops, 33_000, 16_411, torch.float16, [0, 1, 21_844, 21_845, 21_846, 32_766, 32_767, 32_768, 32_769, 32_999], rest)
     if rest:
         _rows(ops, 33_000, 16_385 * 2 - 6, torch.float16, [0, 32_766, 32_767, 32_768, 32_999], rest)
+
+
+@pytest.mark.parametrize("kind,v", [("bfloat16", 65_003), ("bfloat16", 131_072), ("float16", 120_001), ("float32", 30_001), ("float32", 60_003)])
+def test_rows_of_a_large_workgroup(ops, kind, v):
+    """At one temperature a workgroup of 1024 takes rows that it has vectors for."""
+    import torch
+    for rest in (False, True):
+        for temperature in (1.0, 2.0):
+            _rows(ops, 300, v, getattr(torch, kind), [0, 1, 150, 298, 299], rest, temperature)
 
 
 def test_elements_beyond_32_bits(ops):
