@@ -501,10 +501,19 @@ class DenseOps:
                     oapart = piece
         return row, orow, apart, oapart, piece, pieces if piece else 0
 
+    @staticmethod
+    def _apart(table):
+        """Refuses a tensor that is written twice, or read as one state and written as another."""
+        rows = [(*table[i:i + 2], i) for i in range(0, len(table), 8) if table[i + 6] * table[i + 7]]
+        by = {o: i for _, o, i in rows}
+        if len(by) < len(rows) or any(by.get(t, i) != i for t, _, i in rows):
+            _refuse("states: the same tensor twice")
+
     def beam_reorder(self, states, parents, out=None):
         """states[k][b, j] = states[k][b, parents[b, j]] for tensors [batch, beams, ...] of any type, in place; or into the tensors of `out` [batch, keep, ...].  Returns the tensors
         written.  parents [batch, keep] (int32, int64).  A row (what follows the first two dimensions) is neighbouring elements, or pieces of them at one distance, such as the filled
-        part of a cache [batch, beams, heads, room, dim].  A parent outside [0, beams) raises the sticky error; its row becomes zeros, in place it stays as it was."""
+        part of a cache [batch, beams, heads, room, dim].  A parent outside [0, beams) raises the sticky error; its row becomes zeros, in place it stays as it was.
+        Tensors share no memory, except that out[k] may be states[k]."""
         states = list(states)
         pk = self._ids(parents)
         if parents.dim() != 2 or not states:
@@ -531,6 +540,9 @@ class DenseOps:
                 layout = layouts[key] = self._move(t, o, batch, beams, keep)
             table += (t.data_ptr(), o.data_ptr())
             table += layout
+        written = table[1::8]
+        if len(set(written)) < len(written) or (given and not set(written).isdisjoint(table[::8])):
+            self._apart(table)
         table = array("q", table)
         self._run("beam_reorder", self._L.beam_reorder, (states, out, (parents,)), table.buffer_info()[0], len(states), batch, beams, parents.data_ptr(), pk, keep)
         self._written(out)

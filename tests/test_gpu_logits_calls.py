@@ -253,3 +253,24 @@ def test_together_a_step_of_training_and_of_search(ops):
         if step == 1:
             done[2, 1] = True
     ops.check()
+
+
+def test_a_state_given_twice(ops):
+    """Refused, as it would be moved twice; the same tensor may be read for several that are written."""
+    import torch
+    from paper_2208_05321_amd import FreqCacheError
+    a = torch.arange(30., device="cuda").view(2, 3, 5)
+    b, p = a + 100, torch.tensor([[2, 0, 1], [1, 1, 0]], device="cuda")
+    kept, none = a.clone(), torch.empty(2, 3, 0, device="cuda")
+    for states, out in (([a, b, a], None), ([a, a[:, :, :2]], None), ([a, a], [b, b]), ([a, b], [b, a])):
+        with pytest.raises(FreqCacheError) as err:
+            ops.beam_reorder(states, p, out=out)
+        assert err.value.name == "INVALID_ARG"
+    torch.cuda.synchronize()
+    assert torch.equal(a, kept)
+    want = torch.stack([kept[i][p[i]] for i in range(2)])
+    c = ops.beam_reorder([a, a, none, none], p, out=[torch.empty_like(a), torch.empty_like(a), torch.empty_like(none), torch.empty_like(none)])
+    assert torch.equal(c[0], want) and torch.equal(c[1], want)
+    ops.beam_reorder([a, none, none], p, out=[a, none, none])
+    assert torch.equal(a, want)
+    ops.check()

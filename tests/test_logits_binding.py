@@ -65,3 +65,18 @@ def test_layouts_of_states(ops):  # noqa: F811
         with pytest.raises(FreqCacheError) as e:
             ops._state(bad, 2, "t")
         assert e.value.name == "INVALID_ARG"
+
+
+def test_a_state_given_twice(ops):  # noqa: F811
+    """Rows would be moved twice, or read after others had taken their place; a tensor without elements may be there several times."""
+    from paper_2208_05321_amd import FreqCacheError
+    row, none = (20, 20, 20, 20, 20, 1), (0, 0, 0, 0, 0, 1)
+
+    def table(*pairs):
+        return [v for t, o in pairs for v in (t, o, *(row if t or o else none))]
+    for pairs in ([(1, 1), (2, 2), (1, 1)], [(1, 3), (2, 3)], [(1, 3), (2, 1)], [(1, 2), (2, 1)], [(1, 1), (2, 1)], [(0, 0), (1, 2), (2, 4)]):
+        with pytest.raises(FreqCacheError) as e:
+            ops._apart(table(*pairs))
+        assert e.value.name == "INVALID_ARG"
+    for pairs in ([(1, 1), (2, 2), (0, 0), (0, 0)], [(1, 2), (1, 3)], [(1, 1), (2, 2)], [(1, 1), (2, 3), (0, 0)]):
+        ops._apart(table(*pairs))
