@@ -28,9 +28,13 @@ struct BeamArgs {
     const uint8_t* finished;                       // or NULL
     int32_t beams, dim, keep, eos, slices;
 };
-// what a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are in a list of `keep`, filled up with -infinity
+// What a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are a list of `keep`, filled up with -infinity.  A sequence's lists lie side by side, the first entries
+// of all before the second ones: what neighbouring lanes of the next step hold is of different lists, and the first of a lane's is its largest, which makes its bound a good one (the other
+// way round more than BEAM_LIST candidates passed it, and 5 sequences of 32 beams of 131,072 bf16, the 32 best, took 118 us, not 31).
 struct BeamSlice { double sum; float off; };
-struct BeamEntry { float x; int32_t id; };
+struct BeamEntry { float x; uint32_t id; };        // id: and the beam, above it
+constexpr int BEAM_SHIFT = 24;
+static_assert(DENSE_MAX_DIM <= 1 << BEAM_SHIFT && BEAM_MOST <= 1 << (32 - BEAM_SHIFT));
 
 // numbers in the order of unsigned integers (no distinction between zeros)
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -105,7 +109,13 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     __shared__ int count, kept;
     const int lane = threadIdx.x, part = blockIdx.x % a.slices, begin = part * run * Slice::COLUMNS;
     const int64_t local = blockIdx.x / a.slices, row = first + local;
-    if (!beam_lives(a, row) || (a.finished && a.finished[row])) return;
+    const uint32_t all = a.beams * a.slices, seq = blockIdx.x / all, beam = (uint32_t)(local - seq * a.beams) << BEAM_SHIFT;
+    BeamEntry* out = lists + (int64_t)seq * all * a.keep + (blockIdx.x - seq * all);
+    const bool lives = beam_lives(a, row);
+    if (!lives || (a.finished && a.finished[row])) {             // no candidate, or the end again
+        for (int i = lane; i < a.keep; i += LOGIT_THREADS) out[i * all] = lives && part == 0 && i == 0 ? BeamEntry{0.f, beam | (uint32_t)a.eos} : BeamEntry{-INFINITY, 0};
+        return;
+    }
     const T* x = (const T*)a.x + row * a.stride;
     const int end = (int)min((int64_t)a.dim, begin + (int64_t)run * Slice::COLUMNS);
     Slice s;
@@ -162,8 +172,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     const double sum_wave = wave_sum((double)(sum * __builtin_amdgcn_exp2f(off - from_of(off_wave))));
     if ((lane & 63) == 0) { offs[lane >> 6] = off_wave; parts[lane >> 6] = sum_wave; }
     __syncthreads();
-    BeamEntry* out = lists + (local * a.slices + part) * a.keep;
-    auto put = [&](int at, uint64_t key) { out[at] = BeamEntry{unordered((uint32_t)(key >> 32)), (int32_t)~(uint32_t)key}; };
+    auto put = [&](int at, uint64_t key) { out[at * all] = BeamEntry{unordered((uint32_t)(key >> 32)), beam | ~(uint32_t)key}; };
     const uint64_t lowest = (uint64_t)bound() << 32;
     if (count <= BEAM_LIST) {
         for (int i = lane; i < count; i += LOGIT_THREADS) {
@@ -180,7 +189,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
             for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor(rank, o);
             if (rank < a.keep && (lane & 7) == 0) put(rank, key);
         }
-        for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) out[i] = BeamEntry{-INFINITY, 0};
+        for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) out[i * all] = BeamEntry{-INFINITY, 0};
     } else {                                       // (as good as equal logits)
         uint64_t last = ~0ull;
         for (int i = 0; i < a.keep; ++i) {
@@ -197,9 +206,9 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     if (lane == 0) {
         float to = offs[0];
         for (int k = 1; k < WAVES; ++k) to = fmaxf(to, offs[k]);
-        double all = 0.;
-        for (int k = 0; k < WAVES; ++k) all += parts[k] * (double)exp2f(offs[k] - from_of(to));
-        sums[local * a.slices + part] = BeamSlice{all, to};
+        double total = 0.;
+        for (int k = 0; k < WAVES; ++k) total += parts[k] * (double)exp2f(offs[k] - from_of(to));
+        sums[blockIdx.x] = BeamSlice{total, to};
     }
 }
 
@@ -224,14 +233,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
                                                             int32_t token_type, uint8_t* __restrict__ finished_out) {
     constexpr int WAVES = JOIN_THREADS / 64;
     __shared__ double add[BEAM_MOST];              // what a beam's logits lack to be candidates; not finite: there are none
-    __shared__ bool ended[BEAM_MOST];
-    __shared__ uint32_t bounds[WAVES];
-    __shared__ double list_c[BEAM_LIST];
+    __shared__ uint32_t bounds[WAVES], shares[WAVES], highs[WAVES];
+    __shared__ double list_c[BEAM_LIST];           // and bins
     __shared__ Candidate list[BEAM_LIST];
     __shared__ int count;
     const int lane = threadIdx.x;
     const int64_t seq = blockIdx.x, row0 = first + seq * a.beams;
-    const int each = a.slices * a.keep, all = a.beams * each;       // (below 2^22)
+    const int all = a.beams * a.slices * a.keep;                    // (below 2^22)
     const BeamEntry* entries = lists + seq * all;
     BeamEntry held[JOIN_HELD];
     if constexpr (HELD) {
@@ -255,42 +263,88 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
             const float to = from_of(wave_max(q.off));
             v = -0.69314718055994530942 * ((double)to + log2(wave_sum(q.sum * (double)exp2f(q.off - to))));
         }
-        if ((lane & 63) == 0) { add[w] = v + (double)score; ended[w] = end; }
+        if ((lane & 63) == 0) add[w] = v + (double)score;
     }
     if (lane == 0) count = 0;
     __syncthreads();
     // f(candidate) for each of this lane's candidates
     auto candidates = [&](auto f) {
-        auto one = [&](int i, const BeamEntry& e) {
-            const int w = i / each;
+        auto one = [&](const BeamEntry& e) {
+            if (e.x == -INFINITY) return;
+            const int w = e.id >> BEAM_SHIFT;
             const double v = add[w];
-            if (!(v - v == 0.)) return;
-            if (ended[w]) { if (i == w * each) f(Candidate{v, 0.f, w, a.eos}); }
-            else if (e.x != -INFINITY) f(Candidate{v + (double)e.x, e.x, w, e.id});
+            if (v - v == 0.) f(Candidate{v + (double)e.x, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
         };
         if constexpr (HELD) {
 #pragma unroll
-            for (int j = 0; j < JOIN_HELD; ++j) if (lane + j * JOIN_THREADS < all) one(lane + j * JOIN_THREADS, held[j]);
+            for (int j = 0; j < JOIN_HELD; ++j) if (lane + j * JOIN_THREADS < all) one(held[j]);
         } else
-            for (int i = lane; i < all; i += JOIN_THREADS) one(i, entries[i]);
+            for (int i = lane; i < all; i += JOIN_THREADS) one(entries[i]);
     };
+    // Bounds are keys of candidates rounded to 32 bits, which keeps their order.  Two that `keep` candidates reach: the `keep`-th of a wavefront's lanes' largest, and the least of what
+    // an eighth of `keep` of each wavefront's reach.  (Lanes without a candidate count as the lowest key.)
+    auto key_of = [](double c) { return ordered((float)c); };
     double top = -INFINITY;
     candidates([&](const Candidate& q) { top = fmax(top, q.c); });
-    // (one less than the number in 32 bits, which may have been rounded up)
-    const uint32_t mine = wave_bound(ordered((float)top) - 1, a.keep);
-    if ((lane & 63) == 0) bounds[lane >> 6] = mine;
+    const uint32_t top_key = key_of(top), mine = wave_bound(top_key, a.keep), share = wave_bound(top_key, (a.keep + WAVES - 1) / WAVES);
+    const float high = wave_max((float)top);
+    if ((lane & 63) == 0) { bounds[lane >> 6] = mine; shares[lane >> 6] = share; highs[lane >> 6] = ordered(high); }
     __syncthreads();
-    uint32_t key = LOWEST;
+    uint32_t low = shares[0], hi = highs[0];
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) key = max(key, bounds[k]);
-    const double bound = key == LOWEST ? -INFINITY : (double)unordered(key);
-    if (top >= bound && top > -INFINITY)
-        candidates([&](const Candidate& q) {
-            if (q.c < bound) return;
-            const int p = atomicAdd(&count, 1);
-            if (p < BEAM_LIST) { list_c[p] = q.c; list[p] = q; }
-        });
-    __syncthreads();
+    for (int k = 1; k < WAVES; ++k) { low = min(low, shares[k]); hi = max(hi, highs[k]); }
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) low = max(low, bounds[k]);
+    auto collect = [&]() {                         // what is above the bound, and how many
+        if (top_key >= low && top > -INFINITY)
+            candidates([&](const Candidate& q) {
+                if (key_of(q.c) < low) return;
+                const int p = atomicAdd(&count, 1);
+                if (p < BEAM_LIST) { list_c[p] = q.c; list[p] = q; }
+            });
+        __syncthreads();
+        return count;
+    };
+    int got = collect();
+    if (got > BEAM_LIST) {                         // a higher bound: the keys above this one are counted in 1024 bins, and the bin of the `keep`-th in as many again
+        uint32_t* bins = reinterpret_cast<uint32_t*>(list_c);
+        constexpr int BINS = 1024, EACH = BINS / 64;
+        int shift = 1;
+        while (got > BEAM_LIST && shift > 0 && hi > low) {
+            shift = max(0, 22 - __builtin_clz(hi - low));
+            __syncthreads();
+            for (int i = lane; i < BINS; i += JOIN_THREADS) bins[i] = 0;
+            __syncthreads();
+            candidates([&](const Candidate& q) {
+                const uint32_t k = key_of(q.c);
+                if (k >= low) atomicAdd(&bins[min((k - low) >> shift, BINS - 1u)], 1u);
+            });
+            __syncthreads();
+            if (lane < 64) {                       // each lane has EACH bins, the first lane the highest ones
+                const uint32_t* own = bins + (63 - lane) * EACH;
+                int sum = 0;
+                for (int i = 0; i < EACH; ++i) sum += (int)own[i];
+                int upto = sum;
+                for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(upto, o); if (lane >= o) upto += y; }
+                if (upto >= a.keep && upto - sum < a.keep) {
+                    int n = upto - sum, i = EACH;
+                    while (n < a.keep) n += (int)own[--i];
+                    bounds[0] = low + ((uint32_t)((63 - lane) * EACH + i) << shift);
+                    count = n;
+                }
+            }
+            __syncthreads();
+            low = bounds[0];
+            got = count;
+            hi = min(hi, low + (1u << shift) - 1);
+        }
+        if (got <= BEAM_LIST) {
+            __syncthreads();
+            if (lane == 0) count = 0;
+            __syncthreads();
+            got = collect();
+        }
+    }
     auto put = [&](int at, const Candidate& q) {
         const int64_t o = seq * a.keep + at;
         scores_out[o] = (float)q.c;
@@ -298,7 +352,6 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
         if (token_type == FC_TYPE_I64) ((int64_t*)tokens_out)[o] = q.id; else ((int32_t*)tokens_out)[o] = q.id;
         if (finished_out) finished_out[o] = q.id == a.eos;
     };
-    int got = count;
     if (got <= BEAM_LIST) {
         for (int i = lane >> 3; i < got; i += JOIN_THREADS / 8) {    // eight lanes to a candidate
             const double c = list_c[i];
@@ -312,7 +365,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
             if (rank < a.keep && (lane & 7) == 0) put(rank, list[i]);
         }
         got = min(got, a.keep);
-    } else {
+    } else {                                       // (over BEAM_LIST candidates that are equal in 32 bits)
         Candidate last{INFINITY, 0.f, -1, -1};
         got = a.keep;
         for (int i = 0; i < a.keep; ++i) {

@@ -120,3 +120,22 @@ def test_no_sequences(ops):
     import torch
     out = ops.beam_select(torch.empty((0, 4, 100), device="cuda"), torch.empty((0, 4), device="cuda"), 8, eos_id=3)
     assert [tuple(t.shape) for t in out] == [(0, 8)] * 4
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_many_candidates_above_the_first_bound(ops, kind):
+    """Beams far apart, logits that are nearly alike, few beams alive, scores near the lowest number: thousands of candidates lie close together."""
+    import torch
+    k = getattr(torch, kind)
+    for b, w, v, keep, spread in ((2, 32, 40_000, 64, 3.0), (1, 64, 20_011, 64, 1e-3), (3, 10, 131_072, 37, 0.05), (2, 4, 300_001, 64, 30.0)):
+        x, scores, g = _inputs(b, w, v, k, keep, spread)
+        what = (b, w, v, keep, kind)
+        _check(ops, x, scores, keep, what=what)
+        _check(ops, x, scores.flip(1).contiguous() * 20, keep, what=(*what, "the last beam"))
+        _check(ops, x, scores * 1e-4, keep, what=(*what, "close"))
+        one = torch.full_like(scores, NONE)
+        one[:, w // 2] = -1.0
+        _check(ops, x, one, keep, what=(*what, "one alive"))
+        done = torch.rand((b, w), generator=g, device="cuda") < 0.5
+        _check(ops, x, scores * 1e-4, keep, done, 1, what=(*what, "ended"))
+    ops.check()
