@@ -30,7 +30,7 @@ struct BeamArgs {
 };
 // What a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are a list of `keep`, filled up with -infinity.  A sequence's lists lie side by side, the first entries
 // of all before the second ones: what neighbouring lanes of the next step hold is of different lists, and the first of a lane's is its largest, which makes its bound a good one (the other
-// way round more than BEAM_LIST candidates passed it, and 5 sequences of 32 beams of 131,072 bf16, the 32 best, took 118 us, not 31).
+// way round more than BEAM_LIST candidates passed it, and 5 sequences of 32 beams of 131,072 bf16, the 32 best, took 124 us, not 35).
 struct BeamSlice { double sum; float off; };
 struct BeamEntry { float x; uint32_t id; };        // id: and the beam, above it
 constexpr int BEAM_SHIFT = 24;
@@ -224,6 +224,9 @@ __device__ __forceinline__ bool before(const Candidate& p, const Candidate& q) {
 constexpr int JOIN_THREADS = 512;
 // Entries that a lane holds in registers; those of larger searches are read again (all of them read again: one sequence of 4 beams of 131,072 ids, alone, 30.7 us, not 28.1; 64 of 8 as fast).
 constexpr int JOIN_HELD = 4;
+// Candidates above the bound beyond which a higher one is looked for: to rank 1024 takes some 40 us.  us, at 256 / 512 / 1024: one sequence of 32 beams of 131,072 bf16, the 64 best
+// 44.5 / 49.7 / 86.8, one of one beam of 250,000 29 / 80 / 80.
+constexpr int JOIN_FEW = 256;
 
 // One workgroup puts a sequence's beams and slices together.  Everything it needs is asked for at once; what follows are a few steps that wait for one another (one sequence of 4
 // beams of 131,072 ids 13.4 us when lists were read after their lengths and the bound was found by comparing all lanes, 4.1 this way; 64 sequences of 8 beams 21.4 and 8.9).
@@ -267,25 +270,37 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
     }
     if (lane == 0) count = 0;
     __syncthreads();
-    // f(candidate) for each of this lane's candidates
+    // f(candidate) for each of this lane's candidates; whether it is one to consider, or any later one of its list.  All lanes come here together.
     auto candidates = [&](auto f) {
+        bool used;
         auto one = [&](const BeamEntry& e) {
             if (e.x == -INFINITY) return;
             const int w = e.id >> BEAM_SHIFT;
             const double v = add[w];
-            if (v - v == 0.) f(Candidate{v + (double)e.x, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
+            if (v - v == 0.) used |= f(Candidate{v + (double)e.x, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
         };
         if constexpr (HELD) {
+            used = false;
 #pragma unroll
             for (int j = 0; j < JOIN_HELD; ++j) if (lane + j * JOIN_THREADS < all) one(held[j]);
-        } else
-            for (int i = lane; i < all; i += JOIN_THREADS) one(entries[i]);
+        } else {
+            int idle = 0;                          // entries one after the other that f had no use for: of every list one, if there are as many as lists, and what follows in them is lower
+            for (int i = lane; i - lane < all && idle < a.beams * a.slices; i += JOIN_THREADS * JOIN_HELD) {
+                BeamEntry e[JOIN_HELD];
+#pragma unroll
+                for (int j = 0; j < JOIN_HELD; ++j) e[j] = entries[min(i + j * JOIN_THREADS, all - 1)];
+                used = false;
+#pragma unroll
+                for (int j = 0; j < JOIN_HELD; ++j) if (i + j * JOIN_THREADS < all) one(e[j]);
+                idle = __syncthreads_or(used) ? 0 : idle + JOIN_THREADS * JOIN_HELD;
+            }
+        }
     };
     // Bounds are keys of candidates rounded to 32 bits, which keeps their order.  Two that `keep` candidates reach: the `keep`-th of a wavefront's lanes' largest, and the least of what
     // an eighth of `keep` of each wavefront's reach.  (Lanes without a candidate count as the lowest key.)
     auto key_of = [](double c) { return ordered((float)c); };
     double top = -INFINITY;
-    candidates([&](const Candidate& q) { top = fmax(top, q.c); });
+    candidates([&](const Candidate& q) { const bool more = q.c > top; top = fmax(top, q.c); return more; });
     const uint32_t top_key = key_of(top), mine = wave_bound(top_key, a.keep), share = wave_bound(top_key, (a.keep + WAVES - 1) / WAVES);
     const float high = wave_max((float)top);
     if ((lane & 63) == 0) { bounds[lane >> 6] = mine; shares[lane >> 6] = share; highs[lane >> 6] = ordered(high); }
@@ -296,21 +311,21 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) low = max(low, bounds[k]);
     auto collect = [&]() {                         // what is above the bound, and how many
-        if (top_key >= low && top > -INFINITY)
-            candidates([&](const Candidate& q) {
-                if (key_of(q.c) < low) return;
-                const int p = atomicAdd(&count, 1);
-                if (p < BEAM_LIST) { list_c[p] = q.c; list[p] = q; }
-            });
+        candidates([&](const Candidate& q) {
+            if (key_of(q.c) < low) return false;
+            const int p = atomicAdd(&count, 1);
+            if (p < BEAM_LIST) { list_c[p] = q.c; list[p] = q; }
+            return true;
+        });
         __syncthreads();
         return count;
     };
     int got = collect();
-    if (got > BEAM_LIST) {                         // a higher bound: the keys above this one are counted in 1024 bins, and the bin of the `keep`-th in as many again
+    if (got > JOIN_FEW) {                          // a higher bound: the keys above this one are counted in 1024 bins, and the bin of the `keep`-th in as many again
         uint32_t* bins = reinterpret_cast<uint32_t*>(list_c);
         constexpr int BINS = 1024, EACH = BINS / 64;
         int shift = 1;
-        while (got > BEAM_LIST && shift > 0 && hi > low) {
+        while (got > JOIN_FEW && shift > 0 && hi > low) {
             shift = max(0, 22 - __builtin_clz(hi - low));
             __syncthreads();
             for (int i = lane; i < BINS; i += JOIN_THREADS) bins[i] = 0;
@@ -318,6 +333,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
             candidates([&](const Candidate& q) {
                 const uint32_t k = key_of(q.c);
                 if (k >= low) atomicAdd(&bins[min((k - low) >> shift, BINS - 1u)], 1u);
+                return k >= low;
             });
             __syncthreads();
             if (lane < 64) {                       // each lane has EACH bins, the first lane the highest ones
@@ -370,7 +386,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
         got = a.keep;
         for (int i = 0; i < a.keep; ++i) {
             Candidate mine{-INFINITY, 0.f, 1 << 30, 0};
-            candidates([&](const Candidate& q) { if (before(last, q) && before(q, mine)) mine = q; });
+            candidates([&](const Candidate& q) { if (before(last, q) && before(q, mine)) mine = q; return key_of(q.c) >= low; });
             __syncthreads();
             list[lane] = mine;
             for (int o = JOIN_THREADS / 2; o > 0; o >>= 1) {
@@ -432,8 +448,8 @@ int beam_select(fc_dense* d, const void* logits_dev, int32_t type, int64_t logit
         const BeamArgs a{logits_dev, logits_stride, scores_dev, finished_dev, beams, dim, keep, eos_id, 1};
         const int64_t vectors = cdiv(dim, VECTOR<T>);
         // Vectors of a lane: 8, or 2 where slices of 8 are too few to keep all compute units reading.  us, 8 / 2: 64 sequences of 8 beams of 131,072 bf16 33.5 / 40.8, 33 of 5 of 50,021 f32
-        // 15.4 / 17.1, but one of 4 beams of 131,072, alone, 29.4 / 28.0.
-        if (vectors <= LOGIT_THREADS * 2 || batch * beams * cdiv(vectors, LOGIT_THREADS * 8) < 512)
+        // 15.4 / 17.1, but one of 4 beams of 131,072, alone, 29.4 / 28.0.  Not for long lists, as there are four times as many then: one of 32 beams, the 64 best, 36.7 / 44.5.
+        if (vectors <= LOGIT_THREADS * 2 || (keep <= 16 && batch * beams * cdiv(vectors, LOGIT_THREADS * 8) < 512))
             beam_run<T, 2>(d, a, batch, scores_out_dev, parents_out_dev, tokens_out_dev, token_type, finished_out_dev);
         else beam_run<T, 8>(d, a, batch, scores_out_dev, parents_out_dev, tokens_out_dev, token_type, finished_out_dev);
         FC_HIP(hipGetLastError());
