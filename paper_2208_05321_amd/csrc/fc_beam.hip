@@ -4,9 +4,9 @@
 //   the `keep` largest, in descending order; equal ones: lower beam, larger logit, lower id
 //
 // Within a beam the order is that of the logits, so a slice of a row (in registers, read once) gives its `keep` largest logits and its sum of
-// exponentials, and one workgroup for a sequence puts beams and slices together.  64 sequences of 8 beams of 131,072 bf16, the 16 best: 31 us for the first step, 4.3 TB/s; it reads
+// exponentials, and one workgroup for a sequence puts beams and slices together.  64 sequences of 8 beams of 131,072 bf16, the 16 best: 30 us for the first step, 4.5 TB/s; it reads
 // each logit once and writes 8 bytes of lists a candidate, but an exponential and a comparison of each element keep the vector units busy for about two thirds of that time.  The second
-// step takes 5 us, and one sequence of 4 beams 5.2 and 4.0: what waits for one another there are a few accesses.
+// step takes 6 us, and one sequence of 4 beams 5.2 and 3.7: what waits for one another there are a few accesses.
 // The candidates are put in order in 64 bits: sums of exponentials are added up in 64 bits over the lanes, and nothing is rounded before the scores are stored.
 //
 // The `keep` largest of a workgroup's elements: those above a bound that is no larger than the `keep`-th largest are few, and are ranked by
@@ -229,7 +229,7 @@ constexpr int JOIN_HELD = 4;
 constexpr int JOIN_FEW = 256;
 
 // One workgroup puts a sequence's beams and slices together.  Everything it needs is asked for at once; what follows are a few steps that wait for one another (one sequence of 4
-// beams of 131,072 ids 13.4 us when lists were read after their lengths and the bound was found by comparing all lanes, 4.1 this way; 64 sequences of 8 beams 21.4 and 8.9).
+// beams of 131,072 ids 13.4 us when lists were read after their lengths and the bound was found by comparing all lanes, 3.7 this way; 64 sequences of 8 beams 21.4 and 6.2).
 template <bool HELD>
 __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t first, const BeamSlice* __restrict__ sums, const BeamEntry* __restrict__ lists,
                                                             float* __restrict__ scores_out, int32_t* __restrict__ parents_out, void* __restrict__ tokens_out,
