@@ -348,10 +348,10 @@ __device__ __forceinline__ void store_zeros(T* out, int base, int lane, int dim)
 constexpr int distill_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 // Rows that LANES lanes hold: the loss, and the gradient too if it is wanted (grad), which may take the place of the logits: a row is read before any of it is written.  The row waits in
-// registers while one wavefront works on its entries, so what counts is how many rows a compute unit holds: 80 registers and three rows of 64 KB, though some
+// registers while one wavefront works on its entries, so what counts is how many rows a compute unit holds: 80 registers and three rows of 64 KB, or four of 48, though some
 // 40 bytes of a lane then go through memory (16,384 rows of 32,768 bf16: 4 to 8 wavefronts a SIMD 532 / - / 446 / 490 / 586 us).
 template <class T, int LANES, int PER>
-__global__ __launch_bounds__(distill_threads(LANES)) __attribute__((amdgpu_waves_per_eu(LANES <= 512 ? 6 : 4))) void k_distill_row(DistillArgs a, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride, float* __restrict__ loss,
+__global__ __launch_bounds__(distill_threads(LANES)) __attribute__((amdgpu_waves_per_eu(LANES > 512 ? 4 : LANES == 512 && PER == 6 ? 8 : 6))) void k_distill_row(DistillArgs a, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride, float* __restrict__ loss,
                                                                         float* __restrict__ stats, T* grad, int64_t grad_stride) {
     using Slice = RowSlice<T, LANES, PER>;
     constexpr int ROWS = distill_threads(LANES) / LANES;
@@ -546,7 +546,9 @@ void by_part(int64_t n, int64_t vectors, F f) {
     else if (eights <= 5 && cdiv(vectors, LOGIT_THREADS * 4) % 2 == 1) f(integral_constant<int, 4>());
     else f(integral_constant<int, 8>());
 }
-// the same for rows that one workgroup holds
+// the same for rows that one workgroup holds.  6 vectors a lane and not 8 where they are enough: idle lanes take registers from other rows, and with 512 lanes a fourth row fits a compute
+// unit then.  us, 8 / 6: loss and gradient of 4000 rows of 10,000 bf16 62 / 53, of 12,000 65 / 56, of 17,000 108 / 91, of 24,000 113 / 99, of 10,000 f32 83 / 75 (with 512 lanes at three rows a
+// compute unit 96, 106 and 83, the last three; four rows with 256 lanes 55 and 60, the first two).
 constexpr int64_t ROW_MOST = 1024 * 16;
 template <class F>
 void by_row(int64_t vectors, F f) {
@@ -554,7 +556,9 @@ void by_row(int64_t vectors, F f) {
     if (vectors <= 64 * 2) f(integral_constant<int, 64>(), integral_constant<int, 2>());
     else if (vectors <= 64 * 8) f(integral_constant<int, 64>(), integral_constant<int, 8>());
     else if (vectors <= 256 * 4) f(integral_constant<int, 256>(), integral_constant<int, 4>());
+    else if (vectors <= 256 * 6) f(integral_constant<int, 256>(), integral_constant<int, 6>());
     else if (vectors <= 256 * 8) f(integral_constant<int, 256>(), integral_constant<int, 8>());
+    else if (vectors <= 512 * 6) f(integral_constant<int, 512>(), integral_constant<int, 6>());
     else if (vectors <= 512 * 8) f(integral_constant<int, 512>(), integral_constant<int, 8>());
     else if (vectors <= 1024 * 8) f(integral_constant<int, 1024>(), integral_constant<int, 8>());
     else f(integral_constant<int, 1024>(), integral_constant<int, 16>());
@@ -588,7 +592,7 @@ struct DistillCall {
 constexpr int64_t DISTILL_FEW = 64;
 // Whether a workgroup takes a whole row, in one launch, or rows are cut into slices.  Loss and gradient: rows of up to 4096 vectors; larger ones, of which a compute unit holds two or
 // one, only where they leave few lanes idle and have one exponential an element (nothing else runs while a workgroup works).  us, whole rows / slices, bf16: 16,384 rows of 32,768 430 / 564,
-// 4000 of 20,000 111 / 116; one exponential: 4000 of 131,072 476 / 504, 300 of 65,536 30 / 33, 4000 of 60,000 271 / 253 (f32, 2000 of 30,000, 114 / 129), of 50,021 335 / 268;
+// 4000 of 20,000 95 / 116; one exponential: 4000 of 131,072 476 / 504, 300 of 65,536 30 / 33, 4000 of 60,000 271 / 253 (f32, 2000 of 30,000, 114 / 129), of 50,021 335 / 268;
 // two exponentials: 4000 of 131,072 582 / 533, of 65,536 314 / 276.  The loss alone: 16,000 rows of 16,000 bf16 130 / 116, of 30,000 230 / 178, but 100 of 30,000 11.7 / 14.7.
 static bool in_one_workgroup(const DistillCall& c, int64_t vectors) {
     if (!c.bwd) return vectors <= 256 * 4 || (vectors <= 512 * 8 && c.a.n <= 1024);

@@ -65,7 +65,8 @@ def _check(ops, x, at, z, lse, y, w, t, alpha, what):
 KINDS = ["float32", "bfloat16", "float16"]
 # vocabularies: below a vector, around vectors, wavefronts' and workgroups' shares, slices (2048 vectors of 8 or 4), odd
 SIZES = [(5, 1, 1), (3, 2, 2), (7, 7, 3), (9, 8, 8), (6, 9, 4), (4, 64, 5), (5, 511, 16), (3, 1023, 64), (3, 1025, 1), (2, 4096, 100), (3, 4099, 33), (2, 8193, 70),
-         (3, 16_385, 64), (1, 50_021, 20), (2, 131_073, 257), (1, 1, 0), (3, 700, 0), (1, 300_007, 1024)]
+         (3, 16_385, 64), (1, 50_021, 20), (2, 131_073, 257), (1, 1, 0), (3, 700, 0), (1, 300_007, 1024),
+         (2, 7001, 8), (2, 14_003, 5), (3, 28_003, 9)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
