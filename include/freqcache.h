@@ -432,7 +432,8 @@ int distill_grad(fc_dense* d, const float* grad_loss_dev, int64_t grad_loss_stri
 /* One step of beam search: of the candidates (w, v) of each of `batch` sequences,
  *   c = scores[w] + x[w][v] - log(sum over u of exp(x[w][u])),   of a beam with finished[w] != 0 only (w, eos_id) with c = scores[w],
  * the `keep` largest in descending order: scores_out, parents_out (w), tokens_out (v), [batch][keep] each.  Of equal ones the lower beam comes first, then the larger
- * logit, then the lower id.  Candidates are compared in 64 bits, scores are rounded to 32 when stored.
+ * logit, then the lower id.  Candidates are compared in 64 bits, but the log-sum of a beam, which its candidates share, is made of sums in 32 and is off by some 1e-7 (at most 1e-5), whatever the logits
+ * have in common: candidates of different beams that are closer than that may come in either order.  Scores are rounded to 32 bits when stored.
  *   logits of `type` (F32, BF16, F16), batch * beams rows; scores fp32[batch][beams]; beams, keep: 1 to 64; tokens I32 or I64.
  *   finished uint8[batch][beams], may be NULL; finished_out uint8[batch][keep] = (token == eos_id), may be NULL; eos_id -1: none, then both are NULL.
  * A logit of -infinity is no candidate.  A beam whose score is -infinity has none (its logits are not read), nor has one whose score is +infinity or no number or whose

@@ -7,7 +7,9 @@
 // exponentials, and one workgroup for a sequence puts beams and slices together.  64 sequences of 8 beams of 131,072 bf16, the 16 best: 30 us for the first step, 4.5 TB/s; it reads
 // each logit once and writes 8 bytes of lists a candidate, but an exponential and a comparison of each element keep the vector units busy for about two thirds of that time.  The second
 // step takes 6 us, and one sequence of 4 beams 5.2 and 3.7: what waits for one another there are a few accesses.
-// The candidates are put in order in 64 bits: sums of exponentials are added up in 64 bits over the lanes, and nothing is rounded before the scores are stored.
+// The candidates are put in order in 64 bits.  What they are made of holds less: exponentials, and the sum of those that a lane has, are in 32 bits, and only lanes, wavefronts and slices are
+// added up in 64, so that a log-sum is off by some 1e-7 (an element's exponential is one instruction in 32 bits and a function in 64).  Candidates of one beam have it in common; those of
+// different beams that are closer than that may change places.
 //
 // The `keep` largest of a workgroup's elements: those above a bound that is no larger than the `keep`-th largest are few, and are ranked by
 // counting.  The bound comes of the lanes' largest elements, by ballots.
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
                 q.off = fmaxf(q.off, o.off);
             }
             const float to = from_of(wave_max(q.off));
-            v = -0.69314718055994530942 * ((double)to + log2(wave_sum(q.sum * (double)exp2f(q.off - to))));
+            v = -((double)to + log2(wave_sum(q.sum * (double)exp2f(q.off - to)))) / (double)LOG2E;      // (the constant that the exponents were made with: what it is off by cancels)
         }
         if ((lane & 63) == 0) add[w] = v + (double)score;
     }
