@@ -437,7 +437,8 @@ int distill_grad(fc_dense* d, const float* grad_loss_dev, int64_t grad_loss_stri
  *   logits of `type` (F32, BF16, F16), batch * beams rows; scores fp32[batch][beams]; beams, keep: 1 to 64; tokens I32 or I64.
  *   finished uint8[batch][beams], may be NULL; finished_out uint8[batch][keep] = (token == eos_id), may be NULL; eos_id -1: none, then both are NULL.
  * A logit of -infinity is no candidate.  A beam whose score is -infinity has none (its logits are not read), nor has one whose score is +infinity or no number or whose
- * logits hold a +infinity or one that is no number.  Where fewer than `keep` candidates are left the remaining places hold score -infinity, parent 0, token max(eos_id, 0). */
+ * logits hold a +infinity or one that is no number.  Finite logits count wherever they are: ids masked by -1e10 or by the type's lowest value are candidates, far down, and where all of a beam's are
+ * that, equal ones (a score below the lowest number of 32 bits is stored as -infinity).  Where fewer than `keep` candidates are left the remaining places hold score -infinity, parent 0, token max(eos_id, 0). */
 int beam_select(fc_dense* d, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t batch, int32_t beams, int32_t dim, const float* scores_dev,
                 const uint8_t* finished_dev, int32_t eos_id, int32_t keep, float* scores_out_dev, int32_t* parents_out_dev, void* tokens_out_dev, int32_t token_type,
                 uint8_t* finished_out_dev);

@@ -30,10 +30,10 @@ struct BeamArgs {
     const uint8_t* finished;                       // or NULL
     int32_t beams, dim, keep, eos, slices;
 };
-// What a slice leaves: 2^off * sum = its sum of 2^(x log2(e)); its largest logits are a list of `keep`, filled up with -infinity.  A sequence's lists lie side by side, the first entries
+// What a slice leaves: its largest logit `from`, and its sum of 2^(c (x - from)), c = log2(e) rounded to 32 bits; its largest logits are a list of `keep`, filled up with -infinity.  A sequence's lists lie side by side, the first entries
 // of all before the second ones: what neighbouring lanes of the next step hold is of different lists, and the first of a lane's is its largest, which makes its bound a good one (the other
 // way round more than BEAM_LIST candidates passed it, and 5 sequences of 32 beams of 131,072 bf16, the 32 best, took 124 us, not 35).
-struct BeamSlice { double sum; float off; };
+struct BeamSlice { double sum; float from; };
 struct BeamEntry { float x; uint32_t id; };        // id: and the beam, above it
 constexpr int BEAM_SHIFT = 24;
 static_assert(DENSE_MAX_DIM <= 1 << BEAM_SHIFT && BEAM_MOST <= 1 << (32 - BEAM_SHIFT));
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
     constexpr int N = Slice::N, WAVES = LOGIT_THREADS / 64;
     __shared__ uint64_t list[BEAM_LIST], few[BEAM_LIST];
     __shared__ uint64_t best[WAVES];
-    __shared__ float offs[WAVES];
+    __shared__ float froms[WAVES];
     __shared__ double parts[WAVES];
     __shared__ uint32_t bounds[WAVES];
     __shared__ int count, kept;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         for (int k = 1; k < WAVES; ++k) b = min(b, __hip_atomic_load(&bounds[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         return max(b, LOWEST);
     };
-    float lane_top = -INFINITY, off = -INFINITY, sum = 0.f, least = -INFINITY;
+    float lane_top = -INFINITY, sum = 0.f, least = -INFINITY;
     for (int base = begin; base < end; base += Slice::COLUMNS) {
         const int lane = here(threadIdx.x);
         if (base > begin) s.load_long(x, base, lane, a.dim, true);
@@ -137,10 +137,10 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         const float top = s.largest();
         s.forget();
         // sum of exponentials, each lane's from its own largest element so far
-        const float to = fmaxf(off, top * LOG2E);
-        sum = sum * __builtin_amdgcn_exp2f(off - from_of(to)) + s.exponentials(LOG2E, from_of(to));
-        off = to;
-        lane_top = fmaxf(lane_top, top);
+        const float to = fmaxf(lane_top, top);
+        const Exponents f = exponents(to, LOG2E);
+        sum = sum * part_of(lane_top, to, LOG2E) + s.exponentials(f.scale, f.off) * f.back;
+        lane_top = to;
         if (base > begin && !__any(top >= least)) continue;
         const uint32_t mine = wave_bound(ordered(lane_top), (a.keep + WAVES - 1) / WAVES);
         if ((lane & 63) == 0) __hip_atomic_store(&bounds[lane >> 6], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
@@ -170,9 +170,9 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
             }
         }
     }
-    const float off_wave = wave_max(off);
-    const double sum_wave = wave_sum((double)(sum * __builtin_amdgcn_exp2f(off - from_of(off_wave))));
-    if ((lane & 63) == 0) { offs[lane >> 6] = off_wave; parts[lane >> 6] = sum_wave; }
+    const float from_wave = wave_max(lane_top);
+    const double sum_wave = wave_sum((double)(sum * part_of(lane_top, from_wave, LOG2E)));
+    if ((lane & 63) == 0) { froms[lane >> 6] = from_wave; parts[lane >> 6] = sum_wave; }
     __syncthreads();
     auto put = [&](int at, uint64_t key) { out[at * all] = BeamEntry{unordered((uint32_t)(key >> 32)), beam | ~(uint32_t)key}; };
     const uint64_t lowest = (uint64_t)bound() << 32;
@@ -206,10 +206,10 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
         }
     }
     if (lane == 0) {
-        float to = offs[0];
-        for (int k = 1; k < WAVES; ++k) to = fmaxf(to, offs[k]);
+        float to = froms[0];
+        for (int k = 1; k < WAVES; ++k) to = fmaxf(to, froms[k]);
         double total = 0.;
-        for (int k = 0; k < WAVES; ++k) total += parts[k] * (double)exp2f(offs[k] - from_of(to));
+        for (int k = 0; k < WAVES; ++k) total += parts[k] * (double)part_of(froms[k], to, LOG2E);
         sums[blockIdx.x] = BeamSlice{total, to};
     }
 }
@@ -237,7 +237,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
                                                             float* __restrict__ scores_out, int32_t* __restrict__ parents_out, void* __restrict__ tokens_out,
                                                             int32_t token_type, uint8_t* __restrict__ finished_out) {
     constexpr int WAVES = JOIN_THREADS / 64;
-    __shared__ double add[BEAM_MOST];              // what a beam's logits lack to be candidates; not finite: there are none
+    __shared__ double add[BEAM_MOST];              // what a beam's logits, less its largest, lack to be candidates; not finite: there are none
+    __shared__ float tops[BEAM_MOST];              // (far from zero the log-sum itself would be lost in the sum with its largest logit)
     __shared__ uint32_t bounds[WAVES], shares[WAVES], highs[WAVES];
     __shared__ double list_c[BEAM_LIST];           // and bins
     __shared__ Candidate list[BEAM_LIST];
@@ -257,18 +258,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
         const float score = a.scores[row0 + w];
         const bool lives = score - score == 0.f, end = a.finished && a.finished[row0 + w];
         double v = lives ? 0. : -INFINITY;
+        float top = 0.f;
         if (lives && !end) {
             if ((lane & 63) >= a.slices) q = BeamSlice{0., -INFINITY};
             for (int k = (lane & 63) + 64; k < a.slices; k += 64) {
                 const BeamSlice o = s[k];
-                const float to = from_of(fmaxf(q.off, o.off));
-                q.sum = q.sum * (double)exp2f(q.off - to) + o.sum * (double)exp2f(o.off - to);
-                q.off = fmaxf(q.off, o.off);
+                const float to = fmaxf(q.from, o.from);
+                q.sum = q.sum * (double)part_of(q.from, to, LOG2E) + o.sum * (double)part_of(o.from, to, LOG2E);
+                q.from = to;
             }
-            const float to = from_of(wave_max(q.off));
-            v = -((double)to + log2(wave_sum(q.sum * (double)exp2f(q.off - to)))) / (double)LOG2E;      // (the constant that the exponents were made with: what it is off by cancels)
+            top = from_of(wave_max(q.from));
+            v = -log2(wave_sum(q.sum * (double)part_of(q.from, top, LOG2E))) / (double)LOG2E;      // (the constant that the exponents were made with: what it is off by cancels)
         }
-        if ((lane & 63) == 0) add[w] = v + (double)score;
+        if ((lane & 63) == 0) { add[w] = v + (double)score; tops[w] = top; }
     }
     if (lane == 0) count = 0;
     __syncthreads();
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
             if (e.x == -INFINITY) return;
             const int w = e.id >> BEAM_SHIFT;
             const double v = add[w];
-            if (v - v == 0.) used |= f(Candidate{v + (double)e.x, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
+            if (v - v == 0.) used |= f(Candidate{((double)e.x - (double)tops[w]) + v, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
         };
         if constexpr (HELD) {
             used = false;

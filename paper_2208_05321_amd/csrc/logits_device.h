@@ -223,4 +223,20 @@ struct RowSlice {
 // exponentials are taken from `from`: the largest element, or 0 where all are -infinity
 __device__ __forceinline__ float from_of(float m) { return m == -INFINITY ? 0.f : m; }
 
+// How exponentials are taken from an element `from`, the largest: 2^(c (x - from)) = back * 2^(fma(x, scale, -off)), one instruction before an element's exponential, where a difference first and
+// its product would be two.  off is the rounded product of `from`, and back mends its rounding, which reaches 2^32 where the product reaches 2^30, and beyond the range of numbers further out.  From there on elements
+// are so far apart (2^-24 of themselves at least: 64 and more in the exponent) that only those equal to the largest count: scale is a power of two then, which makes the products exact, and they are some
+// 2^40, which leaves nothing of the others.  (c: log2(e) over a temperature of 1/1024 to 1024.)  Infinite or no number: all exponentials are none.
+struct Exponents { float scale, off, back; };
+__device__ __forceinline__ Exponents exponents(float from, float c) {
+    from = from_of(from);
+    const float off = from * c;
+    const bool far = !(fabsf(off) < 0x1p30f);
+    const float scale = far ? __builtin_bit_cast(float, (294u << 23) - (__builtin_bit_cast(uint32_t, from) & 0x7f800000u)) : c;      // 2^(40 - from's exponent)
+    const float o = far ? from * scale : off;
+    return Exponents{scale, o, __builtin_amdgcn_exp2f(fmaf(-from, scale, o))};
+}
+// What a sum of exponentials from `from` counts as in one from `to`, no smaller.
+__device__ __forceinline__ float part_of(float from, float to, float c) { return __builtin_amdgcn_exp2f((from - from_of(to)) * c); }
+
 }  // namespace fc
