@@ -411,8 +411,8 @@ int grad_norm_clip(fc_dense* d, const void* const* grads_dev, void* const* out_d
  * Sums are over the row's entries: an id that is named twice counts twice among P, and once among those that Q_0 leaves out.  Terms with P = 0, and with a factor a or 1 - a of 0, are 0.  A row without
  * entries (or, without teacher_lse, with entries of -infinity only) has no first term (and is left out where a is 1).  A target of -1 leaves the row out: its loss and gradient are 0, whatever its
  * logits hold; other ids outside [0, dim) raise the sticky FC_ERR_ID_OUT_OF_RANGE, an entry then does not count, and a row with such a target is left out.
- * Logits of -infinity are ids of probability 0; rows with logits that are +infinity, no number or all -infinity have a loss and a gradient that are no numbers.  Logits
- * over the temperature are below 2^126 in magnitude.  targets may be NULL where alpha is 1.
+ * Logits of -infinity are ids of probability 0; rows with logits that are +infinity, no number or all -infinity have a loss and a gradient that are no numbers.  Finite logits count wherever they
+ * are: ids masked by -1e10 or by the type's lowest value have a probability of 0 too, but where all are that, equal ones; a loss beyond the range of 32 bits is infinite.  targets may be NULL where alpha is 1.
  *   type, teacher_type F32, BF16, F16; id_type (teacher_ids [n][top]) and target_type I32 or I64; loss fp32[n];
  *   stats fp32[n][12]: what distill_bwd needs of the forward pass (of no meaning otherwise). */
 int distill_fwd(fc_dense* d, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t n, int32_t dim, const void* teacher_ids_dev, int32_t id_type,

@@ -20,7 +20,7 @@ namespace fc {
 
 constexpr int DISTILL_MAX_TOP = 1024;
 constexpr int STATS = 12;                          // numbers of a row that the forward pass leaves for the backward pass
-enum { ST_OFF, ST_COEF, ST_OFF1, ST_COEF1, ST_ALL, ST_INV, ST_ALL1, ST_INV1, ST_NAMED, ST_ZFROM, ST_ZINV, ST_KIND };
+enum { ST_REST, ST_COEF, ST_COEF1, ST_ALL, ST_INV, ST_INV1, ST_NAMED, ST_ZFROM, ST_ZINV, ST_KIND };      // (and two zeros)
 // ST_KIND
 constexpr float ROW_OUT = 0.f, ROW_TARGET_ONLY = 1.f, ROW_ENTRIES = 2.f;
 
@@ -58,32 +58,28 @@ __device__ __forceinline__ bool row_target(const DistillArgs& a, int64_t row, in
     return *y >= 0;
 }
 
-// Sums of exponentials at the temperature and at 1: t = sum of 2^(x ct - off), ct = log2(e) / T rounded to 32 bits; one = sum of 2^(x log2(e) - off1).  The offsets are the
-// rounded products of the largest element, and what is joined or taken further goes by the offsets, so that their rounding cancels (2e-6 of
-// each exponential for logits of 30 otherwise), and so does that of ct but for its share in differences from the largest.
+// Sums of exponentials at the temperature and at 1, from an element of the logits: t = sum of 2^(ct (x - from)), ct = log2(e) / T rounded to 32 bits, and one = sum of 2^(log2(e) (x - from)).  What the
+// rounding of ct makes is in proportion to differences from the largest element, not to the logits; without `two` (the sums at 1 are others than those at the temperature) one is t.
 struct Sums {
-    float off, off1, t, one;
-    __device__ __forceinline__ void join(const Sums& o) {
-        const float most = fmaxf(off, o.off), most1 = fmaxf(off1, o.off1), to = from_of(most), to1 = from_of(most1);
-        t = t * __builtin_amdgcn_exp2f(off - to) + o.t * __builtin_amdgcn_exp2f(o.off - to);
-        one = one * __builtin_amdgcn_exp2f(off1 - to1) + o.one * __builtin_amdgcn_exp2f(o.off1 - to1);
-        off = most;
-        off1 = most1;
+    float from, t, one;
+    __device__ __forceinline__ void join(const Sums& o, float ct, bool two) {
+        const float most = fmaxf(from, o.from);
+        if (two) one = one * part_of(from, most, LOG2E) + o.one * part_of(o.from, most, LOG2E);
+        t = t * part_of(from, most, ct) + o.t * part_of(o.from, most, ct);
+        if (!two) one = t;
+        from = most;
     }
-    // over the wavefront's lanes; two: the sums at 1 are others than those at the temperature
-    __device__ __forceinline__ Sums over_wave(bool two) const {
+    // over the wavefront's lanes
+    __device__ __forceinline__ Sums over_wave(float ct, bool two) const {
         Sums s;
-        s.off = s.off1 = wave_max(off);
-        s.t = s.one = wave_sum(t * __builtin_amdgcn_exp2f(off - from_of(s.off)));
-        if (two) {
-            s.off1 = wave_max(off1);
-            s.one = wave_sum(one * __builtin_amdgcn_exp2f(off1 - from_of(s.off1)));
-        }
+        s.from = wave_max(from);
+        s.t = s.one = wave_sum(t * part_of(from, s.from, ct));
+        if (two) s.one = wave_sum(one * part_of(from, s.from, LOG2E));
         return s;
     }
 };
 constexpr double LN2 = 0.69314718055994530942;
-constexpr Sums NO_SUMS{-INFINITY, -INFINITY, 0.f, 0.f};
+constexpr Sums NO_SUMS{-INFINITY, 0.f, 0.f};
 // What is left of a row, or of a slice, without the named ids where P_0 needs that; twice: an id was seen to be named more than once.
 struct RowSums { Sums rest; float twice; };
 
@@ -129,15 +125,13 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, f
             if (s.twice != 0.f)
                 for (int j = 0; j < k; ++j) counts &= t.id[j] != id;
             if (!counts) continue;
-            const float x = t.x[k];
-            Sums q{x * ct, x * (two ? LOG2E : ct), 0.f, 0.f};
-            q.t = __builtin_amdgcn_exp2f(fmaf(x, ct, -from_of(q.off)));
-            q.one = two ? __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from_of(q.off1))) : q.t;
-            named.join(q);
+            const float x = t.x[k], one = x == -INFINITY ? 0.f : 1.f;
+            named.join(Sums{x, one, one}, ct, two);
         }
-        all.join(named.over_wave(two));
+        all.join(named.over_wave(ct, two), ct, two);
     }
-    const double lse2 = (double)all.off + (double)log2f(all.t);
+    const float from = from_of(all.from);
+    const double log_t = (double)log2f(all.t);
 
     float zmax = -INFINITY;
     bool some = false;
@@ -170,42 +164,41 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, f
             t.z[k] = p;
             part += p;
             if (p == 0.f) continue;                // nothing, also where the student gives nothing
-            const double log_q = ((double)t.x[k] * ct - lse2) * LN2;
+            const double log_q = (((double)t.x[k] - from) * ct - log_t) * LN2;
             kl += p * (float)(d + log_zinv - log_q);
         }
         kl = wave_sum(kl);
         sum_p = wave_sum(part);
         if (a.lse) {
             p0 = fmaxf(0.f, 1.f - sum_p);
-            const double log_q0 = ((double)s.rest.off + (double)log2f(s.rest.t) - lse2) * LN2;
+            const double log_q0 = (((double)s.rest.from - from) * ct + (double)log2f(s.rest.t) - log_t) * LN2;
             q0 = expf((float)log_q0);
             if (p0 > 0.f) kl += p0 * (logf(p0) - (float)log_q0);
         }
     }
     if (lane != 0) return;
     float value = some ? a.alpha * a.temperature * a.temperature * kl : 0.f;
-    if (a.alpha < 1.f) value += (1.f - a.alpha) * (float)(((double)all.off1 + (double)log2f(all.one) - (double)xy * LOG2E) * LN2);
+    if (a.alpha < 1.f) value += (1.f - a.alpha) * (float)((((double)from - xy) * LOG2E + (double)log2f(all.one)) * LN2);
     if (loss) loss[row] = value;
     const float c = sum_p + p0;
     float coef = 0.f, coef1 = 0.f;
     if (s.rest.t != 0.f) {                         // (else there is nothing that is not named, or only logits of -infinity)
-        if (some) coef = a.alpha * a.temperature * (c * q0 - p0) / s.rest.t;
-        if (a.alpha < 1.f) coef1 = (1.f - a.alpha) * exp2f(s.rest.off1 - all.off1) / all.one;
+        if (some) coef = a.alpha * a.temperature * (c * q0 - p0) / s.rest.t * exponents(s.rest.from, ct).back;
+        if (a.alpha < 1.f) coef1 = (1.f - a.alpha) * exp2f((s.rest.from - from) * LOG2E) / all.one * exponents(s.rest.from, LOG2E).back;
     }
     if (all.t == 0.f) coef = NAN;                  // all logits are -infinity
     const bool one = a.temperature == 1.f;         // one exponential stands for both
-    stats[ST_OFF] = from_of(s.rest.off);
+    stats[ST_REST] = s.rest.from;
     stats[ST_COEF] = one ? coef + coef1 : coef;
-    stats[ST_OFF1] = from_of(s.rest.off1);
     stats[ST_COEF1] = one ? 0.f : coef1;
-    stats[ST_ALL] = all.off;
+    stats[ST_ALL] = from;
     stats[ST_INV] = 1.f / all.t;
-    stats[ST_ALL1] = all.off1;
     stats[ST_INV1] = 1.f / all.one;
     stats[ST_NAMED] = c;
     stats[ST_ZFROM] = zmax;
     stats[ST_ZINV] = zinv;
     stats[ST_KIND] = some ? ROW_ENTRIES : a.alpha < 1.f ? ROW_TARGET_ONLY : ROW_OUT;
+    for (int k = ST_KIND + 1; k < STATS; ++k) stats[k] = 0.f;
 }
 
 __device__ __forceinline__ void distill_left_out(int64_t row, int lane, float* loss, float* stats) {
@@ -259,42 +252,47 @@ __device__ __forceinline__ void add_slice(const DistillArgs& a, RowSlice<T, LANE
     s.forget();
     const float top = s.largest();
     s.forget();
-    r.off = r.off1 = top * ct;
-    r.t = r.one = s.exponentials(ct, from_of(r.off));
+    const Exponents f = exponents(top, ct);
+    r.from = top;
+    r.t = r.one = s.exponentials(f.scale, f.off) * f.back;
     if (a.alpha < 1.f && a.temperature != 1.f) {
-        r.off1 = top * LOG2E;
+        const Exponents f1 = exponents(top, LOG2E);
         s.forget();
-        r.one = s.exponentials(LOG2E, from_of(r.off1));
+        r.one = s.exponentials(f1.scale, f1.off) * f1.back;
     }
 }
 // of all the wavefronts of a row, in the first of them
 template <int LANES>
 __device__ __forceinline__ void join_waves(const DistillArgs& a, Sums& r, Sums* lds) {
     const bool two = a.alpha < 1.f && a.temperature != 1.f;
-    r = r.over_wave(two);
+    const float ct = scale_of(a);
+    r = r.over_wave(ct, two);
     if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = r;
         __syncthreads();
         if (threadIdx.x >= 64) return;
         r = threadIdx.x < LANES / 64 ? lds[threadIdx.x] : NO_SUMS;
-        r = r.over_wave(two);
+        r = r.over_wave(ct, two);
     }
 }
 
 // The gradient of a slice in the place of its logits, but for the named ids' and the target's.
 template <class T, int LANES, int PER>
 __device__ __forceinline__ void slice_grad(const DistillArgs& a, RowSlice<T, LANES, PER>& s, float g, const float* st) {
-    const float ct = scale_of(a), off = st[ST_OFF], off1 = st[ST_OFF1], coef = g * st[ST_COEF], coef1 = g * st[ST_COEF1];
+    const Exponents f = exponents(st[ST_REST], scale_of(a)), f1 = exponents(st[ST_REST], LOG2E);        // (their mends are in the coefficients)
+    // (All lanes have the same.  Left to the compiler they are in vector registers, one wavefront a SIMD less for rows of 12,000 16-bit columns; us, none / these / all in scalar ones, loss and gradient
+    // of 16,384 rows of 32,768 bf16 434 / 430 / 415, of 4000 of 24,000 91 / 87 / 88, of 131,072 487 / 467 / 464, of 8000 of 30,000 at temperature 2 218 / 224 / 233.)
+    const float scale = scalar(f.scale), scale1 = scalar(f1.scale), coef = g * st[ST_COEF], coef1 = scalar(g * st[ST_COEF1]);
     const bool two = a.alpha < 1.f && a.temperature != 1.f;
     constexpr int N = RowSlice<T, LANES, PER>::N;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {                // (the choice inside: outside, every element would be converted before it)
         float v[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(s.at(k, e), ct, -off));
+        for (int e = 0; e < N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(s.at(k, e), scale, -f.off));
         if (two) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = fmaf(coef1, __builtin_amdgcn_exp2f(fmaf(s.at(k, e), LOG2E, -off1)), v[e]);
+            for (int e = 0; e < N; ++e) v[e] = fmaf(coef1, __builtin_amdgcn_exp2f(fmaf(s.at(k, e), scale1, -f1.off)), v[e]);
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) s.x[k][e] = (T)v[e];
@@ -305,7 +303,7 @@ template <class T, int LANES>
 __device__ __forceinline__ void mend(const DistillArgs& a, float g, const float* st, const Entries& t, int y, float xy, int base, int end, int lane, T* out) {
     const float ct = scale_of(a), scale = a.alpha * a.temperature, hard = 1.f - a.alpha;
     const int entries = st[ST_KIND] == ROW_ENTRIES ? a.top : 0;
-    const bool here = a.alpha < 1.f && y >= base && y < end;
+    const bool target = a.alpha < 1.f && y >= base && y < end;
     bool y_named = false;
     for (int k = lane; k < entries; k += LANES) {
         const int id = t.id[k];
@@ -324,15 +322,20 @@ __device__ __forceinline__ void mend(const DistillArgs& a, float g, const float*
         }
         y_named |= id == y;
         if (!first) continue;
-        const float q = exp2f(fmaf(t.x[k], ct, -st[ST_ALL])) * st[ST_INV], q1 = a.alpha < 1.f ? exp2f(fmaf(t.x[k], LOG2E, -st[ST_ALL1])) * st[ST_INV1] : 0.f;
+        const float d = t.x[k] - st[ST_ALL], q = exp2f(d * ct) * st[ST_INV], q1 = a.alpha < 1.f ? exp2f(d * LOG2E) * st[ST_INV1] : 0.f;
         out[id] = (T)(g * (scale * (st[ST_NAMED] * q - sum) + hard * (q1 - (id == y ? 1.f : 0.f))));
     }
-    if (here) {                                    // (the same in all lanes of the row)
+    if (target) {                                  // (the same in all lanes of the row)
         if constexpr (LANES > 64) y_named = __syncthreads_or(y_named);
         else y_named = __any(y_named);
         if (!y_named && lane == 0) {
-            float v = g * st[ST_COEF] * __builtin_amdgcn_exp2f(fmaf(xy, ct, -st[ST_OFF]));
-            if (a.temperature != 1.f) v = fmaf(g * st[ST_COEF1], __builtin_amdgcn_exp2f(fmaf(xy, LOG2E, -st[ST_OFF1])), v);
+            const float rest = here(st[ST_REST]);
+            const Exponents f = exponents(rest, ct);
+            float v = g * st[ST_COEF] * __builtin_amdgcn_exp2f(fmaf(xy, f.scale, -f.off));
+            if (a.temperature != 1.f) {
+                const Exponents f1 = exponents(rest, LOG2E);
+                v = fmaf(g * st[ST_COEF1], __builtin_amdgcn_exp2f(fmaf(xy, f1.scale, -f1.off)), v);
+            }
             out[y] = (T)(v - g * hard);
         }
     }
@@ -425,13 +428,15 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_distill_slice(DistillArgs a, 
 
 // The sums of a row's slices, by a wavefront.
 __device__ __forceinline__ RowSums row_sums(const DistillArgs& a, const RowSums* __restrict__ part, int64_t row, int slices) {
+    const float ct = scale_of(a);
+    const bool two = a.alpha < 1.f && a.temperature != 1.f;
     RowSums r{NO_SUMS, 0.f};
     for (int k = threadIdx.x & 63; k < slices; k += 64) {
         const RowSums q = part[row * slices + k];
-        r.rest.join(q.rest);
+        r.rest.join(q.rest, ct, two);
         r.twice = fmaxf(r.twice, q.twice);
     }
-    r.rest = r.rest.over_wave(a.alpha < 1.f && a.temperature != 1.f);
+    r.rest = r.rest.over_wave(ct, two);
     r.twice = __any(r.twice != 0.f) ? 1.f : 0.f;
     return r;
 }

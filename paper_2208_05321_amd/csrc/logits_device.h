@@ -22,11 +22,15 @@ __device__ __forceinline__ float wave_max(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// The lane's number, as a value of this place of the program: what follows from it is worked out here, and not kept in registers from before a loop, or for after it.
-__device__ __forceinline__ int here(int lane) {
-    asm volatile("" : "+v"(lane));
-    return lane;
+// A number (a lane's, for instance) as a value of this place of the program: what follows from it is worked out here, and not kept in registers from before a loop, or for after it.
+template <class N>
+__device__ __forceinline__ N here(N n) {
+    asm volatile("" : "+v"(n));
+    return n;
 }
+
+// A number that all of a wavefront's lanes have, in a scalar register.
+__device__ __forceinline__ float scalar(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 
 // The largest of three; NaN only if all are.  (Written as one instruction: of maxima of elements of 16 bits the compiler makes maxima in 16 bits, and of those, in bf16,
 // maxima in 32 bits that are converted back each, three instructions more an element.)
