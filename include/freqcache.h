@@ -408,7 +408,9 @@ int grad_norm_clip(fc_dense* d, const void* const* grads_dev, void* const* out_d
  *         the entries leave over;  teacher_lse NULL: L is that of the row's entries, and P_0 = 0
  *   Q = softmax(x / T), Q_0 = the sum of Q over the ids that no entry names
  *   loss[i] = a T^2 (sum P_k (log P_k - log Q[t_k]) + P_0 (log P_0 - log Q_0)) + (1 - a) (-log softmax(x)[y])
- * Sums are over the row's entries: an id that is named twice counts twice among P, and once among those that Q_0 leaves out.  Terms with P = 0, and with a factor a or 1 - a of 0, are 0.  A row without
+ * Sums are over the row's entries: an id that is named twice counts twice among P, and once among those that Q_0 leaves out.  Terms with P = 0, and with a factor a or 1 - a of 0, are 0.
+ * Of a teacher whose entries hold everything P_0 is what roundings leave over: where Q_0 is 0 in 32 bits a P_0 of no more than 2^-23 (|L| + |max z / T - L| + top / 64 + 16) counts as 0.
+ * (A larger one makes the loss infinite where the other ids are masked by -infinity, and as large as the mask where that is finite.)  A row without
  * entries (or, without teacher_lse, with entries of -infinity only) has no first term (and is left out where a is 1).  A target of -1 leaves the row out: its loss and gradient are 0, whatever its
  * logits hold; other ids outside [0, dim) raise the sticky FC_ERR_ID_OUT_OF_RANGE, an entry then does not count, and a row with such a target is left out.
  * Logits of -infinity are ids of probability 0; rows with logits that are +infinity, no number or all -infinity have a loss and a gradient that are no numbers.  Finite logits count wherever they

@@ -173,6 +173,9 @@ __device__ __forceinline__ void distill_row(const DistillArgs& a, int64_t row, f
             p0 = fmaxf(0.f, 1.f - sum_p);
             const double log_q0 = (((double)s.rest.from - from) * ct + (double)log2f(s.rest.t) - log_t) * LN2;
             q0 = expf((float)log_q0);
+            // Of a teacher whose entries hold everything P_0 is what roundings leave: of the log-sum, of the exponents and of their sum, half a unit of 32 bits of each, and as much again for a log-sum worked out
+            // in 32 bits.  Where the student gives the others nothing that would cost infinitely much, or whatever number masks them.
+            if (q0 == 0.f && p0 <= 0x1p-23f * (fabsf(lse) + fabsf((float)log_zinv) + (float)a.top / 64 + 16.f)) p0 = 0.f;
             if (p0 > 0.f) kl += p0 * (logf(p0) - (float)log_q0);
         }
     }
