@@ -35,6 +35,9 @@ def _gradient(x, at, z, lse, y, t, alpha):
     grad = alpha * t * (c * q - torch.zeros_like(xd).scatter_add_(1, at.long(), p) - p0[:, None] * r)
     off = alpha * t * (c * (q * (2 * SUM_STEPS + 40) + 4 * small(logq)) * U32 + torch.zeros_like(xd).scatter_add_(1, at.long(), p * (rel_p[:, None] + 4 * U32))
                        + off_p0[:, None] * (q + r) + p0[:, None] * (r * (SUM_STEPS + 24) + 2 * small(logr)) * U32)
+    # An exponential below 2^-126 is 0; they are taken from the rounded product of the largest, off by up to 32 in the exponent before it counts as far: 2^-94 of the probability's factor.  From a product of 2^30 on only what
+    # is equal to the largest counts: f32's neighbours of it are 2^-24 of it, or 64 in the exponent, away: 2^-64.
+    off = off + (alpha * t * c + 1 - alpha) * 2.0 ** -64
     if alpha < 1:
         log1 = torch.log_softmax(x.double(), 1)
         hit = torch.zeros_like(xd).scatter_(1, y.long()[:, None], 1.0)
@@ -116,4 +119,29 @@ def test_a_common_offset(ops, kind, rest):
             for t, alpha in ((1.0, 0.5), (2.0, 0.5), (0.7, 1.0)):
                 x, at, z, lse, y, w = _inputs(n, v, top, torch.float32, v, rest, t)
                 _check(ops, (x + offset).to(k), at, z, lse, y, w, t, alpha, (kind, offset, v, rest, t, alpha))
+    ops.check()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("t", [2.0 ** -10, 2.0 ** 10])
+def test_the_temperatures_limits(ops, t, kind, rest):
+    """Scales from a thousandth to a thousand times: where logits count as far from zero moves with them."""
+    import torch
+    k = getattr(torch, kind)
+    for far in (30.0, 6e4) + ((1e6, 3e7, 1e12, 3e12, 1e30) if kind != "float16" else ()):
+        for n, v, top in ((12, 300, 8), (12, 40_000, 16)):
+            for alpha in (1.0, 0.5):
+                x, at, z, lse, y, w = _inputs(n, v, top, k, v, rest, t)
+                x, z = (x.float() * min(t, 1.0)).to(k), z * t        # (distances that make sense over this temperature; those of cross entropy, beside, do not matter)
+                lse = (torch.logsumexp(z.double() / t, 1) + 0.3).float() if rest else None
+                keep = torch.zeros_like(x, dtype=torch.bool).scatter_(1, at, True)
+                keep[torch.arange(n), y] = True
+                x[0][~keep[0]] = -far
+                x[1, v // 3:] = torch.where(keep[1, v // 3:], x[1, v // 3:], -far)
+                x[2], x[3] = -far, far
+                x[4, (at[4, 0] + 1) % v] = far
+                x[5, at[5, 0]] = far
+                x[6] = (far * (1 + 0.01 * torch.rand(v, device="cuda"))).to(k)
+                _check(ops, x, at, z, lse, y, w, t, alpha, (n, v, kind, far, rest, t, alpha))
     ops.check()
