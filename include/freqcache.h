@@ -453,7 +453,8 @@ typedef struct {
     int64_t piece_bytes, pieces;
 } fc_state;
 /* Reordering of the states of beams: for every tensor, row b * keep + j of dst = row b * beams + parents[b][j] of src.  parents [batch][keep], I32 or I64; beams, keep: 1 to 64.
- * dst may be src (then keep == beams, and the strides are the same): rows that are their own parent are not touched.  Tensors do not overlap otherwise.
+ * dst may be src (then keep == beams, and the strides are the same): rows that are their own parent are not touched.  Tensors do not overlap otherwise, and none that is written overlaps
+ * the parents (dst == parents_dev is refused).
  * A parent outside [0, beams) raises the sticky FC_ERR_ID_OUT_OF_RANGE; its row of dst becomes zeros, in place it stays as it was.  `states` is a host array, read before the call
  * returns; pieces and piece_bytes below 2^31, a row below 2^35 bytes. */
 int beam_reorder(fc_dense* d, const fc_state* states, int32_t count, int64_t batch, int32_t beams, const void* parents_dev, int32_t parent_type, int32_t keep);

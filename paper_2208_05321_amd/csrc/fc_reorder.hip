@@ -126,7 +126,7 @@ int beam_reorder(fc_dense* d, const fc_state* states, int32_t count, int64_t bat
         const fc_state& s = states[k];
         if (s.piece_bytes < 0 || s.pieces < 0) return FC_ERR_INVALID_ARG;
         if (s.piece_bytes == 0 || s.pieces == 0 || batch == 0) continue;
-        if (!s.src || !s.dst || s.pieces >= (int64_t)1 << 31 || s.piece_bytes >= (int64_t)1 << 31 || cdiv(s.piece_bytes, 16) * s.pieces >= (int64_t)1 << 31 ||
+        if (!s.src || !s.dst || s.dst == parents_dev || s.pieces >= (int64_t)1 << 31 || s.piece_bytes >= (int64_t)1 << 31 || cdiv(s.piece_bytes, 16) * s.pieces >= (int64_t)1 << 31 ||
             (s.pieces > 1 && (s.src_piece < s.piece_bytes || s.dst_piece < s.piece_bytes)) ||
             s.src_row < (s.pieces - 1) * s.src_piece + s.piece_bytes || s.dst_row < (s.pieces - 1) * s.dst_piece + s.piece_bytes ||
             (s.src == s.dst && (keep != beams || s.src_row != s.dst_row || (s.pieces > 1 && s.src_piece != s.dst_piece))))

@@ -513,7 +513,8 @@ class DenseOps:
         """states[k][b, j] = states[k][b, parents[b, j]] for tensors [batch, beams, ...] of any type, in place; or into the tensors of `out` [batch, keep, ...].  Returns the tensors
         written.  parents [batch, keep] (int32, int64).  A row (what follows the first two dimensions) is neighbouring elements, or pieces of them at one distance, such as the filled
         part of a cache [batch, beams, heads, room, dim].  A parent outside [0, beams) raises the sticky error; its row becomes zeros, in place it stays as it was.
-        Tensors share no memory, except that out[k] may be states[k]."""
+        Tensors share no memory, except that out[k] may be states[k]; `parents` is none of those that are written.  The rows of all beams and sequences of a tensor are one distance apart: some of the
+        beams of a wider buffer (buffer[:, :beams]) are refused."""
         states = list(states)
         pk = self._ids(parents)
         if parents.dim() != 2 or not states:
@@ -543,6 +544,8 @@ class DenseOps:
         written = table[1::8]
         if len(set(written)) < len(written) or (given and not set(written).isdisjoint(table[::8])):
             self._apart(table)
+        if parents.data_ptr() in written and parents.numel():
+            _refuse("parents: one of the tensors that are written")
         table = array("q", table)
         self._run("beam_reorder", self._L.beam_reorder, (states, out, (parents,)), table.buffer_info()[0], len(states), batch, beams, parents.data_ptr(), pk, keep)
         self._written(out)
