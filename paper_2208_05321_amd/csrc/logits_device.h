@@ -190,13 +190,18 @@ struct RowSlice {
         for (int k = 0; k < PER; ++k) if (largest(k) >= least) at |= 1u << k;
         return at;
     }
-    // sum of 2^(x c - off)
+    // sum of 2^(x c - off); 64 elements are added one after the other, at most
     __device__ __forceinline__ float exponentials(float c, float off) const {
         float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < PER; ++k)
+        for (int j = 0; j < PER; j += 64 / N) {
+            float part = 0.f;
 #pragma unroll
-            for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(at(k, e), c, -off));
+            for (int k = j; k < j + 64 / N && k < PER; ++k)
+#pragma unroll
+                for (int e = 0; e < N; ++e) part += __builtin_amdgcn_exp2f(fmaf(at(k, e), c, -off));
+            sum = j ? sum + part : part;
+        }
         return sum;
     }
     // Stores the slice, whose elements are results by now, but for the row's last vector where that is not a whole one; that is the business of one lane of the row, at the
