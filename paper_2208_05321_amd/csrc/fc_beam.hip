@@ -238,7 +238,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
                                                             int32_t token_type, uint8_t* __restrict__ finished_out) {
     constexpr int WAVES = JOIN_THREADS / 64;
     __shared__ double add[BEAM_MOST];              // what a beam's logits, less its largest, lack to be candidates; not finite: there are none
-    __shared__ float tops[BEAM_MOST];              // (far from zero the log-sum itself would be lost in the sum with its largest logit)
+    __shared__ double tops[BEAM_MOST];             // their largest (far from zero the log-sum itself would be lost in its sum with that); in 64 bits, which saves a conversion a candidate
     __shared__ uint32_t bounds[WAVES], shares[WAVES], highs[WAVES];
     __shared__ double list_c[BEAM_LIST];           // and bins
     __shared__ Candidate list[BEAM_LIST];
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
             top = from_of(wave_max(q.from));
             v = -log2(wave_sum(q.sum * (double)part_of(q.from, top, LOG2E))) / (double)LOG2E;      // (the constant that the exponents were made with: what it is off by cancels)
         }
-        if ((lane & 63) == 0) { add[w] = v + (double)score; tops[w] = top; }
+        if ((lane & 63) == 0) { add[w] = v + (double)score; tops[w] = (double)top; }
     }
     if (lane == 0) count = 0;
     __syncthreads();
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_beam_join(BeamArgs a, int64_t 
             if (e.x == -INFINITY) return;
             const int w = e.id >> BEAM_SHIFT;
             const double v = add[w];
-            if (v - v == 0.) used |= f(Candidate{((double)e.x - (double)tops[w]) + v, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
+            if (v - v == 0.) used |= f(Candidate{((double)e.x - tops[w]) + v, e.x, w, (int32_t)(e.id & ((1u << BEAM_SHIFT) - 1))});
         };
         if constexpr (HELD) {
             used = false;
