@@ -349,7 +349,7 @@ typedef struct fc_dense fc_dense; /* opaque: stream, workspace, sticky error; on
 /* On the current device; hip_stream: hipStream_t (NULL = default stream) of all its calls. */
 int dense_create(void* hip_stream, fc_dense** out);
 /* Allocate now what calls up to these sizes need beyond the caller's memory: token_embed_bwd of max_tokens ids and a table of max_rows rows of max_dim
- * columns, rms_norm_bwd of any number of rows of max_dim columns, grad_norm_clip of max_tensors tensors; distill_* and beam_* of any sizes where max_dim > 0.  What token_embed_bwd needs grows with
+ * columns, rms_norm_bwd of any number of rows of max_dim columns, grad_norm_clip of max_tensors tensors; distill_* and beam_* of any sizes (5 MB) where max_dim > 0.  What token_embed_bwd needs grows with
  * max_tokens * max_dim: a wide norm beside a narrow table is better reserved by a call of its own (max_tokens 0), as the workspace keeps the larger of
  * the two.  Optional: the workspace grows on demand, which costs a hipMalloc and a device-wide
  * synchronisation in that call, and is refused (FC_ERR_HIP) while the stream is captured into a graph; buffers that a captured call uses stay
@@ -426,7 +426,7 @@ int distill_fwd(fc_dense* d, const void* logits_dev, int32_t type, int64_t logit
 int distill_bwd(fc_dense* d, const float* grad_loss_dev, int64_t grad_loss_stride, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t n, int32_t dim,
                 const void* teacher_ids_dev, int32_t id_type, const void* teacher_dev, int32_t teacher_type, int32_t top, const void* targets_dev, int32_t target_type,
                 float temperature, float alpha, const float* stats_dev, void* grad_logits_dev, int64_t grad_logits_stride);
-/* Both in one call, where grad_loss is known beforehand (1 / n for a mean): the same loss and gradient. */
+/* Both in one call, where grad_loss is known beforehand (1 / n for a mean): the same loss and gradient but for the roundings of sums, which are added up in another order for some sizes. */
 int distill_grad(fc_dense* d, const float* grad_loss_dev, int64_t grad_loss_stride, const void* logits_dev, int32_t type, int64_t logits_stride, int64_t n, int32_t dim,
                  const void* teacher_ids_dev, int32_t id_type, const void* teacher_dev, int32_t teacher_type, int32_t top, const float* teacher_lse_dev,
                  const void* targets_dev, int32_t target_type, float temperature, float alpha, float* loss_dev, void* grad_logits_dev, int64_t grad_logits_stride);

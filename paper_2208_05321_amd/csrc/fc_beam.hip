@@ -5,14 +5,18 @@
 //
 // Within a beam the order is that of the logits, so a slice of a row (in registers, read once) gives its `keep` largest logits and its sum of
 // exponentials, and one workgroup for a sequence puts beams and slices together.  64 sequences of 8 beams of 131,072 bf16, the 16 best: 30 us for the first step, 4.5 TB/s; it reads
-// each logit once and writes 8 bytes of lists a candidate, but an exponential and a comparison of each element keep the vector units busy for about two thirds of that time.  The second
-// step takes 6 us, and one sequence of 4 beams 5.2 and 3.7: what waits for one another there are a few accesses.
+// each logit once and writes 8 bytes of lists a candidate.  An exponential and a comparison of each element keep the vector units busy for 49 % of that time, by their counters; wavefronts, four a SIMD, wait
+// for memory or for one another for 40 % of theirs, and 31 % for their turn: loads and arithmetic hardly overlap.  The second step takes 6 us, and one sequence of 4 beams 5.2 and 3.5: what waits for one
+// another there are a few accesses.
 // The candidates are put in order in 64 bits.  What they are made of holds less: exponentials, and the sum of those that a lane has, are in 32 bits, and only lanes, wavefronts and slices are
 // added up in 64, so that a log-sum is off by some 1e-7 (an element's exponential is one instruction in 32 bits and a function in 64).  Candidates of one beam have it in common; those of
 // different beams that are closer than that may change places.
 //
 // The `keep` largest of a workgroup's elements: those above a bound that is no larger than the `keep`-th largest are few, and are ranked by
-// counting.  The bound comes of the lanes' largest elements, by ballots.
+// counting.  The bound comes of the lanes' largest elements, by ballots, and holds the upper 16 bits of their keys: 7 bits behind the first one.  Where it does not keep all but 1024 elements of a workgroup away its
+// slices are read again for each one kept, which takes milliseconds: where fewer ids than that are not masked by a finite value, where very many logits are equal, or where f32 logits lie close together for their
+// size.  us, 64 sequences of 8 beams of 131,072, 16 / 64 kept: bf16 34 / 56, with all but 8 ids at -1e9 1565 / 5900, all equal 1575 / 5900; f32 with a spread of 3, 16 kept, 51, about 100 51, about 1000
+// 1370, about 30,000 1640; one sequence of 4 beams, f32, 4 kept, 12.7, about 1000 19, with all but 8 ids masked, 16 kept, 38.
 #include "logits_device.h"
 
 #include <algorithm>
@@ -192,7 +196,7 @@ __global__ __launch_bounds__(LOGIT_THREADS) void k_beam_slice(BeamArgs a, int64_
             if (rank < a.keep && (lane & 7) == 0) put(rank, key);
         }
         for (int i = got + lane; i < a.keep; i += LOGIT_THREADS) out[i * all] = BeamEntry{-INFINITY, 0};
-    } else {                                       // (as good as equal logits)
+    } else {                                       // (more than BEAM_LIST have the key's upper bits in common with the least of those that are kept)
         uint64_t last = ~0ull;
         for (int i = 0; i < a.keep; ++i) {
             uint64_t mine = 0;

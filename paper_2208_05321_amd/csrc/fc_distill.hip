@@ -7,8 +7,8 @@
 //   d/dx_v = a T [c Q_v - sum of P_k with t_k = v] + (1 - a) [softmax(x)_v - (v = y)] for a named v, c = sum P_k + P_0
 //            a T [c Q_v - P_0 Q_v / Q_0]           + (1 - a) [softmax(x)_v - (v = y)] for the others
 //
-// A slice of a row is in registers, so each pass reads the logits once: HBM bounds it.  8192 rows of 131,072 bf16, loss: 319 us, 6.7 TB/s; loss and gradient together of 16,384 rows of
-// 32,768, each read once and written once: 427 us, 5.0 TB/s (rows wait in registers for their sums); of 4096 rows of 131,072 in two passes 555 us, the second 353, 6.1 TB/s.  With P_0 the sums over the ids that are not named are kept apart from those
+// A slice of a row is in registers, so each pass reads the logits once: HBM bounds it.  Times of calls: 8192 rows of 131,072 bf16, loss: 330 us, 6.5 TB/s; loss and gradient together of
+// 16,384 rows of 32,768, each read once and written once: 412 us, 5.2 TB/s (rows wait in registers for their sums); of 4096 rows of 131,072 in two passes 560 us, of which the second kernel 356, 6.0 TB/s.  With P_0 the sums over the ids that are not named are kept apart from those
 // over the named ones, each relative to its own largest element, so that neither is a difference of nearly equal numbers nor lost below the other.
 // The gradient of the others is then one product with an exponential; the entries and the target are mended afterwards, from their own formula.
 #include "logits_device.h"
@@ -355,7 +355,7 @@ constexpr int distill_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 // Rows that LANES lanes hold: the loss, and the gradient too if it is wanted (grad), which may take the place of the logits: a row is read before any of it is written.  The row waits in
 // registers while one wavefront works on its entries, so what counts is how many rows a compute unit holds: 80 registers and three rows of 64 KB, or four of 48, though some
-// 40 bytes of a lane then go through memory (16,384 rows of 32,768 bf16: 4 to 8 wavefronts a SIMD 532 / - / 446 / 490 / 586 us).
+// 30 bytes of a lane then go through memory (16,384 rows of 32,768 bf16, 4 to 8 wavefronts a SIMD: 475 / 475 / 412 / 471 / 549 us; at temperature 2 580 / 578 / 448 / 524 / 572).
 template <class T, int LANES, int PER>
 __global__ __launch_bounds__(distill_threads(LANES)) __attribute__((amdgpu_waves_per_eu(LANES > 512 ? 4 : LANES == 512 && PER == 6 ? 8 : 6))) void k_distill_row(DistillArgs a, bool stream, const float* __restrict__ grad_loss, int64_t grad_loss_stride, float* __restrict__ loss,
                                                                         float* __restrict__ stats, T* grad, int64_t grad_stride) {
@@ -535,7 +535,7 @@ constexpr size_t DISTILL_WORK = DISTILL_SLICES * (sizeof(RowSums) + STATS * size
 size_t distill_work_bytes() { return DISTILL_WORK; }
 
 // f(lanes of a slice, vectors of a lane), as constants, for the gradient of n rows of `vectors`.  Slices of 4 vectors a lane, or of 2 where those are fewer than four workgroups a
-// compute unit.  us, 8 / 4: 4096 rows of 131,072 bf16 363 / 353, 2000 182 / 170, 3000 of 50,021 155 / 115, 777 f16 38 / 31, 8000 of 30,000 bf16 165 / 161.
+// compute unit.  us, 2 / 4: 32 rows of 131,072 bf16 (512 workgroups of 4) 6.9 / 7.4, 63 10.0 / 10.7, 96 13.6 / 13.4.  us, 8 / 4: 4096 rows of 131,072 bf16 363 / 353, 2000 182 / 170, 3000 of 50,021 155 / 115, 777 f16 38 / 31, 8000 of 30,000 bf16 165 / 161.
 template <class F>
 void by_slice(int64_t n, int64_t vectors, F f) {
     using std::integral_constant;
@@ -545,7 +545,7 @@ void by_slice(int64_t n, int64_t vectors, F f) {
     else f(integral_constant<int, 256>(), integral_constant<int, 4>());
 }
 // f(vectors of a lane) for the sums of rows of more than 1024 vectors.  Slices of 8, or of 4 where the last one of 8 would be half empty, or more, among five at most, or of 2
-// where there are few.  us, 8 / 4: 4096 rows of 131,072 bf16 193 / 215, 8000 of 30,000 77 / 94, 4000 of 100,000 f32 228 / 240, but 3000 of 50,021 bf16 75 / 60.
+// where there are few.  us, 2 / 8: 16 rows of 131,072 bf16 (128 slices of 8) 3.6 / 4.0, 32 4.4 / 4.2, 63 6.7 / 6.5, 96 8.7 / 8.0: the two are alike from 256 on.  us, 8 / 4: 4096 rows of 131,072 bf16 193 / 215, 8000 of 30,000 77 / 94, 4000 of 100,000 f32 228 / 240, but 3000 of 50,021 bf16 75 / 60.
 template <class F>
 void by_part(int64_t n, int64_t vectors, F f) {
     using std::integral_constant;
@@ -597,11 +597,15 @@ struct DistillCall {
     bool fwd, bwd;
 };
 
+// Rows below which the gradient's kernel joins the slices, and no workgroup of 1024 takes a row.  us a call, joined by it / by a kernel of its own / whole rows: temperature 2, 131,072 bf16: one row 14.4 / 17.4,
+// 32 14.2 / 17.8, 63 18.5 / 21.5, 128 27.6 / 31.1, 256 47.3 / 47.8; temperature 1: 32 13.5 / 15.9 / 20.4, 64 17.3 / 21.5 / 22.6, 96 20.7 / 24.6 / 25.3, 128 23.6 / 27.5 / 27.4, 256 42.1 / 42.6 / 36.8: the gradient's
+// kernel is ahead up to some 200 rows.
 constexpr int64_t DISTILL_FEW = 64;
 // Whether a workgroup takes a whole row, in one launch, or rows are cut into slices.  Loss and gradient: rows of up to 4096 vectors; larger ones, of which a compute unit holds two or
 // one, only where they leave few lanes idle and have one exponential an element (nothing else runs while a workgroup works).  us, whole rows / slices, bf16: 16,384 rows of 32,768 430 / 564,
 // 4000 of 20,000 95 / 116; one exponential: 4000 of 131,072 476 / 504, 300 of 65,536 30 / 33, 4000 of 60,000 271 / 253 (f32, 2000 of 30,000, 114 / 129), of 50,021 335 / 268;
-// two exponentials: 4000 of 131,072 582 / 533, of 65,536 314 / 276.  The loss alone: 16,000 rows of 16,000 bf16 130 / 116, of 30,000 230 / 178, but 100 of 30,000 11.7 / 14.7.
+// two exponentials: 4000 of 131,072 582 / 533, of 65,536 314 / 276.  The loss alone: 16,000 rows of 16,000 bf16 130 / 116, of 30,000 230 / 178, but 256 of 30,000
+// 10.7 / 12.8, 1024 17.0 / 20.2, 2048 30.9 / 32.7, 4000 52.6 / 54.0, and of 16,000 12.1 / 15.2 (1024), 29.3 / 36.0 (4000): the two meet beyond 4000 rows.
 static bool in_one_workgroup(const DistillCall& c, int64_t vectors) {
     if (!c.bwd) return vectors <= 256 * 4 || (vectors <= 512 * 8 && c.a.n <= 1024);
     if (vectors <= 512 * 8) return true;

@@ -14,8 +14,8 @@ namespace fc {
 constexpr int STATE_THREADS = 256;
 constexpr int STATE_MOST_BEAMS = 64;
 constexpr int STATE_GROUP = 44;                    // tensors that one launch's arguments can describe
-// Vectors of 16 bytes of a row that a workgroup moves, for every beam.  us, 256 / 512 / 1024: 16 sequences of 8 beams, 24 tensors of 512 KB a row in place 438 / 447 / 456, one
-// sequence of 4 beams (17 tensors of 30 KB; host) 20.5 / 20.7 / 20.5.
+// Vectors of 16 bytes of a row that a workgroup moves, for every beam.  us, 64 / 128 / 256 / 512 / 1024: 16 sequences of 8 beams, 24 tensors of 512 KB a row in place 458 / 433 / 440 / 449 / 457, one
+// sequence of 4 beams (17 tensors of 30 KB; host) 20.4 each.
 constexpr int STATE_TILE = 256;
 struct StateRows {
     const char* src;
@@ -140,8 +140,9 @@ int beam_reorder(fc_dense* d, const fc_state* states, int32_t count, int64_t bat
         bytes += states[k].piece_bytes * states[k].pieces * batch * keep;
         in_place |= states[k].src == states[k].dst;
     }
-    // What the memory-side cache would not hold until it is read is stored past it: 16 x 8 rows of 512 KB of 24 tensors (1.6 GB) 446 / 434 us.  (Loads past it as well: 4 % more, as
-    // a row may have several takers.)
+    // What the memory-side cache would not hold until it is read is stored past it.  us, stores through / past the caches, rows of 512 KB in place: 32 MB 19.5 / 19.8, 64 MB 42.8 / 36.1, 128 MB 79.6 / 76.8, 192 MB
+    // 115.9 / 112.5, 512 MB 306 / 299; into others 26.3 / 26.4, 44.6 / 38.1, 83.0 / 76.9, 119.4 / 111.2, 324 / 304: below 128 MB the line goes by the next reader, who finds them there.  (Loads past the caches as
+    // well, beyond 128 MB: into others 3 % more, as a row may have several takers; in place 9 % less, 440 / 401 for 1.6 GB of 24 tensors, which is not made use of.)
     const bool stream = bytes > (int64_t)128 << 20;
     StateGroup g;
     g.count = 0;
